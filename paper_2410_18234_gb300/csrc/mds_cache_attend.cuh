@@ -1,0 +1,304 @@
+// What the attention kernels over the paged cache share: the parameters, the
+// line of key tiles that the blocks of a grid divide among themselves, bounded
+// waits, and the join of pieces.
+//
+// Rows.  The g query heads that share a key/value head and the nodes of a
+// tree read the same cache: row r = node * g + head of the group.  Work is cut
+// into (sequence, key/value head, tile of rows) groups of key tiles of 128
+// slots; all groups' tiles lie on one line that the blocks of the grid (one
+// per SM) share evenly, so ragged lengths and few sequences load every SM.  A
+// group cut between blocks is joined by the last of them to finish, which
+// adds the pieces in their order: results do not depend on timing.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "mds_cache_internal.h"
+#include "mds_device.cuh"
+
+namespace mds {
+namespace cache {
+namespace {
+
+using dev::bulk_copy;
+using dev::ex2;
+using dev::mbar_arrive;
+using dev::mbar_expect_tx;
+using dev::mbar_init;
+using dev::mbar_init_fence;
+using dev::smem_u32;
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr int kTile = 128;                 // slots of a key tile
+constexpr float kNone = -1e30f;            // reference of a row that has seen nothing
+constexpr float kSlack = 32.f;             // the reference moves when a weight passes 2^32
+constexpr unsigned kWaitTries = 1u << 18;
+
+struct Params {
+  State s;
+  Attend a;
+  int g, rows, row_tiles, stages;
+  int rows_per;            // rows of a row tile
+};
+
+// A sequence's part of the call.
+struct Seq {
+  int q, len, live, end;   // id, committed, live nodes, slots held (a slot behind it is not read)
+};
+
+// A group's key tiles: `sink` tiles from slot 0, then those from `first` on.
+struct Group {
+  int lo, sinks, hi;       // slots seen by a row of the tile: [0, sinks) and [lo, hi)
+  int sink_tiles, first, tiles;
+};
+
+__device__ __forceinline__ Group group_of(const Params& p, const Seq& q, int rt) {
+  Group r;
+  const int i0 = rt * p.rows_per / p.g, i1 = min((rt * p.rows_per + p.rows_per - 1) / p.g, q.live - 1);
+  r.tiles = 0;
+  r.hi = r.lo = r.sinks = r.sink_tiles = r.first = 0;
+  if (i0 >= q.live) return r;
+  r.hi = min(q.len + i1 + 1, q.end);
+  if (p.a.window > 0) {
+    // a chain's node is at its own position; a branch's first node at depth 1
+    const int64_t pos = (int64_t)q.len + (p.a.n - 1 <= p.a.L ? i0 : min(i0, 1));
+    r.lo = (int)min(max(pos - p.a.window + 1, (int64_t)0), (int64_t)q.len);
+    r.sinks = min(p.a.sinks, r.lo);
+  }
+  r.first = r.lo / kTile;
+  r.sink_tiles = min((r.sinks + kTile - 1) / kTile, r.first);
+  r.tiles = r.sink_tiles + max((r.hi + kTile - 1) / kTile - r.first, 0);
+  return r;
+}
+
+__device__ __forceinline__ int tile_slot(const Group& r, int i) {
+  return (i < r.sink_tiles ? i : r.first + i - r.sink_tiles) * kTile;
+}
+
+// Whether any row of the tile sees a slot of the block of 16 from t on.
+__device__ __forceinline__ bool block_seen(const Group& r, int t) {
+  return t < r.hi && (t + kBlock > r.lo || t < r.sinks);
+}
+
+// A wait on a barrier gives up after kWaitTries tries, and at once after
+// another wait of the block has.  A try suspends the thread for up to 20 us by
+// itself; tries that return at once still make milliseconds, far beyond the
+// longest wait of a block for itself.  Kept short: the waits are a good part
+// of the kernels' code, which has to stay in the instruction cache.  A block
+// that gave up says so at its end (report).
+__device__ __forceinline__ bool try_wait(uint64_t* bar, unsigned parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+      : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ void wait(uint64_t* bar, unsigned parity, int* abort) {
+  unsigned i = 0;
+#pragma unroll 1
+  while (!try_wait(bar, parity)) {
+    if (++i > kWaitTries || *reinterpret_cast<volatile int*>(abort)) {
+      *reinterpret_cast<volatile int*>(abort) = 1;
+      break;
+    }
+  }
+}
+// By the thread that started the copies: whether the block gave up; then it
+// leaves the copies in flight time to land before the block ends.
+__device__ __noinline__ void report(int* abort, uint32_t* status) {
+  if (!*reinterpret_cast<volatile int*>(abort)) return;
+  atomicOr(status, MDS_ST_TIMEOUT);
+  for (int i = 0; i < 1000; ++i) __nanosleep(10000);
+}
+
+// Two e4m3 numbers as two halves.
+__device__ __forceinline__ void to_f16(unsigned x, unsigned& lo, unsigned& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(x));
+}
+// The even and the odd bytes of a word as two bfloat16 each: e4m3's exponent
+// and mantissa laid over bfloat16's are the number times 2^-120.
+__device__ __forceinline__ void to_bf16(unsigned x, unsigned& even, unsigned& odd) {
+  const unsigned e = ((x << 4) & 0x07f007f0u) | ((x << 8) & 0x80008000u);
+  const unsigned o = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(0x7b807b80u));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(0x7b807b80u));
+}
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+  unsigned r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// What a block of threads does next on the line of key tiles.
+struct Cursor {
+  int b, h, rt, off;
+};
+
+// The group and tile of unit u (whole warp).
+__device__ Cursor locate(const Params& p, const long long* prefix, const Seq* seqs, long long u) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = p.a.B - 1;
+  while (lo < hi) {   // the last b with prefix[b] <= u
+    const int mid = (lo + hi + 1) / 2;
+    if (prefix[mid] <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  Cursor c;
+  c.b = lo;
+  const long long per = (prefix[lo + 1] - prefix[lo]) / p.s.kv_heads;
+  const long long rem = u - prefix[lo];
+  c.h = (int)(rem / per);
+  long long in = rem % per;
+  const Seq q = seqs[lo];
+  for (int r0 = 0;; r0 += 32) {
+    const int rt = r0 + lane;
+    int t = rt < p.row_tiles ? group_of(p, q, rt).tiles : 0;
+    const int own = t;
+    for (int d = 1; d < 32; d *= 2) {
+      const int x = __shfl_up_sync(kFull, t, d);
+      if (lane >= d) t += x;
+    }
+    const unsigned past = __ballot_sync(kFull, t > in);
+    if (past || r0 + 32 >= p.row_tiles) {
+      const int at = past ? __ffs(past) - 1 : 31;
+      c.rt = r0 + at;
+      c.off = (int)in - (__shfl_sync(kFull, t, at) - __shfl_sync(kFull, own, at));
+      return c;
+    }
+    in -= __shfl_sync(kFull, t, 31);
+  }
+}
+
+// The next group that has tiles.  False past the end.
+__device__ bool advance(const Params& p, const Seq* seqs, Cursor& c, Group& grp) {
+  c.off = 0;
+  for (;;) {
+    if (++c.rt >= p.row_tiles || c.rt * p.rows_per / p.g >= seqs[c.b].live) {
+      c.rt = 0;
+      if (++c.h >= p.s.kv_heads) {
+        c.h = 0;
+        do {
+          if (++c.b >= p.a.B) return false;
+        } while (seqs[c.b].live <= 0);
+      }
+    }
+    grp = group_of(p, seqs[c.b], c.rt);
+    if (grp.tiles > 0) return true;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* out, float4 x);
+template <>
+__device__ __forceinline__ void store4<float>(float* out, float4 x) {
+  *reinterpret_cast<float4*>(out) = x;
+}
+template <>
+__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* out, float4 x) {
+  *reinterpret_cast<uint2*>(out) = uint2{pack_bf16(x.x, x.y), pack_bf16(x.z, x.w)};
+}
+
+// The plan, by all of the block's threads: seqs and the exclusive sums of
+// their tiles, and zeros in the rows of nodes that are not live.
+template <typename T>
+__device__ void plan(const Params& p, long long* prefix, Seq* seqs, int head_dim) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  for (int b = tid; b < p.a.B; b += blockDim.x) {
+    const int id = p.a.seqs[b];
+    Seq q{-1, 0, 0, 0};
+    if (id >= p.s.max_seqs) atomicOr(p.s.status, MDS_ST_BADSEQ);
+    else if (id >= 0) {
+      q.q = id;
+      q.len = p.s.lens[id];
+      q.live = p.a.counts ? min(max(p.a.counts[b], 0), p.a.n) : p.a.n;
+      q.end = p.s.held[id] << p.s.page_log;
+      if (q.len + q.live > q.end && q.live > 0) {
+        atomicOr(p.s.status, MDS_ST_BADSEQ);
+        q.live = min(q.live, max(q.end - q.len, 0));   // rows without a slot of their own are zeros
+      }
+    }
+    seqs[b] = q;
+  }
+  __syncthreads();
+  for (int b = warp; b < p.a.B; b += warps) {
+    const Seq q = seqs[b];
+    long long t = 0;
+    const int tiles = min(p.row_tiles, (q.live * p.g + p.rows_per - 1) / p.rows_per);
+    for (int rt = lane; rt < tiles; rt += 32) t += group_of(p, q, rt).tiles;
+    for (int d = 16; d; d /= 2) t += __shfl_xor_sync(kFull, t, d);
+    if (lane == 0) prefix[b + 1] = t * p.s.kv_heads;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    long long run = 0;
+    if (lane == 0) prefix[0] = 0;
+    for (int b0 = 0; b0 < p.a.B; b0 += 32) {
+      const int b = b0 + lane;
+      long long x = b < p.a.B ? prefix[b + 1] : 0;
+      for (int d = 1; d < 32; d *= 2) {
+        const long long y = __shfl_up_sync(kFull, x, d);
+        if (lane >= d) x += y;
+      }
+      if (b < p.a.B) prefix[b + 1] = run + x;
+      run += __shfl_sync(kFull, x, 31);
+    }
+  }
+  T* out = static_cast<T*>(p.a.out);
+  for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {
+    const int64_t row = (int64_t)p.a.heads * head_dim;
+    const int64_t from = ((int64_t)b * p.a.n + seqs[b].live) * row, to = (int64_t)(b + 1) * p.a.n * row;
+    for (int64_t i = from + tid * 4; i < to; i += blockDim.x * 4) store4(out + i, float4{0.f, 0.f, 0.f, 0.f});
+  }
+  __syncthreads();
+}
+
+// ---------------------------------------------------------- joining pieces
+//
+// A piece's partial sums: per row its reference, its normaliser, and D sums.
+// A block has two: of the group that it continues, and of the one that it
+// begins and another block ends.
+
+__device__ __forceinline__ float* piece_of(const Params& p, int block, bool begins, int head_dim) {
+  return p.s.part + ((int64_t)block * 2 + (begins ? 1 : 0)) * p.rows_per * (head_dim + 2);
+}
+
+// Where row `row` of head group h of sequence b of the list goes.
+template <typename T>
+__device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, int head_dim) {
+  const int64_t node = (int64_t)b * p.a.n + row / p.g;
+  return static_cast<T*>(p.a.out) + (node * p.a.heads + h * p.g + row % p.g) * head_dim;
+}
+
+// Add the pieces that blocks c0..c1 left of a row tile, in their order (256 threads).
+template <typename T, int D>
+__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, int tid) {
+  for (int x = tid; x < p.rows_per * (D / 4); x += 256) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
+    if (row / p.g >= live) continue;
+    auto piece = [&](int cc) { return piece_of(p, cc, cc == c0, D) + r * (D + 2); };
+    float top = kNone;
+    for (int cc = c0; cc <= c1; ++cc) top = fmaxf(top, __ldcg(piece(cc)));
+    float l = 0.f;
+    float4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int cc = c0; cc <= c1; ++cc) {
+      const float* pr = piece(cc);
+      const float2 y = __ldcg(reinterpret_cast<const float2*>(pr));
+      const float2 a = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d));
+      const float2 e = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d) + 1);
+      const float f = ex2(y.x - top);
+      l += y.y * f;
+      o.x += a.x * f, o.y += a.y * f, o.z += e.x * f, o.w += e.y * f;
+    }
+    const float inv = 1.f / l;
+    store4(out_row<T>(p, b, h, row, D) + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+  }
+}
+
+}  // namespace
+}  // namespace cache
+}  // namespace mds

@@ -1,18 +1,11 @@
-// Attention of draft-tree nodes over the 8-bit paged cache.
+// Attention of draft-tree nodes over the 8-bit paged cache, for few rows a
+// key/value head and for 32-bit queries; many rows: mds_cache_many.cu.
 //
 //   o_i = sum_t w_it v_t / sum_t w_it,   w_it = 2^(c q_i . k_t - m_i),   c = scale * log2(e)
 //
 // over the slots t that node i sees, m_i a running reference.  A block of 16
 // slots of one head has one scale 2^a for its keys and one 2^b for its
 // values: 2^a multiplies the block's scores, 2^b its weights.
-//
-// Rows.  The g query heads that share a key/value head and the nodes of a
-// tree read the same cache: row r = node * g + head of the group.  Work is cut
-// into (sequence, key/value head, tile of rows) groups of key tiles of 128
-// slots; all groups' tiles lie on one line that the blocks of the grid (one
-// per SM) share evenly, so ragged lengths and few sequences load every SM.  A
-// group cut between blocks is joined by the last of them to finish, which
-// adds the pieces in their order: results do not depend on timing.
 //
 // Products.  Every e4m3 number is exact in 16 bits, so products are taken in
 // 16 bits with 32-bit sums.  Keys meet queries in half precision: a row of
@@ -22,101 +15,16 @@
 // holds any 2^b: a 16-bit query's weight is rounded once (2^-9 relative, and
 // the normaliser sums the rounded weights, so that a row that sees one token
 // returns that token's value), a 32-bit one's is carried by three terms.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "mds_cache_internal.h"
-#include "mds_device.cuh"
+#include "mds_cache_attend.cuh"
 
 namespace mds {
 namespace cache {
 
 namespace {
 
-using dev::bulk_copy;
-using dev::ex2;
-using dev::mbar_arrive;
-using dev::mbar_expect_tx;
-using dev::mbar_init;
-using dev::mbar_init_fence;
-using dev::mbar_try_wait;
-using dev::smem_u32;
-
-constexpr unsigned kFull = 0xffffffffu;
 constexpr int kWarps = 8;                  // consumers; one more warp loads
-constexpr int kTile = 128;                 // slots of a key tile: 16 a consumer warp
 constexpr int kStageMax = 8;
 constexpr int kJoinStride = 80;            // floats of a joined row's 64 dimensions: rows 16 banks apart
-constexpr float kNone = -1e30f;            // reference of a row that has seen nothing
-constexpr float kSlack = 8.f;              // the reference moves when a score passes it by 2^8
-constexpr unsigned long long kWaitNs = 2000000000ull;
-
-struct Params {
-  State s;
-  Attend a;
-  int g, rows, row_tiles, grid, stages;
-};
-
-// A sequence's part of the call.
-struct Seq {
-  int q, len, live, end;   // id, committed, live nodes, slots held (a slot behind it is not read)
-};
-
-// A group's key tiles: `sink` tiles from slot 0, then those from `first` on.
-struct Group {
-  int lo, sinks, hi;       // slots seen by a row of the tile: [0, sinks) and [lo, hi)
-  int sink_tiles, first, tiles;
-};
-
-__device__ __forceinline__ Group group_of(const Params& p, const Seq& q, int rt, int rows_per) {
-  Group r;
-  const int i0 = rt * rows_per / p.g, i1 = min((rt * rows_per + rows_per - 1) / p.g, q.live - 1);
-  r.tiles = 0;
-  r.hi = r.lo = r.sinks = r.sink_tiles = r.first = 0;
-  if (i0 >= q.live) return r;
-  r.hi = min(q.len + i1 + 1, q.end);
-  if (p.a.window > 0) {
-    // a chain's node is at its own position; a branch's first node at depth 1
-    const int64_t pos = (int64_t)q.len + (p.a.n - 1 <= p.a.L ? i0 : min(i0, 1));
-    r.lo = (int)min(max(pos - p.a.window + 1, (int64_t)0), (int64_t)q.len);
-    r.sinks = min(p.a.sinks, r.lo);
-  }
-  r.first = r.lo / kTile;
-  r.sink_tiles = min((r.sinks + kTile - 1) / kTile, r.first);
-  r.tiles = r.sink_tiles + max((r.hi + kTile - 1) / kTile - r.first, 0);
-  return r;
-}
-
-__device__ __forceinline__ int tile_slot(const Group& r, int i) {
-  return (i < r.sink_tiles ? i : r.first + i - r.sink_tiles) * kTile;
-}
-
-// Whether any row of the tile sees a slot of the block of 16 from t on.
-__device__ __forceinline__ bool block_seen(const Group& r, int t) {
-  return t < r.hi && (t + kBlock > r.lo || t < r.sinks);
-}
-
-__device__ __forceinline__ unsigned long long now_ns() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-
-// A wait on a barrier gives up after kWaitNs, and at once after another has.
-__device__ __noinline__ void wait_long(uint64_t* bar, unsigned parity, int* abort, uint32_t* status) {
-  const unsigned long long until = now_ns() + kWaitNs;
-  while (!*reinterpret_cast<volatile int*>(abort)) {
-    for (int i = 0; i < 16; ++i)
-      if (mbar_try_wait(bar, parity)) return;
-    if (now_ns() > until) {
-      *reinterpret_cast<volatile int*>(abort) = 1;
-      atomicOr(status, MDS_ST_TIMEOUT);
-    }
-  }
-}
-__device__ __forceinline__ void wait(uint64_t* bar, unsigned parity, int* abort, uint32_t* status) {
-  if (!mbar_try_wait(bar, parity)) wait_long(bar, parity, abort, status);
-}
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -133,154 +41,11 @@ __device__ __forceinline__ void mma_bf16(float* c, const unsigned* a, unsigned b
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Two e4m3 numbers as two halves.
-__device__ __forceinline__ void to_f16(unsigned x, unsigned& lo, unsigned& hi) {
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-      : "=r"(lo), "=r"(hi)
-      : "r"(x));
-}
-// The even and the odd bytes of a word as two bfloat16 each: e4m3's exponent
-// and mantissa laid over bfloat16's are the number times 2^-120.
-__device__ __forceinline__ void to_bf16(unsigned x, unsigned& even, unsigned& odd) {
-  const unsigned e = ((x << 4) & 0x07f007f0u) | ((x << 8) & 0x80008000u);
-  const unsigned o = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(0x7b807b80u));
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(0x7b807b80u));
-}
 __device__ __forceinline__ void ldmatrix_x4_trans(unsigned* r, unsigned addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr));
 }
-__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
-  unsigned r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-// What a block of threads does next on the line of key tiles.
-struct Cursor {
-  int b, h, rt, off;
-};
-
-// The group and tile of unit u (whole warp).
-__device__ Cursor locate(const Params& p, const long long* prefix, const Seq* seqs, long long u, int rows_per) {
-  const int lane = threadIdx.x & 31;
-  int lo = 0, hi = p.a.B - 1;
-  while (lo < hi) {   // the last b with prefix[b] <= u
-    const int mid = (lo + hi + 1) / 2;
-    if (prefix[mid] <= u) lo = mid;
-    else hi = mid - 1;
-  }
-  Cursor c;
-  c.b = lo;
-  const long long per = (prefix[lo + 1] - prefix[lo]) / p.s.kv_heads;
-  const long long rem = u - prefix[lo];
-  c.h = (int)(rem / per);
-  long long in = rem % per;
-  const Seq q = seqs[lo];
-  for (int r0 = 0;; r0 += 32) {
-    const int rt = r0 + lane;
-    int t = rt < p.row_tiles ? group_of(p, q, rt, rows_per).tiles : 0;
-    const int own = t;
-    for (int d = 1; d < 32; d *= 2) {
-      const int x = __shfl_up_sync(kFull, t, d);
-      if (lane >= d) t += x;
-    }
-    const unsigned past = __ballot_sync(kFull, t > in);
-    if (past || r0 + 32 >= p.row_tiles) {
-      const int at = past ? __ffs(past) - 1 : 31;
-      c.rt = r0 + at;
-      c.off = (int)in - (__shfl_sync(kFull, t, at) - __shfl_sync(kFull, own, at));
-      return c;
-    }
-    in -= __shfl_sync(kFull, t, 31);
-  }
-}
-
-// The next group that has tiles.  False past the end.
-__device__ bool advance(const Params& p, const Seq* seqs, Cursor& c, Group& grp, int rows_per) {
-  c.off = 0;
-  for (;;) {
-    if (++c.rt >= p.row_tiles || c.rt * rows_per / p.g >= seqs[c.b].live) {
-      c.rt = 0;
-      if (++c.h >= p.s.kv_heads) {
-        c.h = 0;
-        do {
-          if (++c.b >= p.a.B) return false;
-        } while (seqs[c.b].live <= 0);
-      }
-    }
-    grp = group_of(p, seqs[c.b], c.rt, rows_per);
-    if (grp.tiles > 0) return true;
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T* out, float4 x);
-template <>
-__device__ __forceinline__ void store4<float>(float* out, float4 x) {
-  *reinterpret_cast<float4*>(out) = x;
-}
-template <>
-__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* out, float4 x) {
-  *reinterpret_cast<uint2*>(out) = uint2{pack_bf16(x.x, x.y), pack_bf16(x.z, x.w)};
-}
-
-// The plan, by all of the block's threads: seqs and the exclusive sums of
-// their tiles, and zeros in the rows of nodes that are not live.
-template <typename T>
-__device__ void plan(const Params& p, long long* prefix, Seq* seqs, int rows_per, int head_dim) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  for (int b = tid; b < p.a.B; b += blockDim.x) {
-    const int id = p.a.seqs[b];
-    Seq q{-1, 0, 0, 0};
-    if (id >= p.s.max_seqs) atomicOr(p.s.status, MDS_ST_BADSEQ);
-    else if (id >= 0) {
-      q.q = id;
-      q.len = p.s.lens[id];
-      q.live = p.a.counts ? min(max(p.a.counts[b], 0), p.a.n) : p.a.n;
-      q.end = p.s.held[id] << p.s.page_log;
-      if (q.len + q.live > q.end && q.live > 0) {
-        atomicOr(p.s.status, MDS_ST_BADSEQ);
-        q.live = min(q.live, max(q.end - q.len, 0));   // rows without a slot of their own are zeros
-      }
-    }
-    seqs[b] = q;
-  }
-  __syncthreads();
-  for (int b = warp; b < p.a.B; b += warps) {
-    const Seq q = seqs[b];
-    long long t = 0;
-    const int tiles = min(p.row_tiles, (q.live * p.g + rows_per - 1) / rows_per);
-    for (int rt = lane; rt < tiles; rt += 32) t += group_of(p, q, rt, rows_per).tiles;
-    for (int d = 16; d; d /= 2) t += __shfl_xor_sync(kFull, t, d);
-    if (lane == 0) prefix[b + 1] = t * p.s.kv_heads;
-  }
-  __syncthreads();
-  if (warp == 0) {
-    long long run = 0;
-    if (lane == 0) prefix[0] = 0;
-    for (int b0 = 0; b0 < p.a.B; b0 += 32) {
-      const int b = b0 + lane;
-      long long x = b < p.a.B ? prefix[b + 1] : 0;
-      for (int d = 1; d < 32; d *= 2) {
-        const long long y = __shfl_up_sync(kFull, x, d);
-        if (lane >= d) x += y;
-      }
-      if (b < p.a.B) prefix[b + 1] = run + x;
-      run += __shfl_sync(kFull, x, 31);
-    }
-  }
-  T* out = static_cast<T*>(p.a.out);
-  for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {
-    const int64_t row = (int64_t)p.a.heads * head_dim;
-    const int64_t from = ((int64_t)b * p.a.n + seqs[b].live) * row, to = (int64_t)(b + 1) * p.a.n * row;
-    for (int64_t i = from + tid * 4; i < to; i += blockDim.x * 4) store4(out + i, float4{0.f, 0.f, 0.f, 0.f});
-  }
-  __syncthreads();
-}
-
 // ------------------------------------------------------- few rows: 16 or 32
 //
 // Each consumer warp takes one block of 16 slots of a tile for all the rows:
@@ -338,14 +103,14 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
     }
     mbar_init_fence();
   }
-  plan<T>(p, prefix, seqs, F::kRows, D);   // ends in a barrier
+  plan<T>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B];
   const long long per = (total + gridDim.x - 1) / gridDim.x;
   const long long u0 = per * blockIdx.x, u1 = min(u0 + per, total);
   if (u0 >= u1) return;
 
-  Cursor c = locate(p, prefix, seqs, u0, F::kRows);
-  Group grp = group_of(p, seqs[c.b], c.rt, F::kRows);
+  Cursor c = locate(p, prefix, seqs, u0);
+  Group grp = group_of(p, seqs[c.b], c.rt);
   long long u = u0;
 
   if (warp == kWarps) {
@@ -366,7 +131,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
       for (int i = c.off; i < c.off + cnt; ++i) {
         const int next = page_of(i + 1);
         const int t = tile_slot(grp, i) + blk * kBlock;
-        wait(empty + stage, phase, abort, s.status);
+        wait(empty + stage, phase, abort);
         const unsigned takes = __ballot_sync(kFull, page >= 0);
         if (lane == 0) mbar_expect_tx(full + stage, __popc(takes) * kBlock * D);
         __syncwarp();
@@ -385,10 +150,9 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
         if (++stage == p.stages) stage = 0, phase ^= 1u;
       }
       u += cnt;
-      if (u < u1 && !advance(p, seqs, c, grp, F::kRows)) break;
+      if (u < u1 && !advance(p, seqs, c, grp)) break;
     }
-    if (*reinterpret_cast<volatile int*>(abort))   // a wait gave up: leave the copies in flight time to land
-      for (int i = 0; i < 1000; ++i) __nanosleep(10000);
+    report(abort, s.status);
     return;
   }
 
@@ -484,7 +248,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
 
     for (int i = c.off; i < c.off + cnt; ++i) {
       const int t0 = tile_slot(grp, i) + warp * kBlock;
-      wait(full + stage, phase, abort, p.s.status);
+      wait(full + stage, phase, abort);
       if (block_seen(grp, t0)) {
         const char* kb = stage_mem + stage * F::kStageBytes + warp * kBlock * D;
         const unsigned vb = smem_u32(kb + kTile * D);
@@ -627,10 +391,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
     const bool whole = c.off == 0 && cnt == grp.tiles;
     const long long g0 = u - c.off;                       // the group's first unit
     const int c0 = (int)(g0 / per), c1 = (int)((g0 + grp.tiles - 1) / per);
-    constexpr int kPart = F::kRows * (D + 2);
-    float* part = p.s.part + ((int64_t)blockIdx.x * 2 + (c.off ? 0 : 1)) * kPart;
-    T* out = static_cast<T*>(p.a.out) + (int64_t)c.b * p.a.n * p.a.heads * D;
-    auto out_row = [&](int row) { return out + ((int64_t)(row / p.g) * p.a.heads + c.h * p.g + row % p.g) * D; };
+    float* part = piece_of(p, blockIdx.x, c.off == 0, D);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       float f[2];
@@ -669,7 +430,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
           }
           if (whole) {
             const float inv = 1.f / l;
-            store4(out_row(row) + hd * 64 + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+            store4(out_row<T>(p, c.b, c.h, row, D) + hd * 64 + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
           } else {
             float* pr = part + (m * 16 + r) * (D + 2);
             __stcg(reinterpret_cast<float2*>(pr + 2 + hd * 64 + d), float2{o.x, o.y});
@@ -692,46 +453,24 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
       consumers_sync();
       if (*last_s) {
         __threadfence();
-        for (int x = tid; x < F::kRows * (D / 4); x += kWarps * 32) {
-          const int r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
-          if (row / p.g >= q.live) continue;
-          auto piece = [&](int cc) { return p.s.part + ((int64_t)cc * 2 + (cc == c0 ? 1 : 0)) * kPart + r * (D + 2); };
-          float top = kNone;
-          for (int cc = c0; cc <= c1; ++cc) top = fmaxf(top, __ldcg(piece(cc)));
-          float l = 0.f;
-          float4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-          for (int cc = c0; cc <= c1; ++cc) {
-            const float* pr = piece(cc);
-            const float2 y = __ldcg(reinterpret_cast<const float2*>(pr));
-            const float2 a = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d));
-            const float2 b = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d) + 1);
-            const float f = ex2(y.x - top);
-            l += y.y * f;
-            o.x += a.x * f, o.y += a.y * f, o.z += b.x * f, o.w += b.y * f;
-          }
-          const float inv = 1.f / l;
-          store4(out_row(row) + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
-        }
+        join_pieces<T, D>(p, c.b, c.h, row0, q.live, c0, c1, tid);
       }
     }
     u += cnt;
-    if (u < u1 && !advance(p, seqs, c, grp, F::kRows)) break;
+    if (u < u1 && !advance(p, seqs, c, grp)) break;
   }
 }
 
 template <typename T, int D, int MT>
 cudaError_t launch_few(const State& s, const Attend& a, int sms, cudaStream_t st) {
   using F = Few<T, D, MT>;
-  static_assert(2 * 152 * F::kRows * (D + 2) <= (int)kPartFloats, "partial sums");
-  Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, 0};
+  Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, F::kRows};
   p.rows = a.n * p.g;
   p.row_tiles = (p.rows + F::kRows - 1) / F::kRows;
-  p.grid = sms < kJoins ? sms : kJoins;
-  if ((size_t)2 * p.grid * F::kRows * (D + 2) > kPartFloats) p.grid = (int)(kPartFloats / (2 * F::kRows * (D + 2)));
+  const int grid = attend_grid(sms, F::kRows, D);
   p.stages = kStageMax;
   while (p.stages > 2 && F::smem(p.stages, a.B) > 227 * 1024) --p.stages;
-  few_kernel<T, D, MT><<<p.grid, 32 * (kWarps + 1), F::smem(p.stages, a.B), st>>>(p);
+  few_kernel<T, D, MT><<<grid, 32 * (kWarps + 1), F::smem(p.stages, a.B), st>>>(p);
   return cudaGetLastError();
 }
 
@@ -747,18 +486,19 @@ cudaError_t configure() {
   if (e == cudaSuccess) e = configure_few<float, 128, 1>();
   if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 64, 1>();
   if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 128, 1>();
-  if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 64, 2>();
-  if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 128, 2>();
+  if (e == cudaSuccess) e = configure_many();
   return e;
 }
 
+// Rows of 16-bit queries beyond one 16-row product go to the kernel of
+// mds_cache_many.cu.
 cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st) {
-  const bool wide = (int64_t)a.n * (a.heads / s.kv_heads) > 16;
+  const int64_t rows = (int64_t)a.n * (a.heads / s.kv_heads);
   if (s.dtype == MDS_F32)
     return s.head_dim == 64 ? launch_few<float, 64, 1>(s, a, sms, st) : launch_few<float, 128, 1>(s, a, sms, st);
-  if (s.head_dim == 64)
-    return wide ? launch_few<__nv_bfloat16, 64, 2>(s, a, sms, st) : launch_few<__nv_bfloat16, 64, 1>(s, a, sms, st);
-  return wide ? launch_few<__nv_bfloat16, 128, 2>(s, a, sms, st) : launch_few<__nv_bfloat16, 128, 1>(s, a, sms, st);
+  if (rows > 16) return attend_many(s, a, sms, st);
+  return s.head_dim == 64 ? launch_few<__nv_bfloat16, 64, 1>(s, a, sms, st)
+                          : launch_few<__nv_bfloat16, 128, 1>(s, a, sms, st);
 }
 
 }  // namespace cache

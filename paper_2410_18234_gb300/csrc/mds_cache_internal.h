@@ -1,6 +1,6 @@
 // Internal interface of the key/value cache (declared in
 // include/mds_cache.h) between its entry points (mds_cache_api.cu) and its
-// kernels (mds_cache_pages.cu, mds_cache_attend.cu).
+// kernels (mds_cache_pages.cu, mds_cache_few.cu, mds_cache_many.cu).
 #pragma once
 #include <cuda_runtime.h>
 
@@ -61,7 +61,15 @@ struct Attend {
   int layer, B, n, L, heads, window, sinks;
   float scale;
 };
-cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st);
+cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st);        // mds_cache_few.cu
+cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st);   // mds_cache_many.cu
+cudaError_t configure_many();
+// Blocks of an attention kernel: one per SM, as far as the partial sums reach.
+inline int attend_grid(int sms, int rows, int head_dim) {
+  const size_t most = kPartFloats / (2 * (size_t)rows * (head_dim + 2));
+  const int grid = sms < kJoins ? sms : kJoins;
+  return (size_t)grid < most ? grid : (int)most;
+}
 cudaError_t configure();          // kernel attributes, on the current device
 
 // Byte of (token row, dimension) inside a tile or a whole number of 128-byte lines of it.

@@ -1,0 +1,907 @@
+// Attention of draft-tree nodes over the 8-bit paged cache where 17 or more
+// rows (nodes x query heads) share a key/value head: trees with shared heads,
+// chunks of prompts.  The mathematics is that of mds_cache_few.cu; the
+// products run on the tensor cores with their accumulators in tensor memory.
+//
+// Transposed.  A tile of 128 slots meets up to 144 rows:
+//   S^T [128 slots][N rows]  = K [128][D] Q^T          (half precision)
+//   O^T [D][N rows]         += V^T [D][128] W^T        (bfloat16)
+// The slots and the head's dimensions fill the 128 rows that an instruction
+// always has; the attention's rows are its columns, which come in steps of 16:
+// 132 rows (33 nodes of 4 heads) cost 144 columns, where rows on the other
+// side would cost 256.  Keys are widened from 8 bits into tensor memory and
+// values into shared memory once for all rows, by four warps.  Eight warps
+// turn scores into weights, four for each half of the columns.  They read
+// fragments of 8 columns in which a thread holds 2 columns of 4 slots: a
+// column's reference, coefficient and running sum stay in registers, sums
+// over slots wait until the group ends, and a transposing store packs the
+// weights for the second product.
+//
+// Pipeline, tile t: load K, V (bulk copies) | widen K(t + 1), V(t) | S(t + 1)
+// into one of two buffers | weights(t) | O += V(t) W(t).
+//
+// Bound by shared memory: per tile, at D = 128 and N columns, 64 KB of 8-bit
+// rows in and out, 64 KB of wide values in and out, and 1 KB a column for
+// queries read and weights written and read: 220 KB for N = 144, 1760 cycles
+// at 128 bytes a cycle, against 1152 cycles of products and about 1400 for
+// the tile's bytes from HBM.
+#include "mds_cache_attend.cuh"
+
+namespace mds {
+namespace cache {
+
+namespace {
+
+constexpr int kThreads = 512;   // loader, products, memory, scheduler | 4 warps widen | 8 warps weigh
+constexpr int kMaxN = 144;      // columns: three buffers of them and 64 of keys in 512 of tensor memory
+constexpr int kSteps = kMaxN / 16;   // fragments of 8 columns in half of them
+constexpr int kRingMax = 5;
+constexpr int kScaleRing = 8;   // tiles whose scales are held: kRingMax + 3
+constexpr int kJobs = 4;        // groups the scheduler is ahead
+
+enum Bar {
+  kKFull = 0, kKEmpty = kKFull + kRingMax, kVFull = kKEmpty + kRingMax, kVEmpty = kVFull + kRingMax,
+  kWideK = kVEmpty + kRingMax, kWideKFree, kWideV, kWideVFree, kS, kSFree = kS + 2, kW = kSFree + 2,
+  kWFree = kW + 2, kQ = kWFree + 2, kOFree = kQ + 2, kJob, kJobFree = kJob + kJobs, kBars = kJobFree + kJobs
+};
+
+// ------------------------------------------------------------------- PTX
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* at) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(at)) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t addr) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(addr));
+}
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit_to(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+// Eight columns of 16 lanes: thread l has columns 2 (l % 4), + 1 of lane l / 4 (x, y) and of lane l / 4 + 8.
+__device__ __forceinline__ void tmem_ld_frag(float* r, uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st_frag(uint32_t addr, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(r[0]), "f"(r[1]),
+               "f"(r[2]), "f"(r[3])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_row8(float* r, uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st_row16(uint32_t addr, const unsigned* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+// The loaded registers are read after the wait.
+__device__ __forceinline__ void tmem_ld_wait(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7])::"memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void stmatrix_x4_trans(unsigned addr, const unsigned* r) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float b) {
+  unsigned long long r;
+  const float2 c{b, b};
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ void half_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
+__device__ __forceinline__ bool half_any(int half, bool x) {
+  unsigned r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(1 + half), "r"((unsigned)x)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void weigh_sync() { asm volatile("bar.sync 3, 256;" ::: "memory"); }
+
+// Shared-memory operands: rows of 128 bytes, their 16-byte units permuted
+// (unit ^= row mod 8); `lead` is the distance of blocks of 64 elements along
+// the contiguous axis where that axis is the operand's rows, 8 rows are 1024 bytes.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 |
+         2ull << 61;
+}
+// 32-bit sums; M = 128; type 0 half, 1 bfloat16; rows_first: A's contiguous axis is its rows.
+__device__ __forceinline__ uint32_t instruction(int n, uint32_t type, uint32_t rows_first) {
+  return 1u << 4 | type << 7 | type << 10 | rows_first << 15 | (uint32_t)(n >> 3) << 17 | 8u << 24;
+}
+
+struct Row {
+  int node, own;   // node, its branch's first node
+  int64_t out;     // its output's first element, -1: not one of the call's
+};
+
+// A group, or the block's piece of one, as the scheduler publishes it.
+struct Job {
+  int b, h, row0, off, cnt, tiles;             // cnt 0: the end
+  int q, len, live;                            // of the sequence
+  int first_block, last_block;                 // blocks of the grid that hold the group
+  Group grp;
+  __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
+};
+
+// Shared memory from a 1024-byte boundary on.
+struct Layout {
+  int q, w, wide_v, k_ring, v_ring, small, bytes;
+  int nk, nv;
+};
+__host__ __device__ inline Layout layout_of(int D, int N, int B) {
+  Layout l;
+  l.q = 0;
+  l.w = l.q + N * D * 2;
+  l.wide_v = l.w + 2 * N * 256;
+  l.k_ring = l.wide_v + 128 * D * 2;
+  const int small = kScaleRing * 16 * 4 + N * (2 * 16 + 8 + 2 * 8 + 8 + 24) + (kBars + 1) / 2 * 16 + kJobs * (int)sizeof(Job) + 16 + B * 16;
+  const int room = 227 * 1024 - 1024 - l.k_ring - small;
+  const int slots = room / (kTile * D);
+  l.nk = slots / 2 < kRingMax ? slots / 2 : kRingMax;
+  l.nv = slots - l.nk < kRingMax ? slots - l.nk : kRingMax;
+  l.v_ring = l.k_ring + l.nk * kTile * D;
+  l.small = l.v_ring + l.nv * kTile * D;
+  l.bytes = 1024 + l.small + small;
+  return l;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant__ Params p, int N) {
+  extern __shared__ char raw[];
+  char* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  const Layout lay = layout_of(D, N, p.a.B);
+  char* at = base + lay.small;
+  float* scales = reinterpret_cast<float*>(at);            // [kScaleRing][16]: keys' 8, values' 8
+  at += kScaleRing * 16 * 4;
+  Row* row_info = reinterpret_cast<Row*>(at);              // [2][N], by group
+  at += 2 * N * 16;
+  Seq* seqs = reinterpret_cast<Seq*>(at);
+  at += p.a.B * 16;
+  float2* stat = reinterpret_cast<float2*>(at);            // at the group's end: reference, normaliser
+  at += N * 8;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(at);
+  at += (kBars + 1) / 2 * 16;
+  float4* col_info = reinterpret_cast<float4*>(at);        // [2][N / 2]: two columns' coefficients, and references negated
+  at += 2 * N * 8;
+  int64_t* q_at = reinterpret_cast<int64_t*>(at);          // [N]: a row's query, from the sequence's first
+  at += N * 8;
+  float* red = reinterpret_cast<float*>(at);               // [4][N]: a column's maximum, later sum, by each warp
+  float* next = red + 4 * N;                               // [2][N]: references negated, factors of the sums
+  at += 6 * N * 4;
+  Job* jobs = reinterpret_cast<Job*>(at);
+  at += kJobs * sizeof(Job);
+  int* abort = reinterpret_cast<int*>(at);
+  int* last_s = abort + 1;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(abort + 2);
+  long long* prefix = reinterpret_cast<long long*>(base);  // before the queries and weights
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    *abort = 0;
+    for (int i = 0; i < kRingMax; ++i) {
+      mbar_init(bar + kKFull + i, 1 + 32);   // the loader's byte count, and its lanes' scale copies
+      mbar_init(bar + kKEmpty + i, 4);
+      mbar_init(bar + kVFull + i, 1);
+      mbar_init(bar + kVEmpty + i, 4);
+    }
+    mbar_init(bar + kWideK, 4);
+    mbar_init(bar + kWideKFree, 1);
+    mbar_init(bar + kWideV, 4);
+    mbar_init(bar + kWideVFree, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar + kS + i, 1);
+      mbar_init(bar + kSFree + i, 8);
+      mbar_init(bar + kW + i, 8);
+      mbar_init(bar + kWFree + i, 1);
+    }
+    mbar_init(bar + kQ, 4);
+    mbar_init(bar + kQ + 1, 4);
+    mbar_init(bar + kOFree, 8);
+    for (int i = 0; i < kJobs; ++i) {
+      mbar_init(bar + kJob + i, 1);
+      mbar_init(bar + kJobFree + i, 14);   // every warp but the scheduler's and the memory's
+    }
+    mbar_init_fence();
+  }
+  plan<__nv_bfloat16>(p, prefix, seqs, D);   // ends in a barrier
+  const long long total = prefix[p.a.B];
+  const long long per = (total + gridDim.x - 1) / gridDim.x;
+  const long long u0 = per * blockIdx.x, u1 = min(u0 + per, total);
+  if (u0 >= u1) return;
+  Cursor c{0, 0, 0, 0};
+  if (warp == 3) c = locate(p, prefix, seqs, u0);
+  if (warp == 2) tmem_alloc(tmem_at);
+  before_sync();
+  __syncthreads();   // the plan's sums have been read
+  after_sync();
+  const uint32_t tmem = *tmem_at;
+  const uint32_t t_s = tmem, t_o = tmem + 2 * N, t_k = tmem + 3 * N;
+  auto hold = [&](int b, unsigned parity) { wait(bar + b, parity, abort); };
+  // a role takes the jobs in turn
+  auto job_at = [&](int n) -> const Job& {
+    hold(kJob + (n & (kJobs - 1)), (n / kJobs) & 1);
+    return jobs[n & (kJobs - 1)];
+  };
+  auto job_done = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar + kJobFree + (n & (kJobs - 1)));
+  };
+
+  if (warp == 3) {
+    // ---- scheduler
+    Group grp = group_of(p, seqs[c.b], c.rt);
+    long long u = u0;
+    for (int n = 0;; ++n) {
+      hold(kJobFree + (n & (kJobs - 1)), ((n / kJobs) & 1) ^ 1);
+      const int cnt = u < u1 ? (int)min((long long)(grp.tiles - c.off), u1 - u) : 0;
+      if (lane == 0) {
+        Job& j = jobs[n & (kJobs - 1)];
+        j.cnt = cnt;
+        if (cnt) {
+          const Seq q = seqs[c.b];
+          j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
+          j.q = q.q, j.len = q.len, j.live = q.live;
+          j.first_block = (int)((u - c.off) / per);
+          j.last_block = (int)((u - c.off + grp.tiles - 1) / per);
+          j.grp = grp;
+        }
+        mbar_arrive(bar + kJob + (n & (kJobs - 1)));
+      }
+      __syncwarp();
+      if (!cnt) break;
+      u += cnt;
+      if (u < u1) advance(p, seqs, c, grp);
+    }
+  } else if (warp == 0) {
+    // ---- loader: one block of 16 slots a lane (keys: lanes 0..7, values: 8..15)
+    const State& s = p.s;
+    const int kv = (lane >> 3) & 1, blk = lane & 7;
+    const int64_t layer0 = (int64_t)p.a.layer * s.pages;
+    int tile = 0, ks = 0, vs = 0;
+    unsigned kp = 1, vp = 1;
+    for (int n = 0;; ++n) {
+      const Job& job = job_at(n);
+      const int end = job.off + job.cnt, h = job.h;
+      if (!job.cnt) break;
+      const Group grp = job.grp;
+      const int32_t* table = s.table + (int64_t)job.q * s.max_pages;
+      auto page_of = [&](int i) {
+        const int t = tile_slot(grp, i) + blk * kBlock;
+        return lane < 16 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
+      };
+      const int off = job.off;
+      // the queries are read by the time that the group's first tile is here
+      for (int r = lane; r < p.rows_per; r += 32) {
+        const int row = job.row0 + r, node = row / p.g;
+        if (node < job.live) {
+          const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + job.b * p.a.q_seq + node * p.a.q_tok +
+                                   (h * p.g + row - node * p.g) * p.a.q_head;
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+          if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+        }
+      }
+      job_done(n);
+      int page = page_of(off);
+      for (int i = off; i < end; ++i, ++tile) {
+        const int next = page_of(i + 1);
+        const int r = (tile_slot(grp, i) + blk * kBlock) & (s.page_tokens - 1);
+        const unsigned takes = __ballot_sync(kFull, page >= 0);
+        const int64_t row = (((layer0 + page) * 2 + kv) * s.kv_heads + h) * s.page_tokens + r;
+        hold(kKEmpty + ks, kp);
+        if (lane == 0) mbar_expect_tx(bar + kKFull + ks, __popc(takes & 0xffu) * kBlock * D);
+        __syncwarp();
+        if (page >= 0) {
+          if (!kv) bulk_copy(base + lay.k_ring + (ks * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kKFull + ks);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
+                           smem_u32(scales + (tile & (kScaleRing - 1)) * 16 + lane)),
+                       "l"(s.scales + (row >> 4))
+                       : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + kKFull + ks))
+                     : "memory");
+        hold(kVEmpty + vs, vp);
+        if (lane == 0) mbar_expect_tx(bar + kVFull + vs, __popc(takes & 0xff00u) * kBlock * D);
+        __syncwarp();
+        if (page >= 0 && kv)
+          bulk_copy(base + lay.v_ring + (vs * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kVFull + vs);
+        page = next;
+        if (++ks == lay.nk) ks = 0, kp ^= 1u;
+        if (++vs == lay.nv) vs = 0, vp ^= 1u;
+      }
+    }
+    report(abort, s.status);
+  } else if (warp == 1) {
+    // ---- products, issued by one thread: S(t + 1) before O(t)
+    const uint32_t id_s = instruction(N, 0, 0), id_o = instruction(N, 1, 1);
+    const uint32_t q_at = smem_u32(base + lay.q), w_at = smem_u32(base + lay.w), v_at = smem_u32(base + lay.wide_v);
+    int tile = 0, group = 0;
+    auto out_product = [&](int t, bool first) {
+      hold(kW + (t & 1), (t >> 1) & 1);
+      hold(kWideV, t & 1);
+      if (first) hold(kOFree, (group & 1) ^ 1);
+      after_sync();
+      if (lane == 0) {
+#pragma unroll 2
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ss(t_o, operand(v_at + k * 2048, 16384), operand(w_at + (t & 1) * N * 256 + (k >> 2) * N * 128 + (k & 3) * 32, 16),
+                 id_o, !(first && k == 0));
+        commit_to(bar + kWFree + (t & 1));
+        commit_to(bar + kWideVFree);
+      }
+      __syncwarp();
+    };
+    for (;;) {
+      const int cnt = job_at(group).cnt;
+      if (!cnt) break;
+      job_done(group);
+      hold(kQ + (group & 1), (group >> 1) & 1);
+      for (int i = 0; i < cnt; ++i, ++tile) {
+        hold(kWideK, tile & 1);
+        hold(kSFree + (tile & 1), ((tile >> 1) & 1) ^ 1);
+        after_sync();
+        if (lane == 0) {
+#pragma unroll 2
+          for (int k = 0; k < D / 16; ++k)
+            mma_ts(t_s + (tile & 1) * N, t_k + k * 8, operand(q_at + (k >> 2) * N * 128 + (k & 3) * 32, 16), id_s, k > 0);
+          commit_to(bar + kS + (tile & 1));
+          commit_to(bar + kWideKFree);
+        }
+        __syncwarp();
+        if (i > 0) out_product(tile - 1, i == 1);
+      }
+      out_product(tile - 1, cnt == 1);
+      ++group;
+    }
+  } else if (warp >= 4 && warp < 8) {
+    // ---- widen: keys a row a thread into tensor memory, values 16 dimensions
+    // of a slot at a time into shared memory.  Rows of blocks that were not
+    // loaded hold anything: their scores are masked, their values are zeros.
+    const int w4 = warp & 3, key = w4 * 32 + lane;
+    int ks = 0, vs = 0;
+    unsigned kp = 0, vp = 0;
+    const uint32_t k_to = t_k + ((uint32_t)(w4 * 32) << 16);
+    auto keys = [&](int t) {
+      hold(kKFull + ks, kp);
+      hold(kWideKFree, (t & 1) ^ 1);
+      after_sync();
+      const char* src = base + lay.k_ring + ks * kTile * D;
+#pragma unroll 1
+      for (int i = 0; i < D / 32; ++i) {
+        unsigned x[16];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint4 y = *reinterpret_cast<const uint4*>(src + swizzled(key * D + (2 * i + j) * 16));
+          to_f16(y.x, x[8 * j], x[8 * j + 1]);
+          to_f16(y.y, x[8 * j + 2], x[8 * j + 3]);
+          to_f16(y.z, x[8 * j + 4], x[8 * j + 5]);
+          to_f16(y.w, x[8 * j + 6], x[8 * j + 7]);
+        }
+        tmem_st_row16(k_to + i * 16, x);
+      }
+      tmem_st_wait();
+      before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar + kKEmpty + ks);
+        mbar_arrive(bar + kWideK);
+      }
+      if (++ks == lay.nk) ks = 0, kp ^= 1u;
+    };
+    // seen: bit i of the tile's blocks (two a warp)
+    auto values = [&](int t, unsigned seen) {
+      hold(kVFull + vs, vp);
+      hold(kWideVFree, (t & 1) ^ 1);
+      const char* src = base + lay.v_ring + vs * kTile * D;
+      char* dst = base + lay.wide_v;
+      constexpr int kChunks = D / 16;
+#pragma unroll 2
+      for (int it = 0; it < kChunks; ++it) {
+        const int pair = it * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+        const int k = w4 * 32 + octet * 8 + (lane & 7);
+        uint4 y = *reinterpret_cast<const uint4*>(src + swizzled(k * D + chunk * 16));
+        if (!(seen >> (k >> 4) & 1u)) y = uint4{0, 0, 0, 0};
+        uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
+        to_bf16(y.x, a.x, a.y);
+        to_bf16(y.y, a.z, a.w);
+        to_bf16(y.z, b.x, b.y);
+        to_bf16(y.w, b.z, b.w);
+        char* line = dst + (chunk >> 2) * 16384 + k * 128;
+        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2) ^ (k & 7)) << 4)) = a;
+        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2 + 1) ^ (k & 7)) << 4)) = b;
+      }
+      dev::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar + kVEmpty + vs);
+        mbar_arrive(bar + kWideV);
+      }
+      if (++vs == lay.nv) vs = 0, vp ^= 1u;
+    };
+    // a group's queries, scaled to half precision, rows of 128 bytes; and what
+    // its rows are.  The products of the group before have read its queries,
+    // every warp is done with what the rows of the group before that were.
+    auto queries = [&](int n, const Job& job) {
+      const int wt = tid - 128;
+      Row* rows = row_info + (n & 1) * N;
+      float4* cr = col_info + (n & 1) * (N / 2);
+      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + job.b * p.a.q_seq;
+      asm volatile("bar.sync 4, 128;" ::: "memory");
+      for (int r = wt; r < N; r += 128) {
+        const int row = job.row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
+        const bool live = r < p.rows_per && node < job.live;
+        rows[r] = Row{node, node > 0 && p.a.L > 0 ? 1 + (node - 1) / p.a.L * p.a.L : 1,
+                      live ? (((int64_t)job.b * p.a.n + node) * p.a.heads + head) * D : -1};
+        q_at[r] = live ? node * p.a.q_tok + head * p.a.q_head : -1;
+      }
+      asm volatile("bar.sync 4, 128;" ::: "memory");
+      // each warp copies its rows (16 bytes a lane), then scales them in place
+      constexpr int kUnits = D / 8, kAtOnce = 32 / kUnits;
+      char* to = base + lay.q;
+      for (int r0 = w4 * kAtOnce; r0 < N; r0 += 4 * kAtOnce) {
+        const int r = r0 + lane / kUnits, unit = lane % kUnits;
+        const int64_t from = q_at[r];
+        char* dst = to + (unit >> 3) * N * 128 + r * 128 + (((unit & 7) ^ (r & 7)) << 4);
+        if (from >= 0)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(q + from + unit * 8) : "memory");
+        else
+          *reinterpret_cast<uint4*>(dst) = uint4{0, 0, 0, 0};
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+#pragma unroll 2
+      for (int x = w4 * kAtOnce; x < N; x += (x % kAtOnce == kAtOnce - 1) ? 3 * kAtOnce + 1 : 1) {
+        const int r = x;
+        const int at_lane = (lane >> 4) * N * 128 + r * 128 + ((((lane & 15) >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8;
+        uint2 y{0, 0};
+        if (lane * 4 < D) y = *reinterpret_cast<const uint2*>(to + at_lane);
+        const float v[4] = {__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16),
+                            __uint_as_float(y.y & 0xffff0000u)};
+        const float most = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+        const unsigned bits = __reduce_max_sync(kFull, __float_as_uint(most) & 0x7fffffffu);
+        const int e = bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23) - 127 - 14, -112);
+        // the coefficient is positive, so that a masked -inf stays one: the
+        // scale's sign, or 0, goes to the queries
+        const float inv = p.a.scale == 0.f ? 0.f : copysignf(__uint_as_float((unsigned)(127 - e) << 23), p.a.scale);
+        const __half2 a = __floats2half2_rn(v[0] * inv, v[1] * inv), b = __floats2half2_rn(v[2] * inv, v[3] * inv);
+        if (lane * 4 < D)
+          *reinterpret_cast<uint2*>(to + at_lane) =
+              uint2{*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)};
+        if (lane == 0) {
+          float* at_cr = reinterpret_cast<float*>(cr + (r >> 1)) + (r & 1);
+          const float k = fabsf(p.a.scale) * dev::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
+          at_cr[0] = p.a.scale == 0.f ? 1.f : fmaxf(k, 0x1p-100f);
+          at_cr[2] = 0.f;
+        }
+      }
+      dev::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar + kQ + (n & 1));
+    };
+    int tile = 0;
+    unsigned before = 0;
+    for (int n = 0;; ++n) {
+      const Job& job = job_at(n);
+      if (!job.cnt) break;
+      const Group grp = job.grp;
+      const int off = job.off, end = off + job.cnt;
+      // between groups the last values come first: the group's end waits for them
+      if (n) values(tile - 1, before);
+      hold(kWideKFree, (tile & 1) ^ 1);
+      if (n > 1) hold(kJobFree + ((n - 2) & (kJobs - 1)), ((n - 2) / kJobs) & 1);
+      queries(n, job);
+      job_done(n);
+      for (int i = off; i < end; ++i, ++tile) {
+        const unsigned seen = __ballot_sync(kFull, block_seen(grp, tile_slot(grp, i) + (lane & 7) * kBlock)) & 0xffu;
+        keys(tile);
+        if (i > off) values(tile - 1, before);
+        before = seen;
+      }
+    }
+    values(tile - 1, before);
+  } else if (warp >= 8) {
+    // ---- weigh: half of the columns, a quarter of the slots a warp
+    const int half = (warp - 8) >> 2, w4 = warp & 3, tq = lane & 3, gr = lane >> 2;
+    const int ht = tid - 256, NH = N / 2, steps = NH / 8, col0 = half * NH;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
+    // where this lane's rows of a transposed fragment go: slots w4 * 32 + (lane / 8) * 8 .. + 7, columns + lane % 8
+    const uint32_t w_to = smem_u32(base + lay.w) + (uint32_t)((w4 >> 1) * N * 128 + (col0 + (lane & 7)) * 128 +
+                                                             ((((w4 & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4));
+    int tile = 0, group = 0;
+    for (;;) {
+      const Job& job = job_at(group);
+      if (!job.cnt) break;
+      const int row0 = job.row0;
+      const Row* rows = row_info + (group & 1) * N;
+      float4* cr = col_info + (group & 1) * (N / 2);
+      hold(kQ + (group & 1), (group >> 1) & 1);   // rows and coefficients
+      float2 sum[kSteps];
+      float4* my_cr = cr + col0 / 2 + tq;   // step j's are 4 j further
+      unsigned unseen = (1u << (2 * steps)) - 1u;   // this thread's columns that have no reference yet
+      bool move = true;                             // some column of the half has none
+      float least = 1.f;
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        sum[j] = float2{0.f, 0.f};
+        if (j < steps) least = fminf(least, fminf(my_cr[4 * j].x, my_cr[4 * j].y));
+      }
+      // a block's scale is taken as no less than this, so that its product
+      // with a coefficient is not 0 (scores that small are 0 by far)
+      const float scale_floor = 0x1p-120f / least;
+      const Group grp = job.grp;
+      const int off = job.off, end = off + job.cnt, len = job.len;
+      for (int i = off; i < end; ++i, ++tile) {
+        const int kb = tile_slot(grp, i) + w4 * 32;
+        const int b = tile & 1;
+        hold(kS + b, (tile >> 1) & 1);
+        after_sync();
+        const float* sc = scales + (tile & (kScaleRing - 1)) * 16 + w4 * 2;
+        const bool seen0 = block_seen(grp, kb), seen1 = block_seen(grp, kb + kBlock);
+        const float ks0 = seen0 ? fmaxf(sc[0], scale_floor) : 1.f, ks1 = seen1 ? fmaxf(sc[1], scale_floor) : 1.f;
+        const float vs0 = seen0 ? sc[8] : 0.f, vs1 = seen1 ? sc[9] : 0.f;
+        const unsigned vs[2] = {pack_bf16(vs0, vs0), pack_bf16(vs1, vs1)};
+        const uint32_t s_at = t_s + b * N + col0 + lanes;
+        // 8 columns: x[2 k], x[2 k + 1] of slot kb + 8 k + gr
+        auto load = [&](int j, float* x) {
+          tmem_ld_frag(x, s_at + j * 8);
+          tmem_ld_frag(x + 4, s_at + j * 8 + (16u << 16));
+        };
+        auto scores = [&](int j, float* x) {   // less their references
+          const float4 y4 = my_cr[4 * j];
+          const float2 c0 = mul2(float2{y4.x, y4.y}, ks0), c1 = mul2(float2{y4.x, y4.y}, ks1);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 y = fma2(float2{x[2 * k], x[2 * k + 1]}, k < 2 ? c0 : c1, float2{y4.z, y4.w});
+            x[2 * k] = y.x;
+            x[2 * k + 1] = y.y;
+          }
+        };
+        if (kb + 32 > len || (p.a.window > 0 && kb + 32 > p.a.sinks && kb <= len + min(p.a.L, p.a.n - 1) - p.a.window)) {
+          // some slot is masked for some row: -inf in its place.  Dead columns
+          // get zeros, whatever the slots that were not loaded hold.
+#pragma unroll 1
+          for (int j = 0; j < steps; ++j) {
+            float x[8];
+            load(j, x);
+            tmem_ld_wait(x);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const Row row = rows[col0 + j * 8 + tq * 2 + e];
+              const int mine = len + (row.node > 0 ? row.node - row.own + 1 : 0);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int t = kb + k * 8 + gr, node = t - len;
+                bool see = node <= row.node && (node <= 0 || node >= row.own) && t < grp.hi;
+                if (p.a.window > 0) {
+                  const int pos = node <= 0 ? t : len + node - row.own + 1;
+                  see = see && (pos < p.a.sinks || pos > mine - p.a.window);
+                }
+                x[2 * k + e] = row.out < 0 ? 0.f : see ? x[2 * k + e] : dev::kNegInf;
+              }
+            }
+            tmem_st_frag(s_at + j * 8, x);
+            tmem_st_frag(s_at + j * 8 + (16u << 16), x + 4);
+          }
+          tmem_st_wait();
+        }
+        float2 part[kSteps];
+        for (;;) {
+          if (move) {
+            // the columns' maxima over the tile's slots become the references
+#pragma unroll 1
+            for (int j = 0; j < steps; ++j) {
+              float x[8];
+              load(j, x);
+              tmem_ld_wait(x);
+              scores(j, x);
+              float2 m{fmaxf(fmaxf(x[0], x[2]), fmaxf(x[4], x[6])), fmaxf(fmaxf(x[1], x[3]), fmaxf(x[5], x[7]))};
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) {
+                m.x = fmaxf(m.x, __shfl_xor_sync(kFull, m.x, d));
+                m.y = fmaxf(m.y, __shfl_xor_sync(kFull, m.y, d));
+              }
+              if (gr == 0) *reinterpret_cast<float2*>(red + w4 * N + col0 + j * 8 + tq * 2) = m;
+            }
+            half_sync(half);
+            const bool again = i != off;
+            if (again) {   // the sums so far follow: O of the tiles before is complete
+              hold(kWFree + (b ^ 1), ((tile - 1) >> 1) & 1);
+              after_sync();
+            }
+#pragma unroll 1
+            for (int j = 0; j < steps; ++j) {
+              const int col = col0 + j * 8 + tq * 2;
+              float2 m{kNone, kNone};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 y = *reinterpret_cast<const float2*>(red + k * N + col);
+                m.x = fmaxf(m.x, y.x);
+                m.y = fmaxf(m.y, y.y);
+              }
+              // relative to the reference, which only moves up; a column that
+              // had none (relative to 0) takes the maximum
+              float2 up{fmaxf(m.x, 0.f), fmaxf(m.y, 0.f)};
+              if (unseen >> (2 * j) & 1u) {
+                up.x = m.x > kNone ? m.x : 0.f;
+                if (m.x > kNone) unseen &= ~(1u << (2 * j));
+              }
+              if (unseen >> (2 * j) & 2u) {
+                up.y = m.y > kNone ? m.y : 0.f;
+                if (m.y > kNone) unseen &= ~(2u << (2 * j));
+              }
+              // a first reference below 0 finds sums of 0
+              const float2 alpha{ex2(-fmaxf(up.x, 0.f)), ex2(-fmaxf(up.y, 0.f))};
+              if (again) {
+                float x[8];
+                const uint32_t o_at = t_o + col0 + j * 8 + lanes;
+                tmem_ld_frag(x, o_at);
+                tmem_ld_frag(x + 4, o_at + (16u << 16));
+                tmem_ld_wait(x);
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) x[k] *= alpha.x, x[k + 1] *= alpha.y;
+                tmem_st_frag(o_at, x);
+                tmem_st_frag(o_at + (16u << 16), x + 4);
+              }
+              if (w4 == 0 && gr == 0) {
+                const float4 y4 = my_cr[4 * j];
+                *reinterpret_cast<float2*>(next + col) = float2{y4.z - up.x, y4.w - up.y};
+                *reinterpret_cast<float2*>(next + N + col) = alpha;
+              }
+            }
+            if (again) {
+              tmem_st_wait();
+              before_sync();
+            }
+            move = half_any(half, unseen != 0);   // and every thread has read the old references
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j)
+              if (j < steps) {
+                const float2 alpha = *reinterpret_cast<const float2*>(next + N + col0 + j * 8 + tq * 2);
+                sum[j].x *= alpha.x;
+                sum[j].y *= alpha.y;
+              }
+            if ((ht & 127) < NH) {
+              const int col = col0 + (ht & 127);
+              reinterpret_cast<float*>(cr + (col >> 1))[2 + (col & 1)] = next[col];
+            }
+            half_sync(half);
+          }
+          hold(kWFree + b, ((tile >> 1) & 1) ^ 1);
+          float top = kNone;
+          // two steps of fragments are weighed while the next two are loaded
+          float x[2][2][8];
+          load(0, x[0][0]);
+          if (1 < steps) load(1, x[0][1]);
+#pragma unroll
+          for (int j0 = 0; j0 < kSteps; j0 += 2)
+            if (j0 < steps) {
+              float (*now)[8] = x[(j0 >> 1) & 1], (*ahead)[8] = x[((j0 >> 1) & 1) ^ 1];
+              tmem_ld_wait(now[0]);
+              tmem_ld_wait(now[1]);
+              if (j0 + 2 < kSteps && j0 + 2 < steps) load(j0 + 2, ahead[0]);
+              if (j0 + 3 < kSteps && j0 + 3 < steps) load(j0 + 3, ahead[1]);
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                if (j0 + j < kSteps && j0 + j < steps) {
+                  float* y = now[j];
+                  scores(j0 + j, y);
+                  float2 s{0.f, 0.f};
+                  unsigned w[4];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    top = max3(top, y[2 * k], y[2 * k + 1]);
+                    const unsigned pk = pack_bf16(ex2(y[2 * k]), ex2(y[2 * k + 1]));
+                    s = add2(s, float2{__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)});
+                    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(w[k]) : "r"(pk), "r"(vs[k >> 1]));
+                  }
+                  part[j0 + j] = s;
+                  stmatrix_x4_trans(w_to + b * N * 256 + (j0 + j) * 1024, w);
+                }
+            }
+          if (!half_any(half, top > kSlack)) break;
+          move = true;
+        }
+        before_sync();
+        dev::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar + kSFree + b);
+          mbar_arrive(bar + kW + b);
+        }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+          if (j < steps) sum[j] = add2(sum[j], part[j]);
+      }
+
+      // ---- the group's or piece's end: normalisers, then O
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j)
+        if (j < steps) {
+          float2 s = sum[j];
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) {
+            s.x += __shfl_xor_sync(kFull, s.x, d);
+            s.y += __shfl_xor_sync(kFull, s.y, d);
+          }
+          if (gr == 0) {
+            *reinterpret_cast<float2*>(red + w4 * N + col0 + j * 8 + tq * 2) = s;
+            if (w4 == 0) {
+              stat[col0 + j * 8 + tq * 2].x = unseen >> (2 * j) & 1u ? kNone : -my_cr[4 * j].z;
+              stat[col0 + j * 8 + tq * 2 + 1].x = unseen >> (2 * j) & 2u ? kNone : -my_cr[4 * j].w;
+            }
+          }
+        }
+      half_sync(half);
+      const int at_half = ht & 127;
+      if (at_half < NH) {
+        const int col = col0 + at_half;
+        const float l = (red[col] + red[N + col]) + (red[2 * N + col] + red[3 * N + col]);
+        stat[col].y = job.whole() ? 1.f / l : l;
+      }
+      half_sync(half);
+      const bool whole = job.whole();
+      float* piece = piece_of(p, blockIdx.x, off == 0, D);
+      hold(kWFree + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
+      after_sync();
+      if (whole) {
+        // O to bfloat16 rows in the weights' place (transposed like them), then out
+        char* stage = base + lay.w;
+        if (w4 * 32 < D) {
+          const uint32_t to = smem_u32(stage) + (col0 + (lane & 7)) * D * 2 +
+                              (((w4 * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
+#pragma unroll 1
+          for (int j = 0; j < steps; ++j) {
+            float x[8];
+            const uint32_t o_at = t_o + col0 + j * 8 + lanes;
+            tmem_ld_frag(x, o_at);
+            tmem_ld_frag(x + 4, o_at + (16u << 16));
+            const float inv0 = stat[col0 + j * 8 + tq * 2].y, inv1 = stat[col0 + j * 8 + tq * 2 + 1].y;
+            tmem_ld_wait(x);
+            unsigned w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = pack_bf16(x[2 * k] * inv0, x[2 * k + 1] * inv1);
+            stmatrix_x4_trans(to + j * 8 * D * 2, w);
+          }
+        }
+        before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar + kOFree);
+        half_sync(half);
+        constexpr int kUnits = D / 8;   // of 16 bytes a row
+#pragma unroll 1
+        for (int x = ht & 127; x < NH * kUnits; x += 128) {
+          const int col = col0 + x / kUnits, unit = x % kUnits;
+          const int64_t to = rows[col].out;
+          if (to < 0) continue;
+          const uint4 y = *reinterpret_cast<const uint4*>(stage + col * D * 2 + ((unit ^ (col & 7)) << 4));
+          // of every four dimensions the order is 0, 2, 1, 3
+          *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.a.out) + to + unit * 8) =
+              uint4{__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x5410),
+                    __byte_perm(y.z, y.w, 0x7632)};
+        }
+      } else {
+        if (w4 * 32 < D) {
+          const int m = w4 * 32 + lane, dim = (m & ~3) | (m & 1) << 1 | (m >> 1 & 1);
+#pragma unroll 1
+          for (int j = 0; j < steps; ++j) {
+            float x[8];
+            tmem_ld_row8(x, t_o + col0 + j * 8 + lanes);
+            tmem_ld_wait(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int col = col0 + j * 8 + e;
+              if (rows[col].out < 0) continue;
+              __stcg(piece + col * (D + 2) + 2 + dim, x[e]);
+              if (m == 0) __stcg(reinterpret_cast<float2*>(piece + col * (D + 2)), stat[col]);
+            }
+          }
+        }
+        before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar + kOFree);
+      }
+      if (!whole) {
+        // the last piece of the group to arrive adds them all, in order
+        __threadfence();
+        weigh_sync();
+        if (ht == 0) {
+          const bool last = atomicAdd(p.s.joins + job.first_block, 1u) == (unsigned)(job.last_block - job.first_block);
+          if (last) p.s.joins[job.first_block] = 0;
+          *last_s = last;
+        }
+        weigh_sync();
+        if (*last_s) {
+          __threadfence();
+          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ht);
+        }
+      }
+      weigh_sync();   // the weights' place and stat have been read
+      job_done(group);
+      ++group;
+    }
+  }
+  before_sync();
+  __syncthreads();
+  after_sync();
+  if (warp == 2) tmem_free(tmem);
+}
+
+}  // namespace
+
+cudaError_t configure_many() {
+  cudaError_t e = cudaFuncSetAttribute(many_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(many_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  return e;
+}
+
+cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st) {
+  Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, 0};
+  p.rows = a.n * p.g;
+  p.row_tiles = (p.rows + kMaxN - 1) / kMaxN;
+  p.rows_per = (p.rows + p.row_tiles - 1) / p.row_tiles;
+  int N = (p.rows_per + 15) / 16 * 16;
+  if (N < 32) N = 32;
+  const Layout l = layout_of(s.head_dim, N, a.B);
+  const int grid = attend_grid(sms, p.rows_per, s.head_dim);
+  if (s.head_dim == 64)
+    many_kernel<64><<<grid, kThreads, l.bytes, st>>>(p, N);
+  else
+    many_kernel<128><<<grid, kThreads, l.bytes, st>>>(p, N);
+  return cudaGetLastError();
+}
+
+}  // namespace cache
+}  // namespace mds
