@@ -119,14 +119,27 @@ __device__ __forceinline__ void to_f16(unsigned x, unsigned& lo, unsigned& hi) {
       : "=r"(lo), "=r"(hi)
       : "r"(x));
 }
-// The even and the odd bytes of a word as two bfloat16 each: e4m3's exponent
-// and mantissa laid over bfloat16's are the number times 2^-120.
-__device__ __forceinline__ void to_bf16(unsigned x, unsigned& even, unsigned& odd) {
+// The even and the odd bytes of a word as two bfloat16 each, times a power of
+// two: e4m3's exponent and mantissa laid over bfloat16's are the number times
+// 2^-120, and `factor` (two bfloat16) is 2^120 times the power.  A block's
+// values are exact in bfloat16: their scale is at least 2^-117.
+__device__ __forceinline__ void to_bf16(unsigned x, unsigned factor, unsigned& even, unsigned& odd) {
   const unsigned e = ((x << 4) & 0x07f007f0u) | ((x << 8) & 0x80008000u);
   const unsigned o = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(0x7b807b80u));
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(0x7b807b80u));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(factor));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(factor));
 }
+// The factor of a block's scale.  2^7 is the largest that fits; `rest` is what
+// is left of a larger scale (values beyond 57344), as two bfloat16, else 1.
+__device__ __forceinline__ unsigned value_factor(float scale, unsigned& rest) {
+  const unsigned bits = __float_as_uint(scale) >> 16, most = 0x4300u;   // 2^7
+  rest = bits > most ? (bits - most + 0x3f80u) * 0x10001u : 0x3f803f80u;
+  return ((bits > most ? most : bits) + (120u << 7)) * 0x10001u;
+}
+__device__ __forceinline__ void times_rest(unsigned& x, unsigned rest) {
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(rest));
+}
+
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   unsigned r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -273,10 +286,10 @@ __device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, in
   return static_cast<T*>(p.a.out) + (node * p.a.heads + h * p.g + row % p.g) * head_dim;
 }
 
-// Add the pieces that blocks c0..c1 left of a row tile, in their order (256 threads).
+// Add the pieces that blocks c0..c1 left of a row tile, in their order.
 template <typename T, int D>
-__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, int tid) {
-  for (int x = tid; x < p.rows_per * (D / 4); x += 256) {
+__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, int tid, int threads) {
+  for (int x = tid; x < p.rows_per * (D / 4); x += threads) {
     const int r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
     if (row / p.g >= live) continue;
     auto piece = [&](int cc) { return piece_of(p, cc, cc == c0, D) + r * (D + 2); };

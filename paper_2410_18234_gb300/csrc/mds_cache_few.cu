@@ -5,14 +5,14 @@
 //
 // over the slots t that node i sees, m_i a running reference.  A block of 16
 // slots of one head has one scale 2^a for its keys and one 2^b for its
-// values: 2^a multiplies the block's scores, 2^b its weights.
+// values: 2^a multiplies the block's scores, 2^b its values.
 //
 // Products.  Every e4m3 number is exact in 16 bits, so products are taken in
 // 16 bits with 32-bit sums.  Keys meet queries in half precision: a row of
 // queries is first scaled by a power of two to a maximum in [2^14, 2^15),
 // where a bfloat16 query has no rounding, and a 32-bit one is carried by two
 // terms (22 bits and a sign).  Weights meet values in bfloat16, whose range
-// holds any 2^b: a 16-bit query's weight is rounded once (2^-9 relative, and
+// holds any value: a 16-bit query's weight is rounded once (2^-8 relative, and
 // the normaliser sums the rounded weights, so that a row that sees one token
 // returns that token's value), a 32-bit one's is carried by three terms.
 #include "mds_cache_attend.cuh"
@@ -332,9 +332,10 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
                 for (int z = 0; z < 4; ++z) acc[m][x][y][z] *= alpha[z >> 1];
           }
         }
-        // weights, times the values' scale, as the next product's rows
+        // weights, as the next product's rows; the values' scale goes to the values
         unsigned w[MT][F::kW][4];
-        const unsigned vs2 = pack_bf16(vs, vs);
+        unsigned rest;
+        const unsigned factor = value_factor(vs, rest);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
                 if constexpr (F::kW == 1) sum[m][x] += r0 + r1;
                 w0 -= r0;
                 w1 -= r1;
-                asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(w[m][term][2 * j + x]) : "r"(pk), "r"(vs2));
+                w[m][term][2 * j + x] = pk;
               }
             }
 #pragma unroll
@@ -360,8 +361,9 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             unsigned e0, o0, e1, o1;
-            to_bf16(v[2 * y], e0, o0);
-            to_bf16(v[2 * y + 1], e1, o1);
+            to_bf16(v[2 * y], factor, e0, o0);
+            to_bf16(v[2 * y + 1], factor, e1, o1);
+            if (rest != 0x3f803f80u) times_rest(e0, rest), times_rest(o0, rest), times_rest(e1, rest), times_rest(o1, rest);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -453,7 +455,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
       consumers_sync();
       if (*last_s) {
         __threadfence();
-        join_pieces<T, D>(p, c.b, c.h, row0, q.live, c0, c1, tid);
+        join_pieces<T, D>(p, c.b, c.h, row0, q.live, c0, c1, tid, kWarps * 32);
       }
     }
     u += cnt;

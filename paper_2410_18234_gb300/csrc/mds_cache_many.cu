@@ -32,12 +32,15 @@ namespace cache {
 
 namespace {
 
-constexpr int kThreads = 512;   // loader, products, memory, scheduler | 4 warps widen | 8 warps weigh
+constexpr int kWeigh = 12;      // warps that weigh, four for each third of the columns
+constexpr int kThreads = 32 * (12 + kWeigh);   // loader, products, memory, scheduler | 4 widen keys | 4 values | 12 weigh
 constexpr int kMaxN = 144;      // columns: three buffers of them and 64 of keys in 512 of tensor memory
-constexpr int kSteps = kMaxN / 16;   // fragments of 8 columns in half of them
 constexpr int kRingMax = 5;
 constexpr int kScaleRing = 8;   // tiles whose scales are held: kRingMax + 3
 constexpr int kJobs = 4;        // groups the scheduler is ahead
+// Weights are 2^(score - reference), and sums of floats lose nothing by a
+// reference that is not the maximum: it only has to keep them in range.
+constexpr float kMostWeight = 0x1p32f, kLeastWeight = 0x1p-40f;
 
 enum Bar {
   kKFull = 0, kKEmpty = kKFull + kRingMax, kVFull = kKEmpty + kRingMax, kVEmpty = kVFull + kRingMax,
@@ -137,18 +140,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ void half_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
-__device__ __forceinline__ bool half_any(int half, bool x) {
+__device__ __forceinline__ void third_sync(int third) { asm volatile("bar.sync %0, 128;" ::"r"(1 + third) : "memory"); }
+__device__ __forceinline__ bool third_any(int third, bool x) {
   unsigned r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"(1 + half), "r"((unsigned)x)
+      : "r"(1 + third), "r"((unsigned)x)
       : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void weigh_sync() { asm volatile("bar.sync 3, 256;" ::: "memory"); }
+__device__ __forceinline__ void weigh_sync() { asm volatile("bar.sync 4, 384;" ::: "memory"); }
 
 // Shared-memory operands: rows of 128 bytes, their 16-byte units permuted
 // (unit ^= row mod 8); `lead` is the distance of blocks of 64 elements along
@@ -198,14 +201,18 @@ __host__ __device__ inline Layout layout_of(int D, int N, int B) {
   return l;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant__ Params p, int N) {
+// kSteps: fragments of 8 columns in a third of them
+template <int D, int kSteps>
+__global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant__ Params p) {
+  constexpr int N = 24 * kSteps, NC = 8 * kSteps;   // columns, a third of them
   extern __shared__ char raw[];
   char* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const Layout lay = layout_of(D, N, p.a.B);
   char* at = base + lay.small;
-  float* scales = reinterpret_cast<float*>(at);            // [kScaleRing][16]: keys' 8, values' 8
-  at += kScaleRing * 16 * 4;
+  float* k_scales = reinterpret_cast<float*>(at);          // [kScaleRing][8], by tile
+  at += kScaleRing * 8 * 4;
+  float* v_scales = reinterpret_cast<float*>(at);          // [kRingMax][8], by the ring's slot
+  at += kScaleRing * 8 * 4;
   Row* row_info = reinterpret_cast<Row*>(at);              // [2][N], by group
   at += 2 * N * 16;
   Seq* seqs = reinterpret_cast<Seq*>(at);
@@ -234,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     for (int i = 0; i < kRingMax; ++i) {
       mbar_init(bar + kKFull + i, 1 + 32);   // the loader's byte count, and its lanes' scale copies
       mbar_init(bar + kKEmpty + i, 4);
-      mbar_init(bar + kVFull + i, 1);
+      mbar_init(bar + kVFull + i, 1 + 32);
       mbar_init(bar + kVEmpty + i, 4);
     }
     mbar_init(bar + kWideK, 4);
@@ -243,16 +250,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     mbar_init(bar + kWideVFree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar + kS + i, 1);
-      mbar_init(bar + kSFree + i, 8);
-      mbar_init(bar + kW + i, 8);
+      mbar_init(bar + kSFree + i, kWeigh);
+      mbar_init(bar + kW + i, kWeigh);
       mbar_init(bar + kWFree + i, 1);
     }
     mbar_init(bar + kQ, 4);
     mbar_init(bar + kQ + 1, 4);
-    mbar_init(bar + kOFree, 8);
+    mbar_init(bar + kOFree, kWeigh);
     for (int i = 0; i < kJobs; ++i) {
       mbar_init(bar + kJob + i, 1);
-      mbar_init(bar + kJobFree + i, 14);   // every warp but the scheduler's and the memory's
+      mbar_init(bar + kJobFree + i, 10 + kWeigh);   // every warp but the scheduler's and the memory's
     }
     mbar_init_fence();
   }
@@ -345,18 +352,25 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         __syncwarp();
         if (page >= 0) {
           if (!kv) bulk_copy(base + lay.k_ring + (ks * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kKFull + ks);
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
-                           smem_u32(scales + (tile & (kScaleRing - 1)) * 16 + lane)),
-                       "l"(s.scales + (row >> 4))
-                       : "memory");
+          if (!kv)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
+                             smem_u32(k_scales + (tile & (kScaleRing - 1)) * 8 + blk)),
+                         "l"(s.scales + (row >> 4))
+                         : "memory");
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + kKFull + ks))
                      : "memory");
         hold(kVEmpty + vs, vp);
         if (lane == 0) mbar_expect_tx(bar + kVFull + vs, __popc(takes & 0xff00u) * kBlock * D);
         __syncwarp();
-        if (page >= 0 && kv)
+        if (page >= 0 && kv) {
           bulk_copy(base + lay.v_ring + (vs * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kVFull + vs);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(v_scales + vs * 8 + blk)),
+                       "l"(s.scales + (row >> 4))
+                       : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + kVFull + vs))
+                     : "memory");
         page = next;
         if (++ks == lay.nk) ks = 0, kp ^= 1u;
         if (++vs == lay.nv) vs = 0, vp ^= 1u;
@@ -406,12 +420,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       ++group;
     }
   } else if (warp >= 4 && warp < 8) {
-    // ---- widen: keys a row a thread into tensor memory, values 16 dimensions
-    // of a slot at a time into shared memory.  Rows of blocks that were not
-    // loaded hold anything: their scores are masked, their values are zeros.
+    // ---- widen keys, a row a thread, into tensor memory; and the groups'
+    // queries.  Rows of blocks that were not loaded hold anything: their
+    // scores are masked.
     const int w4 = warp & 3, key = w4 * 32 + lane;
-    int ks = 0, vs = 0;
-    unsigned kp = 0, vp = 0;
+    int ks = 0;
+    unsigned kp = 0;
     const uint32_t k_to = t_k + ((uint32_t)(w4 * 32) << 16);
     auto keys = [&](int t) {
       hold(kKFull + ks, kp);
@@ -440,36 +454,6 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       }
       if (++ks == lay.nk) ks = 0, kp ^= 1u;
     };
-    // seen: bit i of the tile's blocks (two a warp)
-    auto values = [&](int t, unsigned seen) {
-      hold(kVFull + vs, vp);
-      hold(kWideVFree, (t & 1) ^ 1);
-      const char* src = base + lay.v_ring + vs * kTile * D;
-      char* dst = base + lay.wide_v;
-      constexpr int kChunks = D / 16;
-#pragma unroll 2
-      for (int it = 0; it < kChunks; ++it) {
-        const int pair = it * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
-        const int k = w4 * 32 + octet * 8 + (lane & 7);
-        uint4 y = *reinterpret_cast<const uint4*>(src + swizzled(k * D + chunk * 16));
-        if (!(seen >> (k >> 4) & 1u)) y = uint4{0, 0, 0, 0};
-        uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
-        to_bf16(y.x, a.x, a.y);
-        to_bf16(y.y, a.z, a.w);
-        to_bf16(y.z, b.x, b.y);
-        to_bf16(y.w, b.z, b.w);
-        char* line = dst + (chunk >> 2) * 16384 + k * 128;
-        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2) ^ (k & 7)) << 4)) = a;
-        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2 + 1) ^ (k & 7)) << 4)) = b;
-      }
-      dev::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(bar + kVEmpty + vs);
-        mbar_arrive(bar + kWideV);
-      }
-      if (++vs == lay.nv) vs = 0, vp ^= 1u;
-    };
     // a group's queries, scaled to half precision, rows of 128 bytes; and what
     // its rows are.  The products of the group before have read its queries,
     // every warp is done with what the rows of the group before that were.
@@ -478,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       Row* rows = row_info + (n & 1) * N;
       float4* cr = col_info + (n & 1) * (N / 2);
       const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + job.b * p.a.q_seq;
-      asm volatile("bar.sync 4, 128;" ::: "memory");
+      asm volatile("bar.sync 5, 128;" ::: "memory");
       for (int r = wt; r < N; r += 128) {
         const int row = job.row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
         const bool live = r < p.rows_per && node < job.live;
@@ -486,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
                       live ? (((int64_t)job.b * p.a.n + node) * p.a.heads + head) * D : -1};
         q_at[r] = live ? node * p.a.q_tok + head * p.a.q_head : -1;
       }
-      asm volatile("bar.sync 4, 128;" ::: "memory");
+      asm volatile("bar.sync 5, 128;" ::: "memory");
       // each warp copies its rows (16 bytes a lane), then scales them in place
       constexpr int kUnits = D / 8, kAtOnce = 32 / kUnits;
       char* to = base + lay.q;
@@ -502,24 +486,28 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
 #pragma unroll 2
-      for (int x = w4 * kAtOnce; x < N; x += (x % kAtOnce == kAtOnce - 1) ? 3 * kAtOnce + 1 : 1) {
-        const int r = x;
-        const int at_lane = (lane >> 4) * N * 128 + r * 128 + ((((lane & 15) >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8;
-        uint2 y{0, 0};
-        if (lane * 4 < D) y = *reinterpret_cast<const uint2*>(to + at_lane);
-        const float v[4] = {__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16),
-                            __uint_as_float(y.y & 0xffff0000u)};
-        const float most = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-        const unsigned bits = __reduce_max_sync(kFull, __float_as_uint(most) & 0x7fffffffu);
+      for (int r0 = w4 * kAtOnce; r0 < N; r0 += 4 * kAtOnce) {
+        const int r = r0 + lane / kUnits, unit = lane % kUnits;
+        uint4* at_lane = reinterpret_cast<uint4*>(to + (unit >> 3) * N * 128 + r * 128 + (((unit & 7) ^ (r & 7)) << 4));
+        const uint4 y = *at_lane;
+        const unsigned w[4] = {y.x, y.y, y.z, y.w};
+        unsigned bits = 0;   // the largest magnitude: bfloat16 order as their bits do
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits = max(bits, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
+#pragma unroll
+        for (int d = 1; d < kUnits; d *= 2) bits = max(bits, __shfl_xor_sync(kFull, bits, d));
         const int e = bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23) - 127 - 14, -112);
         // the coefficient is positive, so that a masked -inf stays one: the
         // scale's sign, or 0, goes to the queries
         const float inv = p.a.scale == 0.f ? 0.f : copysignf(__uint_as_float((unsigned)(127 - e) << 23), p.a.scale);
-        const __half2 a = __floats2half2_rn(v[0] * inv, v[1] * inv), b = __floats2half2_rn(v[2] * inv, v[3] * inv);
-        if (lane * 4 < D)
-          *reinterpret_cast<uint2*>(to + at_lane) =
-              uint2{*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)};
-        if (lane == 0) {
+        unsigned v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __half2 a = __floats2half2_rn(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
+          v[i] = *reinterpret_cast<const unsigned*>(&a);
+        }
+        *at_lane = uint4{v[0], v[1], v[2], v[3]};
+        if (unit == 0) {
           float* at_cr = reinterpret_cast<float*>(cr + (r >> 1)) + (r & 1);
           const float k = fabsf(p.a.scale) * dev::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
           at_cr[0] = p.a.scale == 0.f ? 1.f : fmaxf(k, 0x1p-100f);
@@ -531,30 +519,77 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       if (lane == 0) mbar_arrive(bar + kQ + (n & 1));
     };
     int tile = 0;
-    unsigned before = 0;
+    for (int n = 0;; ++n) {
+      const Job& job = job_at(n);
+      if (!job.cnt) break;
+      const int cnt = job.cnt;
+      hold(kWideKFree, (tile & 1) ^ 1);
+      if (n > 1) hold(kJobFree + ((n - 2) & (kJobs - 1)), ((n - 2) / kJobs) & 1);
+      queries(n, job);
+      job_done(n);
+      for (int i = 0; i < cnt; ++i, ++tile) keys(tile);
+    }
+  } else if (warp >= 8 && warp < 12) {
+    // ---- widen values, 16 dimensions of a slot at a time, into shared memory.
+    // Rows of blocks that were not loaded become zeros.
+    const int w4 = warp & 3;
+    int vs = 0;
+    unsigned vp = 0;
+    // seen: bit i of the tile's blocks (two a warp)
+    auto values = [&](int t, unsigned seen) {
+      hold(kVFull + vs, vp);
+      hold(kWideVFree, (t & 1) ^ 1);
+      const float* sc = v_scales + vs * 8 + w4 * 2;
+      unsigned rest[2];
+      const unsigned factor[2] = {value_factor(sc[0], rest[0]), value_factor(sc[1], rest[1])};
+      const bool large = (seen >> (w4 * 2) & 1u && rest[0] != 0x3f803f80u) || (seen >> (w4 * 2) & 2u && rest[1] != 0x3f803f80u);
+      const char* src = base + lay.v_ring + vs * kTile * D;
+      char* dst = base + lay.wide_v;
+      constexpr int kChunks = D / 16;
+#pragma unroll 4
+      for (int it = 0; it < kChunks; ++it) {
+        const int pair = it * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+        const int k = w4 * 32 + octet * 8 + (lane & 7);
+        uint4 y = *reinterpret_cast<const uint4*>(src + swizzled(k * D + chunk * 16));
+        const bool zero = !(seen >> (k >> 4) & 1u);
+        if (zero) y = uint4{0, 0, 0, 0};
+        uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
+        const unsigned f = zero ? 0u : octet & 2 ? factor[1] : factor[0];
+        to_bf16(y.x, f, a.x, a.y);
+        to_bf16(y.y, f, a.z, a.w);
+        to_bf16(y.z, f, b.x, b.y);
+        to_bf16(y.w, f, b.z, b.w);
+        if (large) {
+          const unsigned g = octet & 2 ? rest[1] : rest[0];
+          times_rest(a.x, g), times_rest(a.y, g), times_rest(a.z, g), times_rest(a.w, g);
+          times_rest(b.x, g), times_rest(b.y, g), times_rest(b.z, g), times_rest(b.w, g);
+        }
+        char* line = dst + (chunk >> 2) * 16384 + k * 128;
+        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2) ^ (k & 7)) << 4)) = a;
+        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2 + 1) ^ (k & 7)) << 4)) = b;
+      }
+      dev::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar + kVEmpty + vs);
+        mbar_arrive(bar + kWideV);
+      }
+      if (++vs == lay.nv) vs = 0, vp ^= 1u;
+    };
+    int tile = 0;
     for (int n = 0;; ++n) {
       const Job& job = job_at(n);
       if (!job.cnt) break;
       const Group grp = job.grp;
       const int off = job.off, end = off + job.cnt;
-      // between groups the last values come first: the group's end waits for them
-      if (n) values(tile - 1, before);
-      hold(kWideKFree, (tile & 1) ^ 1);
-      if (n > 1) hold(kJobFree + ((n - 2) & (kJobs - 1)), ((n - 2) / kJobs) & 1);
-      queries(n, job);
       job_done(n);
-      for (int i = off; i < end; ++i, ++tile) {
-        const unsigned seen = __ballot_sync(kFull, block_seen(grp, tile_slot(grp, i) + (lane & 7) * kBlock)) & 0xffu;
-        keys(tile);
-        if (i > off) values(tile - 1, before);
-        before = seen;
-      }
+      for (int i = off; i < end; ++i, ++tile)
+        values(tile, __ballot_sync(kFull, block_seen(grp, tile_slot(grp, i) + (lane & 7) * kBlock)) & 0xffu);
     }
-    values(tile - 1, before);
-  } else if (warp >= 8) {
-    // ---- weigh: half of the columns, a quarter of the slots a warp
-    const int half = (warp - 8) >> 2, w4 = warp & 3, tq = lane & 3, gr = lane >> 2;
-    const int ht = tid - 256, NH = N / 2, steps = NH / 8, col0 = half * NH;
+  } else if (warp >= 12) {
+    // ---- weigh: a third of the columns, a quarter of the slots a warp
+    const int third = (warp - 12) >> 2, w4 = warp & 3, tq = lane & 3, gr = lane >> 2;
+    const int ht = tid - 384, col0 = third * NC;
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
     // where this lane's rows of a transposed fragment go: slots w4 * 32 + (lane / 8) * 8 .. + 7, columns + lane % 8
     const uint32_t w_to = smem_u32(base + lay.w) + (uint32_t)((w4 >> 1) * N * 128 + (col0 + (lane & 7)) * 128 +
@@ -569,13 +604,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       hold(kQ + (group & 1), (group >> 1) & 1);   // rows and coefficients
       float2 sum[kSteps];
       float4* my_cr = cr + col0 / 2 + tq;   // step j's are 4 j further
-      unsigned unseen = (1u << (2 * steps)) - 1u;   // this thread's columns that have no reference yet
-      bool move = true;                             // some column of the half has none
+      unsigned unseen = (1u << (2 * kSteps)) - 1u;   // this thread's columns that have no reference yet
+      bool pending = true;                          // some column of the third has none
       float least = 1.f;
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
         sum[j] = float2{0.f, 0.f};
-        if (j < steps) least = fminf(least, fminf(my_cr[4 * j].x, my_cr[4 * j].y));
+        least = fminf(least, fminf(my_cr[4 * j].x, my_cr[4 * j].y));
       }
       // a block's scale is taken as no less than this, so that its product
       // with a coefficient is not 0 (scores that small are 0 by far)
@@ -587,11 +622,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         const int b = tile & 1;
         hold(kS + b, (tile >> 1) & 1);
         after_sync();
-        const float* sc = scales + (tile & (kScaleRing - 1)) * 16 + w4 * 2;
+        const float* sc = k_scales + (tile & (kScaleRing - 1)) * 8 + w4 * 2;
         const bool seen0 = block_seen(grp, kb), seen1 = block_seen(grp, kb + kBlock);
         const float ks0 = seen0 ? fmaxf(sc[0], scale_floor) : 1.f, ks1 = seen1 ? fmaxf(sc[1], scale_floor) : 1.f;
-        const float vs0 = seen0 ? sc[8] : 0.f, vs1 = seen1 ? sc[9] : 0.f;
-        const unsigned vs[2] = {pack_bf16(vs0, vs0), pack_bf16(vs1, vs1)};
         const uint32_t s_at = t_s + b * N + col0 + lanes;
         // 8 columns: x[2 k], x[2 k + 1] of slot kb + 8 k + gr
         auto load = [&](int j, float* x) {
@@ -612,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
           // some slot is masked for some row: -inf in its place.  Dead columns
           // get zeros, whatever the slots that were not loaded hold.
 #pragma unroll 1
-          for (int j = 0; j < steps; ++j) {
+          for (int j = 0; j < kSteps; ++j) {
             float x[8];
             load(j, x);
             tmem_ld_wait(x);
@@ -636,12 +669,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
           }
           tmem_st_wait();
         }
+        // Weights first with the references as they are (0 before the first);
+        // only where that gives a weight too large, or none that a first
+        // reference could be judged by, the columns' maxima over the tile's
+        // slots become the references, and the tile is weighed again.
         float2 part[kSteps];
+        bool move = false, left = false;
         for (;;) {
           if (move) {
-            // the columns' maxima over the tile's slots become the references
 #pragma unroll 1
-            for (int j = 0; j < steps; ++j) {
+            for (int j = 0; j < kSteps; ++j) {
               float x[8];
               load(j, x);
               tmem_ld_wait(x);
@@ -654,14 +691,14 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
               }
               if (gr == 0) *reinterpret_cast<float2*>(red + w4 * N + col0 + j * 8 + tq * 2) = m;
             }
-            half_sync(half);
+            third_sync(third);
             const bool again = i != off;
             if (again) {   // the sums so far follow: O of the tiles before is complete
               hold(kWFree + (b ^ 1), ((tile - 1) >> 1) & 1);
               after_sync();
             }
 #pragma unroll 1
-            for (int j = 0; j < steps; ++j) {
+            for (int j = 0; j < kSteps; ++j) {
               const int col = col0 + j * 8 + tq * 2;
               float2 m{kNone, kNone};
 #pragma unroll
@@ -704,55 +741,69 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
               tmem_st_wait();
               before_sync();
             }
-            move = half_any(half, unseen != 0);   // and every thread has read the old references
+            left = third_any(third, unseen != 0);   // and every thread has read the old references
 #pragma unroll
             for (int j = 0; j < kSteps; ++j)
-              if (j < steps) {
+              {
                 const float2 alpha = *reinterpret_cast<const float2*>(next + N + col0 + j * 8 + tq * 2);
                 sum[j].x *= alpha.x;
                 sum[j].y *= alpha.y;
               }
-            if ((ht & 127) < NH) {
+            if ((ht & 127) < NC) {
               const int col = col0 + (ht & 127);
               reinterpret_cast<float*>(cr + (col >> 1))[2 + (col & 1)] = next[col];
             }
-            half_sync(half);
+            third_sync(third);
           }
           hold(kWFree + b, ((tile >> 1) & 1) ^ 1);
-          float top = kNone;
           // two steps of fragments are weighed while the next two are loaded
           float x[2][2][8];
           load(0, x[0][0]);
-          if (1 < steps) load(1, x[0][1]);
+          load(1, x[0][1]);
 #pragma unroll
           for (int j0 = 0; j0 < kSteps; j0 += 2)
-            if (j0 < steps) {
+            {
               float (*now)[8] = x[(j0 >> 1) & 1], (*ahead)[8] = x[((j0 >> 1) & 1) ^ 1];
               tmem_ld_wait(now[0]);
               tmem_ld_wait(now[1]);
-              if (j0 + 2 < kSteps && j0 + 2 < steps) load(j0 + 2, ahead[0]);
-              if (j0 + 3 < kSteps && j0 + 3 < steps) load(j0 + 3, ahead[1]);
+              if (j0 + 2 < kSteps) {
+                load(j0 + 2, ahead[0]);
+                load(j0 + 3, ahead[1]);
+              }
 #pragma unroll
               for (int j = 0; j < 2; ++j)
-                if (j0 + j < kSteps && j0 + j < steps) {
+                {
                   float* y = now[j];
                   scores(j0 + j, y);
-                  float2 s{0.f, 0.f};
                   unsigned w[4];
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {
-                    top = max3(top, y[2 * k], y[2 * k + 1]);
-                    const unsigned pk = pack_bf16(ex2(y[2 * k]), ex2(y[2 * k + 1]));
-                    s = add2(s, float2{__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)});
-                    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(w[k]) : "r"(pk), "r"(vs[k >> 1]));
+                    w[k] = pack_bf16(ex2(y[2 * k]), ex2(y[2 * k + 1]));
+                    const float2 e{__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u)};
+                    part[j0 + j] = k ? add2(part[j0 + j], e) : e;
                   }
-                  part[j0 + j] = s;
                   stmatrix_x4_trans(w_to + b * N * 256 + (j0 + j) * 1024, w);
                 }
             }
-          if (!half_any(half, top > kSlack)) break;
+          // too large a weight for the reference, or (a first reference) too
+          // small ones: this thread's four of a column together
+          float top = 0.f, low = 1.f;
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j)
+            top = max3(top, part[j].x, part[j].y);
+          if (pending && !move) {
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j)
+              {
+                if (unseen >> (2 * j) & 1u) low = fminf(low, part[j].x);
+                if (unseen >> (2 * j) & 2u) low = fminf(low, part[j].y);
+              }
+          }
+          if (!third_any(third, top > kMostWeight || low < kLeastWeight)) break;
           move = true;
         }
+        pending = pending && left;
+        if (!pending) unseen = 0;
         before_sync();
         dev::fence_proxy_async();
         __syncwarp();
@@ -762,13 +813,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         }
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
-          if (j < steps) sum[j] = add2(sum[j], part[j]);
+          sum[j] = add2(sum[j], part[j]);
       }
 
       // ---- the group's or piece's end: normalisers, then O
 #pragma unroll
       for (int j = 0; j < kSteps; ++j)
-        if (j < steps) {
+        {
           float2 s = sum[j];
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) {
@@ -783,14 +834,14 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
             }
           }
         }
-      half_sync(half);
+      third_sync(third);
       const int at_half = ht & 127;
-      if (at_half < NH) {
+      if (at_half < NC) {
         const int col = col0 + at_half;
         const float l = (red[col] + red[N + col]) + (red[2 * N + col] + red[3 * N + col]);
         stat[col].y = job.whole() ? 1.f / l : l;
       }
-      half_sync(half);
+      third_sync(third);
       const bool whole = job.whole();
       float* piece = piece_of(p, blockIdx.x, off == 0, D);
       hold(kWFree + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
@@ -802,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
           const uint32_t to = smem_u32(stage) + (col0 + (lane & 7)) * D * 2 +
                               (((w4 * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
 #pragma unroll 1
-          for (int j = 0; j < steps; ++j) {
+          for (int j = 0; j < kSteps; ++j) {
             float x[8];
             const uint32_t o_at = t_o + col0 + j * 8 + lanes;
             tmem_ld_frag(x, o_at);
@@ -818,10 +869,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar + kOFree);
-        half_sync(half);
+        third_sync(third);
         constexpr int kUnits = D / 8;   // of 16 bytes a row
 #pragma unroll 1
-        for (int x = ht & 127; x < NH * kUnits; x += 128) {
+        for (int x = ht & 127; x < NC * kUnits; x += 128) {
           const int col = col0 + x / kUnits, unit = x % kUnits;
           const int64_t to = rows[col].out;
           if (to < 0) continue;
@@ -835,7 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         if (w4 * 32 < D) {
           const int m = w4 * 32 + lane, dim = (m & ~3) | (m & 1) << 1 | (m >> 1 & 1);
 #pragma unroll 1
-          for (int j = 0; j < steps; ++j) {
+          for (int j = 0; j < kSteps; ++j) {
             float x[8];
             tmem_ld_row8(x, t_o + col0 + j * 8 + lanes);
             tmem_ld_wait(x);
@@ -864,7 +915,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         weigh_sync();
         if (*last_s) {
           __threadfence();
-          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ht);
+          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ht, 32 * kWeigh);
         }
       }
       weigh_sync();   // the weights' place and stat have been read
@@ -878,12 +929,27 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
   if (warp == 2) tmem_free(tmem);
 }
 
+template <int D, int kSteps>
+cudaError_t launch_many(const Params& p, int sms, cudaStream_t st) {
+  const Layout l = layout_of(D, 24 * kSteps, p.a.B);
+  const int grid = attend_grid(sms, p.rows_per, D);
+  many_kernel<D, kSteps><<<grid, kThreads, l.bytes, st>>>(p);
+  return cudaGetLastError();
+}
+template <int D, int kSteps>
+cudaError_t configure_one() {
+  return cudaFuncSetAttribute(many_kernel<D, kSteps>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+}
+
 }  // namespace
 
 cudaError_t configure_many() {
-  cudaError_t e = cudaFuncSetAttribute(many_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(many_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  cudaError_t e = configure_one<64, 2>();
+  if (e == cudaSuccess) e = configure_one<64, 4>();
+  if (e == cudaSuccess) e = configure_one<64, 6>();
+  if (e == cudaSuccess) e = configure_one<128, 2>();
+  if (e == cudaSuccess) e = configure_one<128, 4>();
+  if (e == cudaSuccess) e = configure_one<128, 6>();
   return e;
 }
 
@@ -892,15 +958,9 @@ cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t s
   p.rows = a.n * p.g;
   p.row_tiles = (p.rows + kMaxN - 1) / kMaxN;
   p.rows_per = (p.rows + p.row_tiles - 1) / p.row_tiles;
-  int N = (p.rows_per + 15) / 16 * 16;
-  if (N < 32) N = 32;
-  const Layout l = layout_of(s.head_dim, N, a.B);
-  const int grid = attend_grid(sms, p.rows_per, s.head_dim);
   if (s.head_dim == 64)
-    many_kernel<64><<<grid, kThreads, l.bytes, st>>>(p, N);
-  else
-    many_kernel<128><<<grid, kThreads, l.bytes, st>>>(p, N);
-  return cudaGetLastError();
+    return p.rows_per <= 48 ? launch_many<64, 2>(p, sms, st) : p.rows_per <= 96 ? launch_many<64, 4>(p, sms, st) : launch_many<64, 6>(p, sms, st);
+  return p.rows_per <= 48 ? launch_many<128, 2>(p, sms, st) : p.rows_per <= 96 ? launch_many<128, 4>(p, sms, st) : launch_many<128, 6>(p, sms, st);
 }
 
 }  // namespace cache
