@@ -33,18 +33,18 @@ namespace cache {
 namespace {
 
 constexpr int kWeigh = 12;      // warps that weigh, four for each third of the columns
-constexpr int kThreads = 32 * (12 + kWeigh);   // loader, products, memory, scheduler | 4 widen keys | 4 values | 12 weigh
+constexpr int kThreads = 32 * (12 + kWeigh);   // keys' loader, products, values' loader, scheduler | 4 widen keys | 4 values | 12 weigh
 constexpr int kMaxN = 144;      // columns: three buffers of them and 64 of keys in 512 of tensor memory
 constexpr int kRingMax = 5;
 constexpr int kScaleRing = 8;   // tiles whose scales are held: kRingMax + 3
 constexpr int kJobs = 4;        // groups the scheduler is ahead
 // Weights are 2^(score - reference), and sums of floats lose nothing by a
 // reference that is not the maximum: it only has to keep them in range.
-constexpr float kMostWeight = 0x1p32f, kLeastWeight = 0x1p-40f;
+constexpr float kMostWeight = 0x1p48f, kLeastWeight = 0x1p-60f;
 
 enum Bar {
   kKFull = 0, kKEmpty = kKFull + kRingMax, kVFull = kKEmpty + kRingMax, kVEmpty = kVFull + kRingMax,
-  kWideK = kVEmpty + kRingMax, kWideKFree, kWideV, kWideVFree, kS, kSFree = kS + 2, kW = kSFree + 2,
+  kWideK = kVEmpty + kRingMax, kWideKFree, kWideV, kWideVFree = kWideV + 2, kS = kWideVFree + 2, kSFree = kS + 2, kW = kSFree + 2,
   kWFree = kW + 2, kQ = kWFree + 2, kOFree = kQ + 2, kJob, kJobFree = kJob + kJobs, kBars = kJobFree + kJobs
 };
 
@@ -62,6 +62,11 @@ __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::afte
 __device__ __forceinline__ void commit_to(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
+}
+__device__ __forceinline__ bool elected() {
+  unsigned r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
@@ -179,6 +184,9 @@ struct Job {
   __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
 };
 
+// Buffers of wide values: two where they leave room for the rings.
+__host__ __device__ constexpr int wide_buffers(int N) { return N <= 96 ? 2 : 1; }
+
 // Shared memory from a 1024-byte boundary on.
 struct Layout {
   int q, w, wide_v, k_ring, v_ring, small, bytes;
@@ -189,7 +197,7 @@ __host__ __device__ inline Layout layout_of(int D, int N, int B) {
   l.q = 0;
   l.w = l.q + N * D * 2;
   l.wide_v = l.w + 2 * N * 256;
-  l.k_ring = l.wide_v + 128 * D * 2;
+  l.k_ring = l.wide_v + wide_buffers(N) * 128 * D * 2;
   const int small = kScaleRing * 16 * 4 + N * (2 * 16 + 8 + 2 * 8 + 8 + 24) + (kBars + 1) / 2 * 16 + kJobs * (int)sizeof(Job) + 16 + B * 16;
   const int room = 227 * 1024 - 1024 - l.k_ring - small;
   const int slots = room / (kTile * D);
@@ -205,6 +213,7 @@ __host__ __device__ inline Layout layout_of(int D, int N, int B) {
 template <int D, int kSteps>
 __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant__ Params p) {
   constexpr int N = 24 * kSteps, NC = 8 * kSteps;   // columns, a third of them
+  constexpr int kWide = wide_buffers(N);
   extern __shared__ char raw[];
   char* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const Layout lay = layout_of(D, N, p.a.B);
@@ -246,9 +255,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     }
     mbar_init(bar + kWideK, 4);
     mbar_init(bar + kWideKFree, 1);
-    mbar_init(bar + kWideV, 4);
-    mbar_init(bar + kWideVFree, 1);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(bar + kWideV + i, 4);
+      mbar_init(bar + kWideVFree + i, 1);
       mbar_init(bar + kS + i, 1);
       mbar_init(bar + kSFree + i, kWeigh);
       mbar_init(bar + kW + i, kWeigh);
@@ -259,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     mbar_init(bar + kOFree, kWeigh);
     for (int i = 0; i < kJobs; ++i) {
       mbar_init(bar + kJob + i, 1);
-      mbar_init(bar + kJobFree + i, 10 + kWeigh);   // every warp but the scheduler's and the memory's
+      mbar_init(bar + kJobFree + i, 11 + kWeigh);   // every warp but the scheduler's
     }
     mbar_init_fence();
   }
@@ -312,13 +321,15 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       u += cnt;
       if (u < u1) advance(p, seqs, c, grp);
     }
-  } else if (warp == 0) {
-    // ---- loader: one block of 16 slots a lane (keys: lanes 0..7, values: 8..15)
+  } else if (warp == 0 || warp == 2) {
+    // ---- loaders, of keys and of values: one block of 16 slots a lane (0..7)
     const State& s = p.s;
-    const int kv = (lane >> 3) & 1, blk = lane & 7;
+    const int kv = warp >> 1, blk = lane & 7, slots = kv ? lay.nv : lay.nk;
+    char* ring = base + (kv ? lay.v_ring : lay.k_ring);
+    const int full = kv ? kVFull : kKFull, empty = kv ? kVEmpty : kKEmpty;
     const int64_t layer0 = (int64_t)p.a.layer * s.pages;
-    int tile = 0, ks = 0, vs = 0;
-    unsigned kp = 1, vp = 1;
+    int tile = 0, slot = 0;
+    unsigned parity = 1;
     for (int n = 0;; ++n) {
       const Job& job = job_at(n);
       const int end = job.off + job.cnt, h = job.h;
@@ -327,73 +338,64 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       const int32_t* table = s.table + (int64_t)job.q * s.max_pages;
       auto page_of = [&](int i) {
         const int t = tile_slot(grp, i) + blk * kBlock;
-        return lane < 16 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
+        return lane < 8 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
       };
       const int off = job.off;
-      // the queries are read by the time that the group's first tile is here
-      for (int r = lane; r < p.rows_per; r += 32) {
-        const int row = job.row0 + r, node = row / p.g;
-        if (node < job.live) {
-          const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + job.b * p.a.q_seq + node * p.a.q_tok +
-                                   (h * p.g + row - node * p.g) * p.a.q_head;
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
-          if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+      int page = page_of(off);
+      if (kv) {   // the queries are read by the time that the group's first tile is here
+        for (int r = lane; r < p.rows_per; r += 32) {
+          const int row = job.row0 + r, node = row / p.g;
+          if (node < job.live) {
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + job.b * p.a.q_seq + node * p.a.q_tok +
+                                     (h * p.g + row - node * p.g) * p.a.q_head;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+            if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+          }
         }
       }
       job_done(n);
-      int page = page_of(off);
       for (int i = off; i < end; ++i, ++tile) {
         const int next = page_of(i + 1);
         const int r = (tile_slot(grp, i) + blk * kBlock) & (s.page_tokens - 1);
         const unsigned takes = __ballot_sync(kFull, page >= 0);
         const int64_t row = (((layer0 + page) * 2 + kv) * s.kv_heads + h) * s.page_tokens + r;
-        hold(kKEmpty + ks, kp);
-        if (lane == 0) mbar_expect_tx(bar + kKFull + ks, __popc(takes & 0xffu) * kBlock * D);
+        hold(empty + slot, parity);
+        if (lane == 0) mbar_expect_tx(bar + full + slot, __popc(takes) * kBlock * D);
         __syncwarp();
         if (page >= 0) {
-          if (!kv) bulk_copy(base + lay.k_ring + (ks * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kKFull + ks);
-          if (!kv)
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
-                             smem_u32(k_scales + (tile & (kScaleRing - 1)) * 8 + blk)),
-                         "l"(s.scales + (row >> 4))
-                         : "memory");
-        }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + kKFull + ks))
-                     : "memory");
-        hold(kVEmpty + vs, vp);
-        if (lane == 0) mbar_expect_tx(bar + kVFull + vs, __popc(takes & 0xff00u) * kBlock * D);
-        __syncwarp();
-        if (page >= 0 && kv) {
-          bulk_copy(base + lay.v_ring + (vs * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + kVFull + vs);
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(v_scales + vs * 8 + blk)),
+          bulk_copy(ring + (slot * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + full + slot);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
+                           smem_u32(kv ? v_scales + slot * 8 + blk : k_scales + (tile & (kScaleRing - 1)) * 8 + blk)),
                        "l"(s.scales + (row >> 4))
                        : "memory");
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + kVFull + vs))
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar + full + slot))
                      : "memory");
         page = next;
-        if (++ks == lay.nk) ks = 0, kp ^= 1u;
-        if (++vs == lay.nv) vs = 0, vp ^= 1u;
+        if (++slot == slots) slot = 0, parity ^= 1u;
       }
     }
     report(abort, s.status);
   } else if (warp == 1) {
     // ---- products, issued by one thread: S(t + 1) before O(t)
     const uint32_t id_s = instruction(N, 0, 0), id_o = instruction(N, 1, 1);
-    const uint32_t q_at = smem_u32(base + lay.q), w_at = smem_u32(base + lay.w), v_at = smem_u32(base + lay.wide_v);
+    const uint64_t q_op = operand(smem_u32(base + lay.q), 16), v_op = operand(smem_u32(base + lay.wide_v), 16384);
+    const uint64_t w_op = operand(smem_u32(base + lay.w), 16);
     int tile = 0, group = 0;
     auto out_product = [&](int t, bool first) {
       hold(kW + (t & 1), (t >> 1) & 1);
-      hold(kWideV, t & 1);
+      const int wide = t & (kWide - 1);
+      hold(kWideV + wide, (t / kWide) & 1);
       if (first) hold(kOFree, (group & 1) ^ 1);
       after_sync();
-      if (lane == 0) {
-#pragma unroll 2
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_ss(t_o, operand(v_at + k * 2048, 16384), operand(w_at + (t & 1) * N * 256 + (k >> 2) * N * 128 + (k & 3) * 32, 16),
-                 id_o, !(first && k == 0));
+      if (elected()) {
+        const uint64_t v = v_op + (wide * (128 * D * 2) >> 4);
+        const uint64_t w = w_op + ((t & 1) * N * 256 >> 4);
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)   // 16 slots: 2048 bytes of V, 32 of a row of weights
+          mma_ss(t_o, v + k * (2048 >> 4), w + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), id_o, !(first && k == 0));
         commit_to(bar + kWFree + (t & 1));
-        commit_to(bar + kWideVFree);
+        commit_to(bar + kWideVFree + wide);
       }
       __syncwarp();
     };
@@ -406,10 +408,11 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         hold(kWideK, tile & 1);
         hold(kSFree + (tile & 1), ((tile >> 1) & 1) ^ 1);
         after_sync();
-        if (lane == 0) {
-#pragma unroll 2
+        if (elected()) {
+          const uint32_t to = t_s + (tile & 1) * N;
+#pragma unroll
           for (int k = 0; k < D / 16; ++k)
-            mma_ts(t_s + (tile & 1) * N, t_k + k * 8, operand(q_at + (k >> 2) * N * 128 + (k & 3) * 32, 16), id_s, k > 0);
+            mma_ts(to, t_k + k * 8, q_op + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), id_s, k > 0);
           commit_to(bar + kS + (tile & 1));
           commit_to(bar + kWideKFree);
         }
@@ -538,41 +541,50 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     // seen: bit i of the tile's blocks (two a warp)
     auto values = [&](int t, unsigned seen) {
       hold(kVFull + vs, vp);
-      hold(kWideVFree, (t & 1) ^ 1);
+      const int wide = t & (kWide - 1);
+      hold(kWideVFree + wide, ((t / kWide) & 1) ^ 1);
       const float* sc = v_scales + vs * 8 + w4 * 2;
       unsigned rest[2];
       const unsigned factor[2] = {value_factor(sc[0], rest[0]), value_factor(sc[1], rest[1])};
       const bool large = (seen >> (w4 * 2) & 1u && rest[0] != 0x3f803f80u) || (seen >> (w4 * 2) & 2u && rest[1] != 0x3f803f80u);
       const char* src = base + lay.v_ring + vs * kTile * D;
-      char* dst = base + lay.wide_v;
+      char* dst = base + lay.wide_v + wide * (128 * D * 2);
       constexpr int kChunks = D / 16;
-#pragma unroll 4
-      for (int it = 0; it < kChunks; ++it) {
-        const int pair = it * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
-        const int k = w4 * 32 + octet * 8 + (lane & 7);
-        uint4 y = *reinterpret_cast<const uint4*>(src + swizzled(k * D + chunk * 16));
-        const bool zero = !(seen >> (k >> 4) & 1u);
-        if (zero) y = uint4{0, 0, 0, 0};
-        uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
-        const unsigned f = zero ? 0u : octet & 2 ? factor[1] : factor[0];
-        to_bf16(y.x, f, a.x, a.y);
-        to_bf16(y.y, f, a.z, a.w);
-        to_bf16(y.z, f, b.x, b.y);
-        to_bf16(y.w, f, b.z, b.w);
-        if (large) {
-          const unsigned g = octet & 2 ? rest[1] : rest[0];
-          times_rest(a.x, g), times_rest(a.y, g), times_rest(a.z, g), times_rest(a.w, g);
-          times_rest(b.x, g), times_rest(b.y, g), times_rest(b.z, g), times_rest(b.w, g);
+#pragma unroll 1
+      for (int i0 = 0; i0 < kChunks; i0 += 4) {
+        uint4 y[4];   // read before anything is written: nothing to order between the rows
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pair = (i0 + i) * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+          y[i] = *reinterpret_cast<const uint4*>(src + swizzled((w4 * 32 + octet * 8 + (lane & 7)) * D + chunk * 16));
         }
-        char* line = dst + (chunk >> 2) * 16384 + k * 128;
-        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2) ^ (k & 7)) << 4)) = a;
-        *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2 + 1) ^ (k & 7)) << 4)) = b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pair = (i0 + i) * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+          const int k = w4 * 32 + octet * 8 + (lane & 7);
+          const bool zero = !(seen >> (k >> 4) & 1u);
+          if (zero) y[i] = uint4{0, 0, 0, 0};
+          uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
+          const unsigned f = zero ? 0u : octet & 2 ? factor[1] : factor[0];
+          to_bf16(y[i].x, f, a.x, a.y);
+          to_bf16(y[i].y, f, a.z, a.w);
+          to_bf16(y[i].z, f, b.x, b.y);
+          to_bf16(y[i].w, f, b.z, b.w);
+          if (large) {
+            const unsigned g = octet & 2 ? rest[1] : rest[0];
+            times_rest(a.x, g), times_rest(a.y, g), times_rest(a.z, g), times_rest(a.w, g);
+            times_rest(b.x, g), times_rest(b.y, g), times_rest(b.z, g), times_rest(b.w, g);
+          }
+          char* line = dst + (chunk >> 2) * 16384 + k * 128;
+          *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2) ^ (k & 7)) << 4)) = a;
+          *reinterpret_cast<uint4*>(line + ((((chunk & 3) * 2 + 1) ^ (k & 7)) << 4)) = b;
+        }
       }
       dev::fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(bar + kVEmpty + vs);
-        mbar_arrive(bar + kWideV);
+        mbar_arrive(bar + kWideV + wide);
       }
       if (++vs == lay.nv) vs = 0, vp ^= 1u;
     };
@@ -644,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         if (kb + 32 > len || (p.a.window > 0 && kb + 32 > p.a.sinks && kb <= len + min(p.a.L, p.a.n - 1) - p.a.window)) {
           // some slot is masked for some row: -inf in its place.  Dead columns
           // get zeros, whatever the slots that were not loaded hold.
-#pragma unroll 1
+#pragma unroll 2
           for (int j = 0; j < kSteps; ++j) {
             float x[8];
             load(j, x);
