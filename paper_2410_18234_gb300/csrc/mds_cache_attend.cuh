@@ -269,6 +269,53 @@ __device__ void plan(const Params& p, long long* prefix, Seq* seqs, int head_dim
   __syncthreads();
 }
 
+// ------------------------------------------------------------- the schedule
+//
+// One warp walks the block's part of the line and publishes its groups, kJobs
+// ahead: the divisions and searches stay out of the other warps' code and
+// registers.
+
+constexpr int kJobs = 4;
+
+// A group, or the block's piece of one, as the scheduler publishes it.
+struct Job {
+  int b, h, row0, off, cnt, tiles;             // cnt 0: the end
+  int q, len, live;                            // of the sequence
+  int first_block, last_block;                 // blocks of the grid that hold the group
+  Group grp;
+  __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
+};
+
+// The scheduler warp: c is the place of unit u0.
+__device__ __forceinline__ void schedule(const Params& p, const Seq* seqs, Cursor c, long long per, long long u0,
+                                         long long u1, Job* jobs, uint64_t* ready, uint64_t* taken, int* abort) {
+  const int lane = threadIdx.x & 31;
+  Group grp = group_of(p, seqs[c.b], c.rt);
+  long long u = u0;
+  for (int n = 0;; ++n) {
+    const int slot = n & (kJobs - 1);
+    wait(taken + slot, ((n / kJobs) & 1) ^ 1, abort);
+    const int cnt = u < u1 ? (int)min((long long)(grp.tiles - c.off), u1 - u) : 0;
+    if (lane == 0) {
+      Job& j = jobs[slot];
+      j.cnt = cnt;
+      if (cnt) {
+        const Seq q = seqs[c.b];
+        j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
+        j.q = q.q, j.len = q.len, j.live = q.live;
+        j.first_block = (int)((u - c.off) / per);
+        j.last_block = (int)((u - c.off + grp.tiles - 1) / per);
+        j.grp = grp;
+      }
+      mbar_arrive(ready + slot);
+    }
+    __syncwarp();
+    if (!cnt) break;
+    u += cnt;
+    if (u < u1) advance(p, seqs, c, grp);
+  }
+}
+
 // ---------------------------------------------------------- joining pieces
 //
 // A piece's partial sums: per row its reference, its normaliser, and D sums.

@@ -22,71 +22,88 @@ namespace cache {
 
 namespace {
 
-constexpr int kWarps = 8;                  // consumers; one more warp loads
 constexpr int kStageMax = 8;
-constexpr int kJoinStride = 80;            // floats of a joined row's 64 dimensions: rows 16 banks apart
+constexpr int kJoinStride = 68;   // floats of a joined row's 64 dimensions: two rows are 8 banks apart
 
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
-__device__ __forceinline__ void mma_f16(float* c, const uint4& a, unsigned b0, unsigned b1) {
+__device__ __forceinline__ void mma_f16(float* c, const unsigned* a, uint2 b) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
-__device__ __forceinline__ void mma_bf16(float* c, const unsigned* a, unsigned b0, unsigned b1) {
+__device__ __forceinline__ void mma_bf16(float* c, const unsigned* a, uint2 b) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
-
 __device__ __forceinline__ void ldmatrix_x4_trans(unsigned* r, unsigned addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr));
 }
-// ------------------------------------------------------- few rows: 16 or 32
+__device__ __forceinline__ unsigned transposed(unsigned x) {   // an 8 x 8 matrix of 16-bit numbers
+  unsigned r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+// Transposed, like the kernel for many rows: a product's 16 rows are slots or
+// dimensions, its 8 columns the attention's rows, so that up to 8 rows (one
+// token of 8 query heads) waste nothing of the product that an instruction
+// does, and hold 32 sums a lane where rows on the other side would hold 64.
 //
-// Each consumer warp takes one block of 16 slots of a tile for all the rows:
-// a warp's scores, weights and sums stay in its registers, its key and value
-// scales are two numbers, and the eight warps' sums meet once per group.
-// MT: 16-row tiles.  Q: terms of a query.  W: terms of a weight.
-template <typename T, int D, int MT>
+//   S^T [16 slots][8 rows] = K Q^T,   O^T [16 dimensions][8 rows] += V^T W^T
+//
+// A warp takes one block of 16 slots of a tile for all the rows: its scores,
+// weights and sums stay in registers, its key and value scales are two
+// numbers, and the warps' sums meet once per group.  kSets sets of eight warps
+// take the tiles in turn.
+//
+// Bound by the cache's bytes as far as the instructions go: about 300 for a
+// block of 4096 bytes (half of them widen the values to bfloat16).
+// NT: tiles of 8 rows.
+template <typename T, int D, int NT>
 struct Few {
-  static constexpr int kQ = sizeof(T) == 4 ? 2 : 1;
-  static constexpr int kW = sizeof(T) == 4 ? 3 : 1;
-  static constexpr int kRows = 16 * MT;
+  static constexpr int kQ = sizeof(T) == 4 ? 2 : 1;   // terms of a query
+  static constexpr int kW = sizeof(T) == 4 ? 3 : 1;   // terms of a weight
+  static constexpr int kSets = NT == 1 ? 2 : 1;
+  static constexpr int kWarps = 8 * kSets, kThreads = 32 * kWarps;   // consumers; then a loader and a scheduler
+  static constexpr int kRows = 8 * NT;
   static constexpr int kSteps = D / 16;
   static constexpr int kStageBytes = 2 * kTile * D;
-  static constexpr int kQBytes = MT * kQ * kSteps * 512;
-  static constexpr int kJoinBytes = kWarps * 16 * kJoinStride * 4;
+  static constexpr int kQBytes = NT * kQ * kSteps * 256;
+  static constexpr int kJoinBytes = kWarps * 8 * kJoinStride * 4;
   // after the stages: queries, join buffer, per-warp (reference, sum), row coefficients, stage scales, barriers
   static constexpr int kFixed =
-      kQBytes + kJoinBytes + kWarps * kRows * 8 + kRows * 4 + kStageMax * 16 * 4 + 2 * kStageMax * 8 + 16;
+      kQBytes + kJoinBytes + kWarps * kRows * 8 + kRows * 4 + kStageMax * 16 * 4 + (2 * kStageMax + 2 * kJobs) * 8 + kJobs * (int)sizeof(Job) + 16;
   static int smem(int stages, int B) { return 1024 + stages * kStageBytes + kFixed + (B + 1) * 8 + B * 16 + 16; }
 };
 
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_constant__ Params p) {
-  using F = Few<T, D, MT>;
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(const __grid_constant__ Params p) {
+  using F = Few<T, D, NT>;
   extern __shared__ char raw[];
   char* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   char* stage_mem = base;
   char* at = base + p.stages * F::kStageBytes;
-  uint4* qf = reinterpret_cast<uint4*>(at);
+  uint2* qf = reinterpret_cast<uint2*>(at);
   at += F::kQBytes;
   float* join = reinterpret_cast<float*>(at);
   at += F::kJoinBytes;
   float2* ml = reinterpret_cast<float2*>(at);
-  at += kWarps * F::kRows * 8;
+  at += F::kWarps * F::kRows * 8;
   float* coef = reinterpret_cast<float*>(at);
   at += F::kRows * 4;
   float* stage_scales = reinterpret_cast<float*>(at);
   at += kStageMax * 16 * 4;
   uint64_t* full = reinterpret_cast<uint64_t*>(at);
   uint64_t* empty = full + kStageMax;
-  at += 2 * kStageMax * 8;
+  uint64_t* ready = empty + kStageMax;
+  uint64_t* taken = ready + kJobs;
+  at += (2 * kStageMax + 2 * kJobs) * 8;
+  Job* jobs = reinterpret_cast<Job*>(at);
+  at += kJobs * sizeof(Job);
   int* abort = reinterpret_cast<int*>(at);
   int* last_s = abort + 1;
   at += 16;
@@ -99,7 +116,11 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
     *abort = 0;
     for (int i = 0; i < p.stages; ++i) {
       mbar_init(full + i, 1 + 32);       // the loader's byte count, and its lanes' scale copies
-      mbar_init(empty + i, kWarps);
+      mbar_init(empty + i, 8);
+    }
+    for (int i = 0; i < kJobs; ++i) {
+      mbar_init(ready + i, 1);
+      mbar_init(taken + i, F::kWarps + 1);
     }
     mbar_init_fence();
   }
@@ -109,26 +130,39 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
   const long long u0 = per * blockIdx.x, u1 = min(u0 + per, total);
   if (u0 >= u1) return;
 
-  Cursor c = locate(p, prefix, seqs, u0);
-  Group grp = group_of(p, seqs[c.b], c.rt);
-  long long u = u0;
+  if (warp == F::kWarps + 1) {
+    schedule(p, seqs, locate(p, prefix, seqs, u0), per, u0, u1, jobs, ready, taken, abort);
+    return;
+  }
+  auto job_at = [&](int n) -> const Job& {
+    wait(ready + (n & (kJobs - 1)), (n / kJobs) & 1, abort);
+    return jobs[n & (kJobs - 1)];
+  };
+  auto job_done = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(taken + (n & (kJobs - 1)));
+  };
 
-  if (warp == kWarps) {
+  if (warp == F::kWarps) {
     // ---- loader: one block of 16 slots a lane (keys: lanes 0..7, values: 8..15)
     const State& s = p.s;
     const int kv = (lane >> 3) & 1, blk = lane & 7;
     const int64_t layer0 = (int64_t)p.a.layer * s.pages;
     int stage = 0;
     unsigned phase = 1;
-    while (u < u1) {
-      const int cnt = (int)min((long long)(grp.tiles - c.off), u1 - u);
-      const int32_t* table = s.table + (int64_t)seqs[c.b].q * s.max_pages;
+    for (int n = 0;; ++n) {
+      const Job& job = job_at(n);
+      const int off = job.off, end = off + job.cnt, h = job.h;
+      if (!job.cnt) break;
+      const Group grp = job.grp;
+      const int32_t* table = s.table + (int64_t)job.q * s.max_pages;
+      job_done(n);
       auto page_of = [&](int i) {
         const int t = tile_slot(grp, i) + blk * kBlock;
-        return lane < 16 && i < c.off + cnt && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
+        return lane < 16 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
       };
-      int page = page_of(c.off);
-      for (int i = c.off; i < c.off + cnt; ++i) {
+      int page = page_of(off);
+      for (int i = off; i < end; ++i) {
         const int next = page_of(i + 1);
         const int t = tile_slot(grp, i) + blk * kBlock;
         wait(empty + stage, phase, abort);
@@ -136,7 +170,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
         if (lane == 0) mbar_expect_tx(full + stage, __popc(takes) * kBlock * D);
         __syncwarp();
         if (page >= 0) {
-          const int64_t tile = ((layer0 + page) * 2 + kv) * s.kv_heads + c.h;
+          const int64_t tile = ((layer0 + page) * 2 + kv) * s.kv_heads + h;
           const int r = t & (s.page_tokens - 1);
           const uint8_t* src = s.pool + (tile * s.page_tokens + r) * D;
           bulk_copy(stage_mem + stage * F::kStageBytes + (kv * kTile + blk * kBlock) * D, src, kBlock * D, full + stage);
@@ -149,15 +183,14 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
         page = next;
         if (++stage == p.stages) stage = 0, phase ^= 1u;
       }
-      u += cnt;
-      if (u < u1 && !advance(p, seqs, c, grp)) break;
     }
     report(abort, s.status);
     return;
   }
 
   // ---- consumers
-  const int gr = lane >> 2, tq = lane & 3;
+  auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(F::kThreads) : "memory"); };
+  const int gr = lane >> 2, tq = lane & 3, set = warp >> 3, blk = warp & 7;
   unsigned k_at[2][D / 64], v_at[D / 32];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
@@ -168,18 +201,18 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
     const int key = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * x + (lane >> 4);
     v_at[x] = swizzled(key * D + chunk * 16);
   }
-  int stage = 0;
+  int stage = 0, turn = 0;
   unsigned phase = 0;
-  while (u < u1) {
-    const Seq q = seqs[c.b];
-    const int cnt = (int)min((long long)(grp.tiles - c.off), u1 - u);
-    const int row0 = c.rt * F::kRows;
+  for (int n = 0;; ++n) {
+    const Job& job = job_at(n);
+    if (!job.cnt) break;
+    const int row0 = job.row0;
     // queries of the group: scaled, in the order of the products' fragments
-    for (int r = warp; r < F::kRows; r += kWarps) {
-      const int row = row0 + r, node = row / p.g, head = c.h * p.g + row % p.g;
+    for (int r = warp; r < F::kRows; r += F::kWarps) {
+      const int row = row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
       float x[4] = {0.f, 0.f, 0.f, 0.f};
-      if (lane * 4 < D && node < q.live) {
-        const T* src = static_cast<const T*>(p.a.q) + c.b * p.a.q_seq + node * p.a.q_tok + head * p.a.q_head + lane * 4;
+      if (lane * 4 < D && node < job.live) {
+        const T* src = static_cast<const T*>(p.a.q) + job.b * p.a.q_seq + node * p.a.q_tok + head * p.a.q_head + lane * 4;
         if constexpr (sizeof(T) == 4) {
           const float4 y = __ldg(reinterpret_cast<const float4*>(src));
           x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
@@ -197,7 +230,6 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
       if (lane == 0) coef[r] = p.a.scale * dev::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
       if (lane * 4 < D) {
         const int chunk = lane >> 2, step = (chunk >> 2) * 4 + (lane & 3), to = (r & 7) * 4 + (chunk & 3);
-        const int half = (r >> 3) & 1, mt = r >> 4;
 #pragma unroll
         for (int term = 0; term < F::kQ; ++term) {
           unsigned w[2];
@@ -211,233 +243,227 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
             const __half2 hh = __floats2half2_rn(y0, y1);
             w[i] = *reinterpret_cast<const unsigned*>(&hh);
           }
-          unsigned* dst = reinterpret_cast<unsigned*>(qf + ((mt * F::kQ + term) * F::kSteps + step) * 32 + to);
-          dst[half] = w[0];
-          dst[2 + half] = w[1];
+          qf[(((r >> 3) * F::kQ + term) * F::kSteps + step) * 32 + to] = uint2{w[0], w[1]};
         }
       }
     }
-    // the rows' nodes
-    int node[MT][2], own[MT][2];   // node, and the first node of its branch
+    // this lane's rows, 2 tq and 2 tq + 1 of each tile of 8
+    int node[NT][2], own[NT][2];   // node, and the first node of its branch
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int i = (row0 + m * 16 + x * 8 + gr) / p.g;
+        const int i = (row0 + m * 8 + tq * 2 + x) / p.g;
         node[m][x] = i;
         own[m][x] = i > 0 && p.a.L > 0 ? 1 + (i - 1) / p.a.L * p.a.L : 1;
       }
     consumers_sync();
-    float rc[MT][2], ref[MT][2], sum[MT][2], acc[MT][D / 16][2][4];
+    float rc[NT][2], ref[NT][2], sum[NT][2], acc[NT][D / 16][4];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        rc[m][x] = coef[m * 16 + x * 8 + gr];
+        rc[m][x] = coef[m * 8 + tq * 2 + x];
         ref[m][x] = kNone;
         sum[m][x] = 0.f;
       }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int x = 0; x < D / 16; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int z = 0; z < 4; ++z) acc[m][x][y][z] = 0.f;
+        for (int z = 0; z < 4; ++z) acc[m][x][z] = 0.f;
 
-    for (int i = c.off; i < c.off + cnt; ++i) {
-      const int t0 = tile_slot(grp, i) + warp * kBlock;
-      wait(full + stage, phase, abort);
-      if (block_seen(grp, t0)) {
-        const char* kb = stage_mem + stage * F::kStageBytes + warp * kBlock * D;
-        const unsigned vb = smem_u32(kb + kTile * D);
-        const float ks = stage_scales[stage * 16 + warp], vs = stage_scales[stage * 16 + 8 + warp];
-        float sc[MT][2][4];
+    const Group grp = job.grp;
+    const int off = job.off, end = off + job.cnt, len = job.len;
+    for (int i = off; i < end; ++i) {
+      const int t0 = tile_slot(grp, i) + blk * kBlock;
+      if ((turn++ & (F::kSets - 1)) == set) {
+        wait(full + stage, phase, abort);
+        if (block_seen(grp, t0)) {
+          const char* kb = stage_mem + stage * F::kStageBytes + blk * kBlock * D;
+          const unsigned vb = smem_u32(kb + kTile * D);
+          const float ks = stage_scales[stage * 16 + blk], vs = stage_scales[stage * 16 + 8 + blk];
+          // scores: x[m][2 h + r] of slot t0 + gr + 8 h and row 2 tq + r; even and
+          // odd steps into sums of their own, for shorter chains of products
+          float sc[2][NT][4];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) sc[m][j][z] = 0.f;
+              for (int z = 0; z < 4; ++z) sc[h][m][z] = 0.f;
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) {
-          uint4 kx[2];
+          for (int x = 0; x < D / 64; ++x) {
+            const uint4 k0 = *reinterpret_cast<const uint4*>(kb + k_at[0][x]);
+            const uint4 k1 = *reinterpret_cast<const uint4*>(kb + k_at[1][x]);
+            const unsigned w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-          for (int j = 0; j < 2; ++j) kx[j] = *reinterpret_cast<const uint4*>(kb + k_at[j][x]);
+            for (int y = 0; y < 4; ++y) {
+              unsigned a[4];
+              to_f16(w0[y], a[0], a[2]);
+              to_f16(w1[y], a[1], a[3]);
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            unsigned b[2][2];
+              for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) to_f16(y == 0 ? kx[j].x : y == 1 ? kx[j].y : y == 2 ? kx[j].z : kx[j].w, b[j][0], b[j][1]);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-              for (int term = 0; term < F::kQ; ++term) {
-                const uint4 a = qf[((m * F::kQ + term) * F::kSteps + x * 4 + y) * 32 + lane];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) mma_f16(sc[m][j], a, b[j][0], b[j][1]);
-              }
-          }
-        }
-        // scores in log2 units, masked
-        const bool plain = t0 + kBlock <= q.len &&
-                           (p.a.window <= 0 || t0 + kBlock <= p.a.sinks || t0 > q.len + min(p.a.L, p.a.n - 1) - p.a.window);
-        bool moves = false;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const float f = rc[m][x] * ks;
-            float top = kNone;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                float y = sc[m][j][2 * x + z] * f;
-                if (!plain) {
-                  const int t = t0 + j * 8 + tq * 2 + z, at_node = t - q.len, i_row = node[m][x], b0 = own[m][x];
-                  bool see = at_node <= i_row && (at_node <= 0 || at_node >= b0);
-                  if (p.a.window > 0) {
-                    const int pos = at_node <= 0 ? t : q.len + at_node - b0 + 1;
-                    const int mine = q.len + (i_row > 0 ? i_row - b0 + 1 : 0);
-                    see = see && (pos < p.a.sinks || pos > mine - p.a.window);
-                  }
-                  y = see && t < grp.hi ? y : dev::kNegInf;
-                }
-                sc[m][j][2 * x + z] = y;
-                top = fmaxf(top, y);
-              }
-            moves |= top > ref[m][x] + kSlack;
-          }
-        if (__any_sync(kFull, moves)) {
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            float alpha[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float top = fmaxf(fmaxf(sc[m][0][2 * x], sc[m][0][2 * x + 1]), fmaxf(sc[m][1][2 * x], sc[m][1][2 * x + 1]));
-              top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
-              top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
-              top = fmaxf(top, ref[m][x]);
-              alpha[x] = ex2(ref[m][x] - top);
-              ref[m][x] = top;
-              sum[m][x] *= alpha[x];
+                for (int term = 0; term < F::kQ; ++term)
+                  mma_f16(sc[y & 1][m], a, qf[((m * F::kQ + term) * F::kSteps + x * 4 + y) * 32 + lane]);
             }
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-              for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) acc[m][x][y][z] *= alpha[z >> 1];
           }
-        }
-        // weights, as the next product's rows; the values' scale goes to the values
-        unsigned w[MT][F::kW][4];
-        unsigned rest;
-        const unsigned factor = value_factor(vs, rest);
+          // in log2 units, masked
+          const bool plain = t0 + kBlock <= len &&
+                             (p.a.window <= 0 || t0 + kBlock <= p.a.sinks || t0 > len + min(p.a.L, p.a.n - 1) - p.a.window);
+          float w[NT][4];
+          bool moves = false;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+          for (int m = 0; m < NT; ++m)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+            for (int z = 0; z < 4; ++z) w[m][z] = (sc[0][m][z] + sc[1][m][z]) * (rc[m][z & 1] * ks);
+          if (!plain) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float w0 = ex2(sc[m][j][2 * x] - ref[m][x]), w1 = ex2(sc[m][j][2 * x + 1] - ref[m][x]);
-              if constexpr (F::kW > 1) sum[m][x] += w0 + w1;
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const int t = t0 + (z >> 1) * 8 + gr, at_node = t - len, i_row = node[m][z & 1], b0 = own[m][z & 1];
+                bool see = at_node <= i_row && (at_node <= 0 || at_node >= b0) && t < grp.hi;
+                if (p.a.window > 0) {
+                  const int pos = at_node <= 0 ? t : len + at_node - b0 + 1;
+                  const int mine = len + (i_row > 0 ? i_row - b0 + 1 : 0);
+                  see = see && (pos < p.a.sinks || pos > mine - p.a.window);
+                }
+                if (!see) w[m][z] = dev::kNegInf;
+              }
+          }
+#pragma unroll
+          for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) moves |= fmaxf(w[m][r], w[m][2 + r]) > ref[m][r] + kSlack;
+          if (__any_sync(kFull, moves)) {
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
+              float alpha[2];
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                float top = fmaxf(w[m][r], w[m][2 + r]);
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+                top = fmaxf(top, ref[m][r]);
+                alpha[r] = ex2(ref[m][r] - top);
+                ref[m][r] = top;
+                sum[m][r] *= alpha[r];
+              }
+#pragma unroll
+              for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) acc[m][x][z] *= alpha[z & 1];
+            }
+          }
+          // weights; the values' scale goes to the values
+          uint2 b[NT][F::kW];
+#pragma unroll
+          for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float w0 = ex2(w[m][2 * h] - ref[m][0]), w1 = ex2(w[m][2 * h + 1] - ref[m][1]);
+              if constexpr (F::kW > 1) sum[m][0] += w0, sum[m][1] += w1;
 #pragma unroll
               for (int term = 0; term < F::kW; ++term) {
                 const unsigned pk = pack_bf16(w0, w1);
                 const float r0 = __uint_as_float(pk << 16), r1 = __uint_as_float(pk & 0xffff0000u);
-                if constexpr (F::kW == 1) sum[m][x] += r0 + r1;
+                if constexpr (F::kW == 1) sum[m][0] += r0, sum[m][1] += r1;
                 w0 -= r0;
                 w1 -= r1;
-                w[m][term][2 * j + x] = pk;
+                (h ? b[m][term].y : b[m][term].x) = transposed(pk);
               }
             }
+          unsigned rest;
+          const unsigned factor = value_factor(vs, rest);
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x) {
-          unsigned v[4];
-          ldmatrix_x4_trans(v, vb + v_at[x]);
+          for (int x = 0; x < D / 32; ++x) {
+            unsigned v[4];
+            ldmatrix_x4_trans(v, vb + v_at[x]);
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            unsigned e0, o0, e1, o1;
-            to_bf16(v[2 * y], factor, e0, o0);
-            to_bf16(v[2 * y + 1], factor, e1, o1);
-            if (rest != 0x3f803f80u) times_rest(e0, rest), times_rest(o0, rest), times_rest(e1, rest), times_rest(o1, rest);
+            for (int y = 0; y < 2; ++y) {
+              unsigned a[4];   // even and odd dimensions of 8 slots, then of the other 8
+              to_bf16(v[2 * y], factor, a[0], a[1]);
+              to_bf16(v[2 * y + 1], factor, a[2], a[3]);
+              if (rest != 0x3f803f80u) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-              for (int term = 0; term < F::kW; ++term) {
-                mma_bf16(acc[m][2 * x + y][0], w[m][term], e0, e1);
-                mma_bf16(acc[m][2 * x + y][1], w[m][term], o0, o1);
+                for (int z = 0; z < 4; ++z) times_rest(a[z], rest);
               }
+#pragma unroll
+              for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int term = 0; term < F::kW; ++term) mma_bf16(acc[m][2 * x + y], a, b[m][term]);
+            }
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty + stage);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty + stage);
       if (++stage == p.stages) stage = 0, phase ^= 1u;
     }
 
-    // ---- the eight warps' sums meet
+    // ---- the warps' sums meet
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float l = sum[m][x];
-        l += __shfl_xor_sync(kFull, l, 1);
-        l += __shfl_xor_sync(kFull, l, 2);
-        if (tq == 0) ml[warp * F::kRows + m * 16 + x * 8 + gr] = float2{ref[m][x], l};
+      for (int r = 0; r < 2; ++r) {
+        float l = sum[m][r];
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l += __shfl_xor_sync(kFull, l, d);
+        if (gr == 0) ml[warp * F::kRows + m * 8 + tq * 2 + r] = float2{ref[m][r], l};
       }
     consumers_sync();
-    const bool whole = c.off == 0 && cnt == grp.tiles;
-    const long long g0 = u - c.off;                       // the group's first unit
-    const int c0 = (int)(g0 / per), c1 = (int)((g0 + grp.tiles - 1) / per);
-    float* part = piece_of(p, blockIdx.x, c.off == 0, D);
+    const bool whole = job.whole();
+    float* part = piece_of(p, blockIdx.x, off == 0, D);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int m = 0; m < NT; ++m) {
       float f[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int r = 0; r < 2; ++r) {
         float top = kNone;
 #pragma unroll
-        for (int wq = 0; wq < kWarps; ++wq) top = fmaxf(top, ml[wq * F::kRows + m * 16 + x * 8 + gr].x);
-        f[x] = ex2(ref[m][x] - top);
+        for (int wq = 0; wq < F::kWarps; ++wq) top = fmaxf(top, ml[wq * F::kRows + m * 8 + tq * 2 + r].x);
+        f[r] = ex2(ref[m][r] - top);
       }
 #pragma unroll
       for (int hd = 0; hd < D / 64; ++hd) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            const float (*ac)[4] = acc[m][hd * 4 + ch];
-            *reinterpret_cast<float4*>(join + (warp * 16 + x * 8 + gr) * kJoinStride + ch * 16 + tq * 4) =
-                float4{ac[0][2 * x] * f[x], ac[1][2 * x] * f[x], ac[0][2 * x + 1] * f[x], ac[1][2 * x + 1] * f[x]};
+          for (int r = 0; r < 2; ++r) {
+            const float* ac = acc[m][hd * 4 + ch];
+            *reinterpret_cast<float2*>(join + (warp * 8 + tq * 2 + r) * kJoinStride + ch * 16 + gr * 2) =
+                float2{ac[r] * f[r], ac[2 + r] * f[r]};
           }
         consumers_sync();
-        const int r = tid >> 4, d = (tid & 15) * 4, row = row0 + m * 16 + r;
-        if (row / p.g < q.live) {
-          float4 o{0.f, 0.f, 0.f, 0.f};
-          float top = kNone, l = 0.f;
+        if (tid < 256) {
+          const int r = tid >> 5, d = lane * 2, row = row0 + m * 8 + r;
+          if (row / p.g < job.live) {
+            float2 o{0.f, 0.f};
+            float top = kNone, l = 0.f;
 #pragma unroll
-          for (int wq = 0; wq < kWarps; ++wq) {
-            const float4 y = *reinterpret_cast<const float4*>(join + (wq * 16 + r) * kJoinStride + d);
-            o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
-            top = fmaxf(top, ml[wq * F::kRows + m * 16 + r].x);
-          }
+            for (int wq = 0; wq < F::kWarps; ++wq) {
+              const float2 y = *reinterpret_cast<const float2*>(join + (wq * 8 + r) * kJoinStride + d);
+              o.x += y.x, o.y += y.y;
+              top = fmaxf(top, ml[wq * F::kRows + m * 8 + r].x);
+            }
 #pragma unroll
-          for (int wq = 0; wq < kWarps; ++wq) {
-            const float2 y = ml[wq * F::kRows + m * 16 + r];
-            l += y.y * ex2(y.x - top);
-          }
-          if (whole) {
-            const float inv = 1.f / l;
-            store4(out_row<T>(p, c.b, c.h, row, D) + hd * 64 + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
-          } else {
-            float* pr = part + (m * 16 + r) * (D + 2);
-            __stcg(reinterpret_cast<float2*>(pr + 2 + hd * 64 + d), float2{o.x, o.y});
-            __stcg(reinterpret_cast<float2*>(pr + 2 + hd * 64 + d) + 1, float2{o.z, o.w});
-            if (hd == 0 && (tid & 15) == 0) __stcg(reinterpret_cast<float2*>(pr), float2{top, l});
+            for (int wq = 0; wq < F::kWarps; ++wq) {
+              const float2 y = ml[wq * F::kRows + m * 8 + r];
+              l += y.y * ex2(y.x - top);
+            }
+            if (whole) {
+              const float inv = 1.f / l;
+              T* to = out_row<T>(p, job.b, job.h, row, D) + hd * 64 + d;
+              if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(to) = float2{o.x * inv, o.y * inv};
+              else *reinterpret_cast<unsigned*>(to) = pack_bf16(o.x * inv, o.y * inv);
+            } else {
+              float* pr = part + (m * 8 + r) * (D + 2);
+              __stcg(reinterpret_cast<float2*>(pr + 2 + hd * 64 + d), o);
+              if (hd == 0 && lane == 0) __stcg(reinterpret_cast<float2*>(pr), float2{top, l});
+            }
           }
         }
         consumers_sync();
@@ -448,59 +474,64 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 1) few_kernel(const __grid_
       __threadfence();
       consumers_sync();
       if (tid == 0) {
-        const bool last = atomicAdd(p.s.joins + c0, 1u) == (unsigned)(c1 - c0);
-        if (last) p.s.joins[c0] = 0;
+        const bool last = atomicAdd(p.s.joins + job.first_block, 1u) == (unsigned)(job.last_block - job.first_block);
+        if (last) p.s.joins[job.first_block] = 0;
         *last_s = last;
       }
       consumers_sync();
       if (*last_s) {
         __threadfence();
-        join_pieces<T, D>(p, c.b, c.h, row0, q.live, c0, c1, tid, kWarps * 32);
+        join_pieces<T, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, tid, F::kThreads);
       }
     }
-    u += cnt;
-    if (u < u1 && !advance(p, seqs, c, grp)) break;
+    job_done(n);
   }
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int NT>
 cudaError_t launch_few(const State& s, const Attend& a, int sms, cudaStream_t st) {
-  using F = Few<T, D, MT>;
+  using F = Few<T, D, NT>;
   Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, F::kRows};
   p.rows = a.n * p.g;
   p.row_tiles = (p.rows + F::kRows - 1) / F::kRows;
   const int grid = attend_grid(sms, F::kRows, D);
   p.stages = kStageMax;
   while (p.stages > 2 && F::smem(p.stages, a.B) > 227 * 1024) --p.stages;
-  few_kernel<T, D, MT><<<grid, 32 * (kWarps + 1), F::smem(p.stages, a.B), st>>>(p);
+  few_kernel<T, D, NT><<<grid, F::kThreads + 64, F::smem(p.stages, a.B), st>>>(p);
   return cudaGetLastError();
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int NT>
 cudaError_t configure_few() {
-  return cudaFuncSetAttribute(few_kernel<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  return cudaFuncSetAttribute(few_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
 }
 
 }  // namespace
 
 cudaError_t configure() {
   cudaError_t e = configure_few<float, 64, 1>();
+  if (e == cudaSuccess) e = configure_few<float, 64, 2>();
   if (e == cudaSuccess) e = configure_few<float, 128, 1>();
+  if (e == cudaSuccess) e = configure_few<float, 128, 2>();
   if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 64, 1>();
+  if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 64, 2>();
   if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 128, 1>();
+  if (e == cudaSuccess) e = configure_few<__nv_bfloat16, 128, 2>();
   if (e == cudaSuccess) e = configure_many();
   return e;
 }
 
-// Rows of 16-bit queries beyond one 16-row product go to the kernel of
-// mds_cache_many.cu.
+// Rows of 16-bit queries beyond 16 go to the kernel of mds_cache_many.cu.
 cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st) {
   const int64_t rows = (int64_t)a.n * (a.heads / s.kv_heads);
-  if (s.dtype == MDS_F32)
-    return s.head_dim == 64 ? launch_few<float, 64, 1>(s, a, sms, st) : launch_few<float, 128, 1>(s, a, sms, st);
+  if (s.dtype == MDS_F32) {
+    if (s.head_dim == 64) return rows > 8 ? launch_few<float, 64, 2>(s, a, sms, st) : launch_few<float, 64, 1>(s, a, sms, st);
+    return rows > 8 ? launch_few<float, 128, 2>(s, a, sms, st) : launch_few<float, 128, 1>(s, a, sms, st);
+  }
   if (rows > 16) return attend_many(s, a, sms, st);
-  return s.head_dim == 64 ? launch_few<__nv_bfloat16, 64, 1>(s, a, sms, st)
-                          : launch_few<__nv_bfloat16, 128, 1>(s, a, sms, st);
+  if (s.head_dim == 64)
+    return rows > 8 ? launch_few<__nv_bfloat16, 64, 2>(s, a, sms, st) : launch_few<__nv_bfloat16, 64, 1>(s, a, sms, st);
+  return rows > 8 ? launch_few<__nv_bfloat16, 128, 2>(s, a, sms, st) : launch_few<__nv_bfloat16, 128, 1>(s, a, sms, st);
 }
 
 }  // namespace cache

@@ -37,7 +37,6 @@ constexpr int kThreads = 32 * (12 + kWeigh);   // keys' loader, products, values
 constexpr int kMaxN = 144;      // columns: three buffers of them and 64 of keys in 512 of tensor memory
 constexpr int kRingMax = 5;
 constexpr int kScaleRing = 8;   // tiles whose scales are held: kRingMax + 3
-constexpr int kJobs = 4;        // groups the scheduler is ahead
 // Weights are 2^(score - reference), and sums of floats lose nothing by a
 // reference that is not the maximum: it only has to keep them in range.
 constexpr float kMostWeight = 0x1p48f, kLeastWeight = 0x1p-60f;
@@ -175,15 +174,6 @@ struct Row {
   int64_t out;     // its output's first element, -1: not one of the call's
 };
 
-// A group, or the block's piece of one, as the scheduler publishes it.
-struct Job {
-  int b, h, row0, off, cnt, tiles;             // cnt 0: the end
-  int q, len, live;                            // of the sequence
-  int first_block, last_block;                 // blocks of the grid that hold the group
-  Group grp;
-  __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
-};
-
 // Buffers of wide values: two where they leave room for the rings.
 __host__ __device__ constexpr int wide_buffers(int N) { return N <= 96 ? 2 : 1; }
 
@@ -297,30 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
   };
 
   if (warp == 3) {
-    // ---- scheduler
-    Group grp = group_of(p, seqs[c.b], c.rt);
-    long long u = u0;
-    for (int n = 0;; ++n) {
-      hold(kJobFree + (n & (kJobs - 1)), ((n / kJobs) & 1) ^ 1);
-      const int cnt = u < u1 ? (int)min((long long)(grp.tiles - c.off), u1 - u) : 0;
-      if (lane == 0) {
-        Job& j = jobs[n & (kJobs - 1)];
-        j.cnt = cnt;
-        if (cnt) {
-          const Seq q = seqs[c.b];
-          j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
-          j.q = q.q, j.len = q.len, j.live = q.live;
-          j.first_block = (int)((u - c.off) / per);
-          j.last_block = (int)((u - c.off + grp.tiles - 1) / per);
-          j.grp = grp;
-        }
-        mbar_arrive(bar + kJob + (n & (kJobs - 1)));
-      }
-      __syncwarp();
-      if (!cnt) break;
-      u += cnt;
-      if (u < u1) advance(p, seqs, c, grp);
-    }
+    schedule(p, seqs, c, per, u0, u1, jobs, bar + kJob, bar + kJobFree, abort);
   } else if (warp == 0 || warp == 2) {
     // ---- loaders, of keys and of values: one block of 16 slots a lane (0..7)
     const State& s = p.s;
