@@ -73,7 +73,7 @@ struct Few {
   static constexpr int kSteps = D / 16;
   static constexpr int kStageBytes = 2 * kTile * D;
   static constexpr int kQBytes = NT * kQ * kSteps * 256;
-  static constexpr int kJoinBytes = kWarps * 8 * kJoinStride * 4;
+  static constexpr int kJoinBytes = 8 * 8 * kJoinStride * 4;
   // after the stages: queries, join buffer, per-warp (reference, sum), row coefficients, stage scales, barriers
   static constexpr int kFixed =
       kQBytes + kJoinBytes + kWarps * kRows * 8 + kRows * 4 + kStageMax * 16 * 4 + (2 * kStageMax + 2 * kJobs) * 8 + kJobs * (int)sizeof(Job) + 16;
@@ -429,26 +429,35 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       }
 #pragma unroll
       for (int hd = 0; hd < D / 64; ++hd) {
+        // the sets after another: each adds what the one before left of its block
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch)
+        for (int st = F::kSets - 1; st >= 0; --st) {
+          if (set == st) {
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float* ac = acc[m][hd * 4 + ch];
-            *reinterpret_cast<float2*>(join + (warp * 8 + tq * 2 + r) * kJoinStride + ch * 16 + gr * 2) =
-                float2{ac[r] * f[r], ac[2 + r] * f[r]};
+            for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                const float* ac = acc[m][hd * 4 + ch];
+                float2* at = reinterpret_cast<float2*>(join + (blk * 8 + tq * 2 + r) * kJoinStride + ch * 16 + gr * 2);
+                float2 x{ac[r] * f[r], ac[2 + r] * f[r]};
+                if (st < F::kSets - 1) x.x += at->x, x.y += at->y;
+                *at = x;
+              }
           }
-        consumers_sync();
+          consumers_sync();
+        }
         if (tid < 256) {
           const int r = tid >> 5, d = lane * 2, row = row0 + m * 8 + r;
           if (row / p.g < job.live) {
             float2 o{0.f, 0.f};
             float top = kNone, l = 0.f;
 #pragma unroll
-            for (int wq = 0; wq < F::kWarps; ++wq) {
+            for (int wq = 0; wq < 8; ++wq) {
               const float2 y = *reinterpret_cast<const float2*>(join + (wq * 8 + r) * kJoinStride + d);
               o.x += y.x, o.y += y.y;
-              top = fmaxf(top, ml[wq * F::kRows + m * 8 + r].x);
             }
+#pragma unroll
+            for (int wq = 0; wq < F::kWarps; ++wq) top = fmaxf(top, ml[wq * F::kRows + m * 8 + r].x);
 #pragma unroll
             for (int wq = 0; wq < F::kWarps; ++wq) {
               const float2 y = ml[wq * F::kRows + m * 8 + r];
@@ -496,7 +505,10 @@ cudaError_t launch_few(const State& s, const Attend& a, int sms, cudaStream_t st
   p.row_tiles = (p.rows + F::kRows - 1) / F::kRows;
   const int grid = attend_grid(sms, F::kRows, D);
   p.stages = kStageMax;
-  while (p.stages > 2 && F::smem(p.stages, a.B) > 227 * 1024) --p.stages;
+  // A stage's tiles all belong to one set: a consumer waits for each of the
+  // stage's phases in turn (a wait tells two phases apart, not three).
+  static_assert(kStageMax % F::kSets == 0, "stages by sets");
+  while (p.stages > 2 && F::smem(p.stages, a.B) > 227 * 1024) p.stages -= F::kSets;
   few_kernel<T, D, NT><<<grid, F::kThreads + 64, F::smem(p.stages, a.B), st>>>(p);
   return cudaGetLastError();
 }
