@@ -100,6 +100,7 @@ class Cache:
 
     def __init__(self, layers, pages, kv_heads, head_dim, max_seqs, max_pages, page_tokens=64, dtype="bf16", device=0):
         self.device = torch.device("cuda", device)
+        self._index = int(device)
         self.layers, self.pages, self.page_tokens = int(layers), int(pages), int(page_tokens)
         self.kv_heads, self.head_dim = int(kv_heads), int(head_dim)
         self.max_seqs, self.max_pages = int(max_seqs), int(max_pages)
@@ -143,20 +144,21 @@ class Cache:
         """Address of an int32 tensor of this shape on the cache's device."""
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
             raise MdsError(MDS_EINVAL, f"{name}: contiguous int32 on {self.device}, got {t.dtype} on {t.device}")
-        if tuple(t.shape) != shape:
+        if t.shape != shape:
             raise MdsError(MDS_ESHAPE, f"{name} has shape {tuple(t.shape)}, expected {shape}")
         return t.data_ptr()
 
     def _seqs(self, seqs):
         if seqs.dim() != 1:
             raise MdsError(MDS_ESHAPE, f"seqs has shape {tuple(seqs.shape)}, expected (B,)")
-        return self._ints("seqs", seqs, (seqs.shape[0],)), seqs.shape[0]
+        B = seqs.shape[0]
+        return self._ints("seqs", seqs, (B,)), B
 
     def _rows(self, name, t, B, heads=None):
         """Check [B][n][heads][head_dim] of any strides but the last; strides of the first three axes."""
-        if t.dtype != self.dtype or t.device != self.device:
+        if t.dtype is not self.dtype or t.get_device() != self._index:
             raise MdsError(MDS_EINVAL, f"{name}: {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
         s = t.shape
         if len(s) != 4 or s[0] != B or s[3] != self.head_dim or (heads is not None and s[2] != heads):
@@ -173,7 +175,7 @@ class Cache:
             for t in given:
                 if tuple(t.shape) != shape:
                     raise MdsError(MDS_ESHAPE, f"out has shape {tuple(t.shape)}, expected {shape}")
-                if t.dtype != self.dtype or t.device != self.device or not t.is_contiguous():
+                if t.dtype is not self.dtype or t.get_device() != self._index or not t.is_contiguous():
                     raise MdsError(MDS_EINVAL, f"out: contiguous {self.dtype} on {self.device}")
             return given
         if isinstance(stream, torch.cuda.Stream):

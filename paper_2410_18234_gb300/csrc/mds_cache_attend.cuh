@@ -333,29 +333,44 @@ __device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, in
   return static_cast<T*>(p.a.out) + (node * p.a.heads + h * p.g + row % p.g) * head_dim;
 }
 
-// Add the pieces that blocks c0..c1 left of a row tile, in their order.
+// Add the pieces that blocks c0..c1 left of a row tile, in their order.  First
+// a warp a row finds its reference and normaliser (in `stat`, shared memory of
+// rows_per), then every thread adds four dimensions of a row.
 template <typename T, int D>
-__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, int tid, int threads) {
+__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, float2* stat, int tid,
+                            int threads) {
+  const int lane = tid & 31, stride = 2 * p.rows_per * (D + 2);
+  const float* first = piece_of(p, c0, true, D);
+  const float* later = piece_of(p, c0, false, D);   // + stride for each block further
+  for (int r = tid >> 5; r < p.rows_per; r += threads >> 5) {
+    float top = kNone, l = 0.f;
+    for (int cc = lane; cc <= c1 - c0; cc += 32)
+      top = fmaxf(top, __ldcg((cc ? later + (int64_t)cc * stride : first) + r * (D + 2)));
+#pragma unroll
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+    for (int cc = lane; cc <= c1 - c0; cc += 32) {
+      const float2 y = __ldcg(reinterpret_cast<const float2*>((cc ? later + (int64_t)cc * stride : first) + r * (D + 2)));
+      l += y.y * ex2(y.x - top);
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
+    if (lane == 0) stat[r] = float2{top, 1.f / l};
+  }
+  asm volatile("bar.sync 15, %0;" ::"r"(threads) : "memory");
   for (int x = tid; x < p.rows_per * (D / 4); x += threads) {
     const int r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
     if (row / p.g >= live) continue;
-    auto piece = [&](int cc) { return piece_of(p, cc, cc == c0, D) + r * (D + 2); };
-    float top = kNone;
-    for (int cc = c0; cc <= c1; ++cc) top = fmaxf(top, __ldcg(piece(cc)));
-    float l = 0.f;
+    const float2 st = stat[r];
     float4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int cc = c0; cc <= c1; ++cc) {
-      const float* pr = piece(cc);
-      const float2 y = __ldcg(reinterpret_cast<const float2*>(pr));
+#pragma unroll 8
+    for (int cc = 0; cc <= c1 - c0; ++cc) {
+      const float* pr = (cc ? later + (int64_t)cc * stride : first) + r * (D + 2);
+      const float f = ex2(__ldcg(pr) - st.x);
       const float2 a = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d));
       const float2 e = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d) + 1);
-      const float f = ex2(y.x - top);
-      l += y.y * f;
       o.x += a.x * f, o.y += a.y * f, o.z += e.x * f, o.w += e.y * f;
     }
-    const float inv = 1.f / l;
-    store4(out_row<T>(p, b, h, row, D) + d, float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+    store4(out_row<T>(p, b, h, row, D) + d, float4{o.x * st.y, o.y * st.y, o.z * st.y, o.w * st.y});
   }
 }
 

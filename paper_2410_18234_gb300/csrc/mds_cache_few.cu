@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       consumers_sync();
       if (*last_s) {
         __threadfence();
-        join_pieces<T, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, tid, F::kThreads);
+        join_pieces<T, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ml, tid, F::kThreads);
       }
     }
     job_done(n);

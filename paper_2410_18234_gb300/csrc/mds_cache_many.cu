@@ -894,7 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         weigh_sync();
         if (*last_s) {
           __threadfence();
-          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ht, 32 * kWeigh);
+          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, stat, ht, 32 * kWeigh);
         }
       }
       weigh_sync();   // the weights' place and stat have been read

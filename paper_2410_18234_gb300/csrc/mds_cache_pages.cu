@@ -90,27 +90,22 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const State 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int P = s.page_tokens;
   if (tid == 0) total = copied = freed = 0;
-  for (int b = warp; b < B; b += kPlanThreads / 32) {
+  for (int b = tid; b < B; b += kPlanThreads) {
     const int q = sequence(s, seqs, b);
     int2 c = {0, 0};
     if (q >= 0) {
       const int len = s.lens[q], held = s.held[q], k = live_count(counts, b, n);
       const int first = len >> s.page_log, end = (len + k + P - 1) >> s.page_log;
       if (k > 0 && end > s.max_pages) {
-        if (lane == 0) atomicOr(s.status, MDS_ST_NOPAGES);
+        atomicOr(s.status, MDS_ST_NOPAGES);
         c.x = -1;
       } else if (k > 0) {
         const int32_t* row = s.table + (int64_t)q * s.max_pages;
-        for (int p0 = first; p0 < end; p0 += 32) {
-          const int p = p0 + lane;
-          const bool in = p < end, absent = in && p >= held;
-          const bool shared = in && !absent && s.ref[row[p]] > 1;
-          c.x += __popc(__ballot_sync(kFull, absent || shared));
-          c.y += __popc(__ballot_sync(kFull, shared));
-        }
+        for (int p = first; p < min(end, held); ++p) c.y += s.ref[row[p]] > 1;
+        c.x = c.y + max(end - max(first, held), 0);
       }
     }
-    if (lane == 0) need[b] = c;
+    need[b] = c;
   }
   __syncthreads();
   // exclusive sums; a sequence beyond the free pages gets none
@@ -161,35 +156,37 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const State 
     }
   }
   __syncthreads();
-  // hand them out; which pages are shared is still as it was counted
-  for (int b = warp; b < B; b += kPlanThreads / 32) {
-    const int2 off = need[b];
+  // hand them out; which pages are shared is still as it was counted.  Pages
+  // held, a thread a sequence: there are few from slot len on; then the new
+  // ones, which may be thousands of a sequence, a warp a sequence.
+  for (int b = tid; b < B; b += kPlanThreads) {
+    int2 off = need[b];
     if (off.x < 0) continue;
     const int q = seqs[b];
     const int len = s.lens[q], held = s.held[q], k = live_count(counts, b, n);
-    const int first = len >> s.page_log, end = (len + k + P - 1) >> s.page_log;
+    const int end = (len + k + P - 1) >> s.page_log;
     int32_t* row = s.table + (int64_t)q * s.max_pages;
-    int at = off.x, cat = off.y;
-    for (int p0 = first; p0 < end; p0 += 32) {
-      const int p = p0 + lane;
-      const bool in = p < end, absent = in && p >= held;
-      const int old = in && !absent ? row[p] : -1;
-      const bool shared = old >= 0 && s.ref[old] > 1;
-      const unsigned get = __ballot_sync(kFull, absent || shared), cp = __ballot_sync(kFull, shared);
-      const unsigned below = (1u << lane) - 1u;
-      if (absent || shared) {
-        const int r = at + __popc(get & below);
-        row[p] = s.fresh[r];
-        if (shared) {
-          int32_t* c = s.copies + 3 * (int64_t)(cat + __popc(cp & below));
-          c[0] = old;
-          c[1] = s.fresh[r];
-          c[2] = min(P, len + k - p * P);
-        }
-      }
-      at += __popc(get);
-      cat += __popc(cp);
+    for (int p = len >> s.page_log; p < min(end, held); ++p) {
+      const int old = row[p];
+      if (s.ref[old] <= 1) continue;
+      const int fresh = s.fresh[off.x++];
+      row[p] = fresh;
+      int32_t* c = s.copies + 3 * (int64_t)off.y++;
+      c[0] = old;
+      c[1] = fresh;
+      c[2] = min(P, len + k - p * P);
     }
+    need[b].x = off.x;
+  }
+  __syncthreads();
+  for (int b = warp; b < B; b += kPlanThreads / 32) {
+    const int at = need[b].x;
+    if (at < 0) continue;
+    const int q = seqs[b];
+    const int len = s.lens[q], held = s.held[q], k = live_count(counts, b, n);
+    const int from = max(len >> s.page_log, held), end = (len + k + P - 1) >> s.page_log;
+    int32_t* row = s.table + (int64_t)q * s.max_pages;
+    for (int p = from + lane; p < end; p += 32) row[p] = s.fresh[at + p - from];
     __syncwarp();
     if (lane == 0 && end > held) s.held[q] = end;
   }
@@ -241,12 +238,121 @@ __global__ void __launch_bounds__(256) copy_kernel(const State s) {
 // ------------------------------------------------------------ the quantiser
 
 // A warp holds one block of one head: U = head_dim / 16 lanes a row, 16
-// values a lane, 32 / U rows at once, U / 2 times.
-template <int U>
+// values a lane, 32 / U rows at once, U / 2 times.  The kernels wait for
+// memory, not for arithmetic, so what a lane holds decides how many warps hide
+// that: bfloat16 inputs, and the values of stored bytes (exact in bfloat16),
+// stay packed.
+constexpr unsigned kInf = 0x7f800000u;   // magnitudes of floats order as their bits do
+
+template <typename T>
+struct Lane16;
+
+template <>
+struct Lane16<__nv_bfloat16> {
+  uint4 w[2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    w[0] = __ldg(reinterpret_cast<const uint4*>(p));
+    w[1] = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+  }
+  __device__ __forceinline__ void zero() { w[0] = w[1] = uint4{0, 0, 0, 0}; }
+  __device__ __forceinline__ unsigned get(int i) const {
+    const uint4& x = w[i >> 2];
+    return (i & 3) == 0 ? x.x : (i & 3) == 1 ? x.y : (i & 3) == 2 ? x.z : x.w;
+  }
+  __device__ __forceinline__ void set(int i, unsigned v) {
+    uint4& x = w[i >> 2];
+    ((i & 3) == 0 ? x.x : (i & 3) == 1 ? x.y : (i & 3) == 2 ? x.z : x.w) = v;
+  }
+  __device__ __forceinline__ void values(const float* v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __nv_bfloat162 x = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      set(i, *reinterpret_cast<const unsigned*>(&x));
+    }
+  }
+  // NaN becomes 0; the largest magnitude of the finite values, or kInf and
+  // more where any is not (then once more with `clean`)
+  template <bool clean>
+  __device__ __forceinline__ unsigned largest() {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      unsigned lo = get(i) << 16 & 0x7fff0000u, hi = get(i) & 0x7fff0000u;
+      if (clean) {
+        set(i, (lo > kInf ? 0u : get(i) & 0xffffu) | (hi > kInf ? 0u : get(i) & 0xffff0000u));
+        lo = lo >= kInf ? 0u : lo;
+        hi = hi >= kInf ? 0u : hi;
+      }
+      m = max(m, max(lo, hi));
+    }
+    return m;
+  }
+  __device__ __forceinline__ float at(int i) const {
+    return __uint_as_float(i & 1 ? get(i >> 1) & 0xffff0000u : get(i >> 1) << 16);
+  }
+};
+
+template <>
+struct Lane16<float> {
+  float v[16];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = __ldg(reinterpret_cast<const float4*>(p) + i);
+      v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+  }
+  __device__ __forceinline__ void values(const float* x) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = x[i];
+  }
+  template <bool clean>
+  __device__ __forceinline__ unsigned largest() {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      unsigned x = __float_as_uint(v[i]) & 0x7fffffffu;
+      if (clean) {
+        if (x > kInf) v[i] = 0.f;
+        x = x >= kInf ? 0u : x;
+      }
+      m = max(m, x);
+    }
+    return m;
+  }
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+};
+
+template <typename T, int U>
 struct Block {
   static constexpr int kPasses = U / 2;
   static constexpr int kRows = 32 / U;
-  float v[kPasses][16];
+  Lane16<T> v[kPasses];
+
+  // The scale: the least e in [-117, 119] with max <= 448 * 2^e, from the
+  // maximum's exponent x and mantissa m: 448 = 1.75 * 2^8, so e = x - 8 if
+  // m <= 1.75, else x - 7.  Lane-uniform.  Returns 2^e and sets inv to 2^-e.
+  __device__ __forceinline__ float scale(float* inv, bool* odd) {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) m = max(m, v[i].template largest<false>());
+    unsigned bits = __reduce_max_sync(kFull, m);
+    *odd = bits >= kInf;
+    if (*odd) {
+      m = 0;
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) m = max(m, v[i].template largest<true>());
+      bits = __reduce_max_sync(kFull, m);
+    }
+    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = bits == 0 ? 0 : min(max(e, -117), 119);
+    *inv = __uint_as_float((unsigned)(127 - e) << 23);
+    return __uint_as_float((unsigned)(127 + e) << 23);
+  }
 };
 
 __device__ __forceinline__ void decode16(const uint4& x, float scale, float* v) {
@@ -266,72 +372,27 @@ __device__ __forceinline__ void decode16(const uint4& x, float scale, float* v) 
   }
 }
 
-__device__ __forceinline__ uint4 encode16(const float* v, float inv) {
+template <typename T>
+__device__ __forceinline__ uint4 encode16(const Lane16<T>& v, float inv) {
   unsigned w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
         "mov.b32 %0, {a, b};\n\t}"
         : "=r"(w[i])
-        : "f"(v[4 * i] * inv), "f"(v[4 * i + 1] * inv), "f"(v[4 * i + 2] * inv), "f"(v[4 * i + 3] * inv));
+        : "f"(v.at(4 * i) * inv), "f"(v.at(4 * i + 1) * inv), "f"(v.at(4 * i + 2) * inv), "f"(v.at(4 * i + 3) * inv));
   }
   return uint4{w[0], w[1], w[2], w[3]};
 }
 
-// The block's scale: the least e in [-117, 119] with max <= 448 * 2^e, from
-// the maximum's exponent x and mantissa m: 448 = 1.75 * 2^8, so e = x - 8 if
-// m <= 1.75, else x - 7.  Lane-uniform.  Returns 2^e and sets inv to 2^-e.
-template <int U>
-__device__ __forceinline__ float block_scale(const Block<U>& blk, float* inv) {
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < Block<U>::kPasses; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float x = fabsf(blk.v[i][j]);
-      a = fmaxf(a, x <= 3.402823466e38f ? x : 0.f);
-    }
-  const unsigned bits = __reduce_max_sync(kFull, __float_as_uint(a));   // non-negative floats order as integers
-  int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-  e = bits == 0 ? 0 : min(max(e, -117), 119);
-  *inv = __uint_as_float((unsigned)(127 - e) << 23);
-  return __uint_as_float((unsigned)(127 + e) << 23);
-}
-
 // ------------------------------------------------------------------- append
-
-template <typename T>
-__device__ __forceinline__ void load16(const T* p, float* v);
-template <>
-__device__ __forceinline__ void load16<float>(const float* p, float* v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 x = __ldg(reinterpret_cast<const float4*>(p) + i);
-    v[4 * i] = x.x;
-    v[4 * i + 1] = x.y;
-    v[4 * i + 2] = x.z;
-    v[4 * i + 3] = x.w;
-  }
-}
-template <>
-__device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16* p, float* v) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i);
-    const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-      v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    }
-  }
-}
 
 // One warp per (sequence, block, key or value, head), heads next to one
 // another: what the warps of a block of threads read is contiguous.  Bound by
-// the bytes of the new tokens in and the blocks out.
+// the latency of the lookups (sequence, length, page) in front of the new
+// tokens' bytes, and by those.
 template <typename T, int U>
-__global__ void __launch_bounds__(256) append_kernel(const State s, int layer, const int32_t* seqs,
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) append_kernel(const State s, int layer, const int32_t* seqs,
                                                      const int32_t* counts, const T* k, longlong3 ks, const T* v,
                                                      longlong3 vs, int n, int nb, int64_t units) {
   const int lane = threadIdx.x & 31;
@@ -346,42 +407,43 @@ __global__ void __launch_bounds__(256) append_kernel(const State s, int layer, c
   const int len = s.lens[q], c = live_count(counts, b, n);
   const int t0 = (len / kBlock + j) * kBlock;
   if (c == 0 || t0 >= len + c) return;
+  using Blk = Block<T, U>;
+  Blk blk;
+  const int row = lane / U, unit = lane % U;
+  const longlong3 st = kv ? vs : ks;
+  const T* src = (kv ? v : k) + b * st.x + h * st.z + unit * 16;
+#pragma unroll
+  for (int i = 0; i < Blk::kPasses; ++i) {
+    const int t = t0 + i * Blk::kRows + row;
+    if (t >= len && t < len + c) blk.v[i].load(src + (int64_t)(t - len) * st.y);
+    else blk.v[i].zero();
+  }
   const int page = page_at(s, q, t0);
   if (page < 0 || s.ref[page] > 1) {
     if (lane == 0) atomicOr(s.status, MDS_ST_BADSEQ);
     return;
   }
-  using Blk = Block<U>;
-  Blk blk;
-  const int row = lane / U, unit = lane % U;
   const int64_t tile = tile_of(s, layer, page, kv, h);
   const int r0 = t0 & (s.page_tokens - 1);
   uint8_t* base = s.pool + tile * (s.page_tokens * s.head_dim) + r0 * s.head_dim;
   float* scale_at = s.scales + tile * (s.page_tokens / kBlock) + r0 / kBlock;
-  const longlong3 st = kv ? vs : ks;
-  const T* src = (kv ? v : k) + b * st.x + h * st.z + unit * 16;
-  const float was = t0 < len ? *scale_at : 0.f;
-  bool odd = false;
+  float was = 0.f;
+  if (t0 < len) {
+    was = *scale_at;
 #pragma unroll
-  for (int i = 0; i < Blk::kPasses; ++i) {
-    const int r = i * Blk::kRows + row, t = t0 + r;
-    if (t < len) {
-      decode16(*reinterpret_cast<const uint4*>(base + swizzled(r * s.head_dim + unit * 16)), was, blk.v[i]);
-    } else if (t < len + c) {
-      load16(src + (int64_t)(t - len) * st.y, blk.v[i]);
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        odd |= !(fabsf(blk.v[i][x]) <= 3.402823466e38f);
-        if (blk.v[i][x] != blk.v[i][x]) blk.v[i][x] = 0.f;
+    for (int i = 0; i < Blk::kPasses; ++i) {
+      const int r = i * Blk::kRows + row;
+      if (t0 + r < len) {
+        float x[16];
+        decode16(*reinterpret_cast<const uint4*>(base + swizzled(r * s.head_dim + unit * 16)), was, x);
+        blk.v[i].values(x);
       }
-    } else {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) blk.v[i][x] = 0.f;
     }
   }
-  if (odd) atomicOr(s.status, MDS_ST_NONFINITE);
   float inv;
-  const float scale = block_scale(blk, &inv);
+  bool odd;
+  const float scale = blk.scale(&inv, &odd);
+  if (odd && lane == 0) atomicOr(s.status, MDS_ST_NONFINITE);
   if (lane == 0) *scale_at = scale;
 #pragma unroll
   for (int i = 0; i < Blk::kPasses; ++i) {
@@ -399,7 +461,7 @@ __global__ void __launch_bounds__(256) append_kernel(const State s, int layer, c
 // behind it lie behind it.  One warp moves one tile's blocks in that order.
 // The last of a sequence's blocks of threads to finish shortens the sequence.
 template <int U>
-__global__ void __launch_bounds__(256) commit_kernel(const State s, const int32_t* seqs, const int32_t* accept,
+__global__ void __launch_bounds__(256, 3) commit_kernel(const State s, const int32_t* seqs, const int32_t* accept,
                                                      const int32_t* drafts, const int32_t* out_tokens, int K, int L) {
   __shared__ int branch_s, last_s;
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -434,7 +496,7 @@ __global__ void __launch_bounds__(256) commit_kernel(const State s, const int32_
     a = -1;
   }
   if (!bad && shift) {
-    using Blk = Block<U>;
+    using Blk = Block<__nv_bfloat16, U>;
     const int tiles = s.layers * 2 * s.kv_heads;
     const int row = lane / U, unit = lane % U;
     const int tile_bytes = s.page_tokens * s.head_dim, per = s.page_tokens / kBlock;
@@ -442,29 +504,36 @@ __global__ void __launch_bounds__(256) commit_kernel(const State s, const int32_
       const int layer = x / (2 * s.kv_heads), kvh = x % (2 * s.kv_heads);
       for (int t0 = (len + 1) / kBlock * kBlock; t0 <= len + a; t0 += kBlock) {
         Blk blk;
+        uint4 bytes[Blk::kPasses];
+        float sc[Blk::kPasses];
 #pragma unroll
         for (int i = 0; i < Blk::kPasses; ++i) {
           const int t = t0 + i * Blk::kRows + row;
+          bytes[i] = uint4{0, 0, 0, 0};
+          sc[i] = 0.f;
           if (t <= len + a) {
             const int from = t <= len ? t : t + (int)shift, fr = from & (s.page_tokens - 1);
             const int64_t tile = tile_of(s, layer, table[from >> s.page_log], 0, kvh);
-            const float sc = s.scales[tile * per + fr / kBlock];
-            decode16(*reinterpret_cast<const uint4*>(s.pool + tile * tile_bytes + swizzled(fr * s.head_dim + unit * 16)),
-                     sc, blk.v[i]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) blk.v[i][e] = 0.f;
+            sc[i] = s.scales[tile * per + fr / kBlock];
+            bytes[i] = *reinterpret_cast<const uint4*>(s.pool + tile * tile_bytes + swizzled(fr * s.head_dim + unit * 16));
           }
         }
+#pragma unroll
+        for (int i = 0; i < Blk::kPasses; ++i) {
+          float v[16];
+          decode16(bytes[i], sc[i], v);
+          blk.v[i].values(v);
+        }
         float inv;
-        const float scale = block_scale(blk, &inv);   // every lane's sources have been read
+        bool odd;
+        const float scale = blk.scale(&inv, &odd);   // every lane's sources have been read
         const int r0 = t0 & (s.page_tokens - 1);
         const int64_t tile = tile_of(s, layer, table[t0 >> s.page_log], 0, kvh);
         if (lane == 0) s.scales[tile * per + r0 / kBlock] = scale;
 #pragma unroll
         for (int i = 0; i < Blk::kPasses; ++i) {
           const int r = i * Blk::kRows + row;
-          if (t0 + r <= len + a)
+          if (t0 + r <= len + a && (t0 + r > len || scale != sc[i]))
             *reinterpret_cast<uint4*>(s.pool + tile * tile_bytes + swizzled((r0 + r) * s.head_dim + unit * 16)) =
                 encode16(blk.v[i], inv);
         }
@@ -523,52 +592,66 @@ __global__ void __launch_bounds__(128) truncate_kernel(const State s, const int3
   }
 }
 
-__device__ __forceinline__ void store16(float* p, const float* v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    reinterpret_cast<float4*>(p)[i] = float4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+// The values of sizeof(uint4) / sizeof(T) bytes, as 16 bytes.
+__device__ __forceinline__ void widened(const uint8_t* at, float scale, uint4& y, float) {
+  const unsigned x = *reinterpret_cast<const unsigned*>(at);
+  float v[16];
+  decode16(uint4{x, 0, 0, 0}, scale, v);
+  y = uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
 }
-__device__ __forceinline__ void store16(__nv_bfloat16* p, const float* v) {
-  unsigned w[8];
+__device__ __forceinline__ void widened(const uint8_t* at, float scale, uint4& y, __nv_bfloat16) {
+  const uint2 x = *reinterpret_cast<const uint2*>(at);
+  float v[16];
+  decode16(uint4{x.x, x.y, 0, 0}, scale, v);
+  unsigned w[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: 4 significant bits
-    w[i] = *reinterpret_cast<const unsigned*>(&x);
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 z = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: 4 significant bits
+    w[i] = *reinterpret_cast<const unsigned*>(&z);
   }
-  reinterpret_cast<uint4*>(p)[0] = uint4{w[0], w[1], w[2], w[3]};
-  reinterpret_cast<uint4*>(p)[1] = uint4{w[4], w[5], w[6], w[7]};
+  y = uint4{w[0], w[1], w[2], w[3]};
 }
 
-// One thread turns 16 bytes of one token's key and of its value.
+// One block of threads turns 16 tokens of one sequence and layer; the lookups
+// are done once a token.  A thread writes 16 bytes of a key and of a value at
+// a time, so that a warp's stores are whole lines: the written bytes bound it.
 template <typename T>
 __global__ void __launch_bounds__(256) read_kernel(const State s, int layer0, const int32_t* seqs,
-                                                   const int32_t* start, const int32_t* counts, T* k, T* v, int n,
-                                                   int B, int64_t units) {
-  const int U = s.head_dim / 16, row = U * s.kv_heads;
-  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (u >= units) return;
-  const int hu = (int)(u % row), h = hu / U, unit = hu % U;
-  const int64_t token = u / row;
-  const int i = (int)(token % n);
-  const int64_t lb = token / n;
-  const int b = (int)(lb % B), layer = layer0 + (int)(lb / B);
-  const int q = sequence(s, seqs, b);
-  float x[2][16] = {};
-  if (q >= 0 && i < live_count(counts, b, n)) {
-    const int64_t t = (int64_t)(start ? start[b] : 0) + i;
-    if (t >= 0 && t < (int64_t)s.held[q] << s.page_log) {
-      const int page = page_at(s, q, (int)t), r = (int)t & (s.page_tokens - 1);
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const int64_t tile = tile_of(s, layer, page, kv, h);
-        decode16(*reinterpret_cast<const uint4*>(s.pool + tile * (s.page_tokens * s.head_dim) +
-                                                 swizzled(r * s.head_dim + unit * 16)),
-                 s.scales[tile * (s.page_tokens / kBlock) + r / kBlock], x[kv]);
+                                                   const int32_t* start, const int32_t* counts, T* k, T* v, int n) {
+  __shared__ int page_s[16], row_s[16];
+  constexpr int kEach = 16 / sizeof(T);
+  const int U = s.head_dim / kEach, row = U * s.kv_heads, tid = threadIdx.x;
+  const int b = blockIdx.y, layer = layer0 + blockIdx.z, i0 = blockIdx.x * 16, here = min(16, n - i0);
+  if (tid < 16) {
+    const int q = sequence(s, seqs, b), i = i0 + tid;
+    int page = -1, r = 0;
+    if (q >= 0 && i < live_count(counts, b, n)) {
+      const int64_t t = (int64_t)(start ? start[b] : 0) + i;
+      if (t >= 0 && t < (int64_t)s.held[q] << s.page_log) {
+        page = page_at(s, q, (int)t);
+        r = (int)t & (s.page_tokens - 1);
       }
     }
+    page_s[tid] = page;
+    row_s[tid] = r;
   }
-  store16(k + u * 16, x[0]);
-  store16(v + u * 16, x[1]);
+  __syncthreads();
+  const int64_t out = (((int64_t)blockIdx.z * gridDim.y + b) * n + i0) * row;   // units of 16 bytes
+  const int per = s.page_tokens / kBlock;
+  const int64_t kv_step = s.kv_heads;   // a head's value is that many tiles behind its key
+#pragma unroll 4
+  for (int x = tid; x < here * row; x += 256) {
+    const int i = x / row, hu = x - i * row, h = hu / U, unit = hu - h * U, page = page_s[i], r = row_s[i];
+    uint4 ky{0, 0, 0, 0}, vy{0, 0, 0, 0};
+    if (page >= 0) {
+      const int64_t tile = tile_of(s, layer, page, 0, h), tile_bytes = s.page_tokens * s.head_dim;
+      const uint8_t* at = s.pool + tile * tile_bytes + swizzled(r * s.head_dim + unit * kEach);
+      widened(at, s.scales[tile * per + r / kBlock], ky, T());
+      widened(at + kv_step * tile_bytes, s.scales[(tile + kv_step) * per + r / kBlock], vy, T());
+    }
+    reinterpret_cast<uint4*>(k)[out + x] = ky;
+    reinterpret_cast<uint4*>(v)[out + x] = vy;
+  }
 }
 
 __global__ void __launch_bounds__(256) clear_kernel(const State s) {
@@ -613,8 +696,9 @@ cudaError_t append(const State& s, int layer, const int32_t* seqs, const int32_t
 
 cudaError_t commit(const State& s, const int32_t* seqs, const int32_t* accept, const int32_t* drafts,
                    const int32_t* out_tokens, int K, int L, int B, cudaStream_t st) {
-  // without drafts nothing moves: one block a sequence
-  const int tiles = s.layers * 2 * s.kv_heads, want = drafts ? (tiles + 7) / 8 : 1;
+  // without drafts nothing moves: one block of threads a sequence; else one
+  // for every 16 tiles, two a warp: a block's lookups cost more than a tile
+  const int tiles = s.layers * 2 * s.kv_heads, want = drafts ? (tiles + 15) / 16 : 1;
   const dim3 grid((unsigned)min(want, 64), (unsigned)B);
   if (s.head_dim == 128)
     commit_kernel<8><<<grid, 256, 0, st>>>(s, seqs, accept, drafts, out_tokens, K, L);
@@ -635,15 +719,13 @@ cudaError_t truncate(const State& s, const int32_t* seqs, const int32_t* lens, i
 
 cudaError_t read(const State& s, int layer, const int32_t* seqs, const int32_t* start, const int32_t* counts, void* k,
                  void* v, int n, int B, cudaStream_t st) {
-  const int64_t units = (int64_t)(layer < 0 ? s.layers : 1) * B * n * s.kv_heads * (s.head_dim / 16);
-  const unsigned grid = (unsigned)((units + 255) / 256);
+  const dim3 grid((unsigned)((n + 15) / 16), (unsigned)B, (unsigned)(layer < 0 ? s.layers : 1));
   const int l0 = layer < 0 ? 0 : layer;
   if (s.dtype == MDS_F32)
-    read_kernel<<<grid, 256, 0, st>>>(s, l0, seqs, start, counts, static_cast<float*>(k), static_cast<float*>(v), n, B,
-                                      units);
+    read_kernel<<<grid, 256, 0, st>>>(s, l0, seqs, start, counts, static_cast<float*>(k), static_cast<float*>(v), n);
   else
     read_kernel<<<grid, 256, 0, st>>>(s, l0, seqs, start, counts, static_cast<__nv_bfloat16*>(k),
-                                      static_cast<__nv_bfloat16*>(v), n, B, units);
+                                      static_cast<__nv_bfloat16*>(v), n);
   return cudaGetLastError();
 }
 
