@@ -170,8 +170,8 @@ __device__ __forceinline__ uint32_t instruction(int n, uint32_t type, uint32_t r
 }
 
 struct Row {
-  int node, own;   // node, its branch's first node
-  int64_t out;     // its output's first element, -1: not one of the call's
+  int own, depth;   // its branch's first node; nodes of the branch that it sees: its depth
+  int64_t out;      // its output's first element, -1: not one of the call's
 };
 
 // Buffers of wide values: two where they leave room for the rings.
@@ -436,7 +436,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       for (int r = wt; r < N; r += 128) {
         const int row = job.row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
         const bool live = r < p.rows_per && node < job.live;
-        rows[r] = Row{node, node > 0 && p.a.L > 0 ? 1 + (node - 1) / p.a.L * p.a.L : 1,
+        const int own = node > 0 && p.a.L > 0 ? 1 + (node - 1) / p.a.L * p.a.L : 1;
+        rows[r] = Row{own, node > 0 ? node - own + 1 : 0,
                       live ? (((int64_t)job.b * p.a.n + node) * p.a.heads + head) * D : -1};
         q_at[r] = live ? node * p.a.q_tok + head * p.a.q_head : -1;
       }
@@ -511,9 +512,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       const int wide = t & (kWide - 1);
       hold(kWideVFree + wide, ((t / kWide) & 1) ^ 1);
       const float* sc = v_scales + vs * 8 + w4 * 2;
-      unsigned rest[2];
-      const unsigned factor[2] = {value_factor(sc[0], rest[0]), value_factor(sc[1], rest[1])};
-      const bool large = (seen >> (w4 * 2) & 1u && rest[0] != 0x3f803f80u) || (seen >> (w4 * 2) & 2u && rest[1] != 0x3f803f80u);
+      // a block that was not loaded holds anything: times 0
+      unsigned rest[2], factor[2];
+      bool large = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool in = seen >> (w4 * 2 + i) & 1u;
+        factor[i] = in ? value_factor(sc[i], rest[i]) : 0u;
+        if (!in) rest[i] = 0x3f803f80u;
+        large = large || rest[i] != 0x3f803f80u;
+      }
       const char* src = base + lay.v_ring + vs * kTile * D;
       char* dst = base + lay.wide_v + wide * (128 * D * 2);
       constexpr int kChunks = D / 16;
@@ -522,17 +530,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         uint4 y[4];   // read before anything is written: nothing to order between the rows
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int pair = (i0 + i) * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+          const int octet = (i0 + i) * 4 / kChunks, chunk = ((i0 + i) * 4 + (lane >> 3)) % kChunks;
           y[i] = *reinterpret_cast<const uint4*>(src + swizzled((w4 * 32 + octet * 8 + (lane & 7)) * D + chunk * 16));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int pair = (i0 + i) * 4 + (lane >> 3), octet = pair / kChunks, chunk = pair % kChunks;
+          // the same eight slots for all lanes, so one of the warp's two blocks
+          const int octet = (i0 + i) * 4 / kChunks, chunk = ((i0 + i) * 4 + (lane >> 3)) % kChunks;
           const int k = w4 * 32 + octet * 8 + (lane & 7);
-          const bool zero = !(seen >> (k >> 4) & 1u);
-          if (zero) y[i] = uint4{0, 0, 0, 0};
+          const unsigned f = octet & 2 ? factor[1] : factor[0];
           uint4 a, b;   // of every four dimensions the order is 0, 2, 1, 3
-          const unsigned f = zero ? 0u : octet & 2 ? factor[1] : factor[0];
           to_bf16(y[i].x, f, a.x, a.y);
           to_bf16(y[i].y, f, a.z, a.w);
           to_bf16(y[i].z, f, b.x, b.y);
@@ -631,15 +638,15 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const Row row = rows[col0 + j * 8 + tq * 2 + e];
-              const int mine = len + (row.node > 0 ? row.node - row.own + 1 : 0);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                const int t = kb + k * 8 + gr, node = t - len;
-                bool see = node <= row.node && (node <= 0 || node >= row.own) && t < grp.hi;
+                const int t = kb + k * 8 + gr, up = t - len - row.own;   // nodes up its branch
+                bool see = t <= len || (unsigned)up < (unsigned)row.depth;
                 if (p.a.window > 0) {
-                  const int pos = node <= 0 ? t : len + node - row.own + 1;
-                  see = see && (pos < p.a.sinks || pos > mine - p.a.window);
+                  const int pos = t <= len ? t : len + up + 1;
+                  see = see && (pos < p.a.sinks || pos > len + row.depth - p.a.window);
                 }
+                see = see && t < grp.hi;
                 x[2 * k + e] = row.out < 0 ? 0.f : see ? x[2 * k + e] : dev::kNegInf;
               }
             }
