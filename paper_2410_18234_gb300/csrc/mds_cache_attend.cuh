@@ -37,6 +37,7 @@ constexpr unsigned kWaitTries = 1u << 18;
 struct Params {
   State s;
   Attend a;
+  int span;                // slots that one copy brings: a page, or a tile's part of it
   int g, rows, row_tiles, stages;
   int rows_per;            // rows of a row tile
 };
@@ -75,9 +76,11 @@ __device__ __forceinline__ int tile_slot(const Group& r, int i) {
   return (i < r.sink_tiles ? i : r.first + i - r.sink_tiles) * kTile;
 }
 
-// Whether any row of the tile sees a slot of the block of 16 from t on.
-__device__ __forceinline__ bool block_seen(const Group& r, int t) {
-  return t < r.hi && (t + kBlock > r.lo || t < r.sinks);
+// Whether any row of the tile sees a slot of the block of 16 from t on; or of
+// `span` slots from t on.  The pool holds finite numbers everywhere, so a copy
+// may bring slots that no row sees.
+__device__ __forceinline__ bool block_seen(const Group& r, int t, int span = kBlock) {
+  return t < r.hi && (t + span > r.lo || t < r.sinks);
 }
 
 // A wait on a barrier gives up after kWaitTries tries, and at once after

@@ -144,7 +144,8 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
   };
 
   if (warp == F::kWarps) {
-    // ---- loader: one block of 16 slots a lane (keys: lanes 0..7, values: 8..15)
+    // ---- loader: one block of 16 slots a lane (keys: lanes 0..7, values: 8..15);
+    // the first of a page's blocks copies for all of them
     const State& s = p.s;
     const int kv = (lane >> 3) & 1, blk = lane & 7;
     const int64_t layer0 = (int64_t)p.a.layer * s.pages;
@@ -158,22 +159,24 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       const int32_t* table = s.table + (int64_t)job.q * s.max_pages;
       job_done(n);
       auto page_of = [&](int i) {
-        const int t = tile_slot(grp, i) + blk * kBlock;
-        return lane < 16 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
+        const int t = (tile_slot(grp, i) + blk * kBlock) & -p.span;
+        return lane < 16 && i < end && block_seen(grp, t, p.span) ? __ldg(table + (t >> s.page_log)) : -1;
       };
       int page = page_of(off);
       for (int i = off; i < end; ++i) {
         const int next = page_of(i + 1);
         const int t = tile_slot(grp, i) + blk * kBlock;
         wait(empty + stage, phase, abort);
-        const unsigned takes = __ballot_sync(kFull, page >= 0);
-        if (lane == 0) mbar_expect_tx(full + stage, __popc(takes) * kBlock * D);
+        const bool copies = page >= 0 && (t & (p.span - 1)) == 0;   // the first block of its span
+        const unsigned takes = __ballot_sync(kFull, copies);
+        if (lane == 0) mbar_expect_tx(full + stage, __popc(takes) * p.span * D);
         __syncwarp();
         if (page >= 0) {
           const int64_t tile = ((layer0 + page) * 2 + kv) * s.kv_heads + h;
           const int r = t & (s.page_tokens - 1);
           const uint8_t* src = s.pool + (tile * s.page_tokens + r) * D;
-          bulk_copy(stage_mem + stage * F::kStageBytes + (kv * kTile + blk * kBlock) * D, src, kBlock * D, full + stage);
+          if (copies)
+            bulk_copy(stage_mem + stage * F::kStageBytes + (kv * kTile + blk * kBlock) * D, src, p.span * D, full + stage);
           const float* sc = s.scales + ((tile * s.page_tokens + r) >> 4);
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(stage_scales + stage * 16 + lane)),
                        "l"(sc)
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
 template <typename T, int D, int NT>
 cudaError_t launch_few(const State& s, const Attend& a, int sms, cudaStream_t st) {
   using F = Few<T, D, NT>;
-  Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, F::kRows};
+  Params p{s, a, s.page_tokens < kTile ? s.page_tokens : kTile, a.heads / s.kv_heads, 0, 0, 0, F::kRows};
   p.rows = a.n * p.g;
   p.row_tiles = (p.rows + F::kRows - 1) / F::kRows;
   const int grid = attend_grid(sms, F::kRows, D);

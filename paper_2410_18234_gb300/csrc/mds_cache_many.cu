@@ -289,7 +289,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
   if (warp == 3) {
     schedule(p, seqs, c, per, u0, u1, jobs, bar + kJob, bar + kJobFree, abort);
   } else if (warp == 0 || warp == 2) {
-    // ---- loaders, of keys and of values: one block of 16 slots a lane (0..7)
+    // ---- loaders, of keys and of values: one block of 16 slots a lane (0..7);
+    // the first of a page's blocks copies for all of them
     const State& s = p.s;
     const int kv = warp >> 1, blk = lane & 7, slots = kv ? lay.nv : lay.nk;
     char* ring = base + (kv ? lay.v_ring : lay.k_ring);
@@ -304,8 +305,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       const Group grp = job.grp;
       const int32_t* table = s.table + (int64_t)job.q * s.max_pages;
       auto page_of = [&](int i) {
-        const int t = tile_slot(grp, i) + blk * kBlock;
-        return lane < 8 && i < end && block_seen(grp, t) ? __ldg(table + (t >> s.page_log)) : -1;
+        const int t = (tile_slot(grp, i) + blk * kBlock) & -p.span;
+        return lane < 8 && i < end && block_seen(grp, t, p.span) ? __ldg(table + (t >> s.page_log)) : -1;
       };
       const int off = job.off;
       int page = page_of(off);
@@ -324,13 +325,14 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       for (int i = off; i < end; ++i, ++tile) {
         const int next = page_of(i + 1);
         const int r = (tile_slot(grp, i) + blk * kBlock) & (s.page_tokens - 1);
-        const unsigned takes = __ballot_sync(kFull, page >= 0);
+        const bool copies = page >= 0 && ((blk * kBlock) & (p.span - 1)) == 0;   // the first block of its span
+        const unsigned takes = __ballot_sync(kFull, copies);
         const int64_t row = (((layer0 + page) * 2 + kv) * s.kv_heads + h) * s.page_tokens + r;
         hold(empty + slot, parity);
-        if (lane == 0) mbar_expect_tx(bar + full + slot, __popc(takes) * kBlock * D);
+        if (lane == 0) mbar_expect_tx(bar + full + slot, __popc(takes) * p.span * D);
         __syncwarp();
         if (page >= 0) {
-          bulk_copy(ring + (slot * kTile + blk * kBlock) * D, s.pool + row * D, kBlock * D, bar + full + slot);
+          if (copies) bulk_copy(ring + (slot * kTile + blk * kBlock) * D, s.pool + row * D, p.span * D, bar + full + slot);
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
                            smem_u32(kv ? v_scales + slot * 8 + blk : k_scales + (tile & (kScaleRing - 1)) * 8 + blk)),
                        "l"(s.scales + (row >> 4))
@@ -940,7 +942,7 @@ cudaError_t configure_many() {
 }
 
 cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st) {
-  Params p{s, a, a.heads / s.kv_heads, 0, 0, 0, 0};
+  Params p{s, a, s.page_tokens < kTile ? s.page_tokens : kTile, a.heads / s.kv_heads, 0, 0, 0, 0};
   p.rows = a.n * p.g;
   p.row_tiles = (p.rows + kMaxN - 1) / kMaxN;
   p.rows_per = (p.rows + p.row_tiles - 1) / p.row_tiles;
