@@ -321,12 +321,16 @@ __device__ __forceinline__ void schedule(const Params& p, const Seq* seqs, Curso
 
 // ---------------------------------------------------------- joining pieces
 //
-// A piece's partial sums: per row its reference, its normaliser, and D sums.
-// A block has two: of the group that it continues, and of the one that it
-// begins and another block ends.
+// A piece's partial sums: per row its reference, its normaliser, two unused
+// places, and D sums.  A block has two: of the group that it continues, and of
+// the one that it begins and another block ends.
 
-__device__ __forceinline__ float* piece_of(const Params& p, int block, bool begins, int head_dim) {
-  return p.s.part + ((int64_t)block * 2 + (begins ? 1 : 0)) * p.rows_per * (head_dim + 2);
+template <int D>
+constexpr int kPieceRow = D + 4;
+
+template <int D>
+__device__ __forceinline__ float* piece_of(const Params& p, int block, bool begins) {
+  return p.s.part + ((int64_t)block * 2 + (begins ? 1 : 0)) * p.rows_per * kPieceRow<D>;
 }
 
 // Where row `row` of head group h of sequence b of the list goes.
@@ -337,43 +341,70 @@ __device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, in
 }
 
 // Add the pieces that blocks c0..c1 left of a row tile, in their order.  First
-// a warp a row finds its reference and normaliser (in `stat`, shared memory of
-// rows_per), then every thread adds four dimensions of a row.
-template <typename T, int D>
+// the rows' references and normalisers (into `stat`, shared memory of
+// rows_per), then the dimensions, four a thread, kItems such and kAhead pieces
+// at a time: a join is a wait for memory at the end of a block, so loads are
+// issued together (many rows have few pieces, few rows many).
+template <typename T, int D, int kItems, int kAhead>
 __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, float2* stat, int tid,
                             int threads) {
-  const int lane = tid & 31, stride = 2 * p.rows_per * (D + 2);
-  const float* first = piece_of(p, c0, true, D);
-  const float* later = piece_of(p, c0, false, D);   // + stride for each block further
-  for (int r = tid >> 5; r < p.rows_per; r += threads >> 5) {
-    float top = kNone, l = 0.f;
-    for (int cc = lane; cc <= c1 - c0; cc += 32)
-      top = fmaxf(top, __ldcg((cc ? later + (int64_t)cc * stride : first) + r * (D + 2)));
+  constexpr int R = kPieceRow<D>;
+  const int lane = tid & 31, pieces = c1 - c0 + 1;
+  const int64_t stride = 2 * (int64_t)p.rows_per * R;
+  const float* first = piece_of<D>(p, c0, true);
+  const float* later = piece_of<D>(p, c0, false);   // + stride for each block further
+  auto at = [&](int cc, int r) { return (cc ? later + cc * stride : first) + r * R; };
+  if (pieces <= 8 && p.rows_per <= threads) {   // a thread a row
+    if (tid < p.rows_per) {
+      float2 y[8];
+      float top = kNone, l = 0.f;
 #pragma unroll
-    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-    for (int cc = lane; cc <= c1 - c0; cc += 32) {
-      const float2 y = __ldcg(reinterpret_cast<const float2*>((cc ? later + (int64_t)cc * stride : first) + r * (D + 2)));
-      l += y.y * ex2(y.x - top);
+      for (int cc = 0; cc < 8; ++cc) y[cc] = cc < pieces ? __ldcg(reinterpret_cast<const float2*>(at(cc, tid))) : float2{kNone, 0.f};
+#pragma unroll
+      for (int cc = 0; cc < 8; ++cc) top = fmaxf(top, y[cc].x);
+#pragma unroll
+      for (int cc = 0; cc < 8; ++cc) l += y[cc].y * ex2(y[cc].x - top);
+      stat[tid] = float2{top, 1.f / l};
     }
+  } else {   // a warp a row, a lane a piece
+    for (int r = tid >> 5; r < p.rows_per; r += threads >> 5) {
+      float top = kNone, l = 0.f;
+      for (int cc = lane; cc < pieces; cc += 32) top = fmaxf(top, __ldcg(at(cc, r)));
 #pragma unroll
-    for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
-    if (lane == 0) stat[r] = float2{top, 1.f / l};
+      for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+      for (int cc = lane; cc < pieces; cc += 32) {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(at(cc, r)));
+        l += y.y * ex2(y.x - top);
+      }
+#pragma unroll
+      for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
+      if (lane == 0) stat[r] = float2{top, 1.f / l};
+    }
   }
   asm volatile("bar.sync 15, %0;" ::"r"(threads) : "memory");
-  for (int x = tid; x < p.rows_per * (D / 4); x += threads) {
-    const int r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
-    if (row / p.g >= live) continue;
-    const float2 st = stat[r];
-    float4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int cc = 0; cc <= c1 - c0; ++cc) {
-      const float* pr = (cc ? later + (int64_t)cc * stride : first) + r * (D + 2);
-      const float f = ex2(__ldcg(pr) - st.x);
-      const float2 a = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d));
-      const float2 e = __ldcg(reinterpret_cast<const float2*>(pr + 2 + d) + 1);
-      o.x += a.x * f, o.y += a.y * f, o.z += e.x * f, o.w += e.y * f;
+  const int items = p.rows_per * (D / 4);
+  for (int x0 = tid; x0 < items; x0 += kItems * threads) {
+    float4 o[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) o[i] = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll kAhead
+    for (int cc = 0; cc < pieces; ++cc) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int x = min(x0 + i * threads, items - 1), r = x / (D / 4), d = x % (D / 4) * 4;
+        const float* pr = at(cc, r);
+        const float f = ex2(__ldcg(pr) - stat[r].x);
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(pr + 4 + d));
+        o[i].x += y.x * f, o[i].y += y.y * f, o[i].z += y.z * f, o[i].w += y.w * f;
+      }
     }
-    store4(out_row<T>(p, b, h, row, D) + d, float4{o.x * st.y, o.y * st.y, o.z * st.y, o.w * st.y});
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int x = x0 + i * threads, r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
+      if (x >= items || row / p.g >= live) continue;
+      const float inv = stat[r].y;
+      store4(out_row<T>(p, b, h, row, D) + d, float4{o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv});
+    }
   }
 }
 

@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       }
     consumers_sync();
     const bool whole = job.whole();
-    float* part = piece_of(p, blockIdx.x, off == 0, D);
+    float* part = piece_of<D>(p, blockIdx.x, off == 0);
 #pragma unroll
     for (int m = 0; m < NT; ++m) {
       float f[2];
@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
               if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(to) = float2{o.x * inv, o.y * inv};
               else *reinterpret_cast<unsigned*>(to) = pack_bf16(o.x * inv, o.y * inv);
             } else {
-              float* pr = part + (m * 8 + r) * (D + 2);
-              __stcg(reinterpret_cast<float2*>(pr + 2 + hd * 64 + d), o);
+              float* pr = part + (m * 8 + r) * kPieceRow<D>;
+              __stcg(reinterpret_cast<float2*>(pr + 4 + hd * 64 + d), o);
               if (hd == 0 && lane == 0) __stcg(reinterpret_cast<float2*>(pr), float2{top, l});
             }
           }
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       consumers_sync();
       if (*last_s) {
         __threadfence();
-        join_pieces<T, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ml, tid, F::kThreads);
+        join_pieces<T, D, 1, 8>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, ml, tid, F::kThreads);
       }
     }
     job_done(n);

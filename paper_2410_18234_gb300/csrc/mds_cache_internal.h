@@ -66,7 +66,7 @@ cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t s
 cudaError_t configure_many();
 // Blocks of an attention kernel: one per SM, as far as the partial sums reach.
 inline int attend_grid(int sms, int rows, int head_dim) {
-  const size_t most = kPartFloats / (2 * (size_t)rows * (head_dim + 2));
+  const size_t most = kPartFloats / (2 * (size_t)rows * (head_dim + 4));
   const int grid = sms < kJoins ? sms : kJoins;
   return (size_t)grid < most ? grid : (int)most;
 }

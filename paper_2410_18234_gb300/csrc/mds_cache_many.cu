@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       }
       third_sync(third);
       const bool whole = job.whole();
-      float* piece = piece_of(p, blockIdx.x, off == 0, D);
+      float* piece = piece_of<D>(p, blockIdx.x, off == 0);
       hold(kWFree + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
       after_sync();
       if (whole) {
@@ -882,8 +882,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
             for (int e = 0; e < 8; ++e) {
               const int col = col0 + j * 8 + e;
               if (rows[col].out < 0) continue;
-              __stcg(piece + col * (D + 2) + 2 + dim, x[e]);
-              if (m == 0) __stcg(reinterpret_cast<float2*>(piece + col * (D + 2)), stat[col]);
+              __stcg(piece + col * kPieceRow<D> + 4 + dim, x[e]);
+              if (m == 0) __stcg(reinterpret_cast<float2*>(piece + col * kPieceRow<D>), stat[col]);
             }
           }
         }
@@ -903,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         weigh_sync();
         if (*last_s) {
           __threadfence();
-          join_pieces<__nv_bfloat16, D>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, stat, ht, 32 * kWeigh);
+          join_pieces<__nv_bfloat16, D, 4, 2>(p, job.b, job.h, row0, job.live, job.first_block, job.last_block, stat, ht, 32 * kWeigh);
         }
       }
       weigh_sync();   // the weights' place and stat have been read
