@@ -143,8 +143,11 @@ int mds_cache_append(mds_cache* cache, int layer, const int32_t* seqs, const int
  * q_heads is kv_heads * g, 1 <= g <= MDS_CACHE_MAX_GROUP.  Products of
  * queries with keys are exact for 16-bit queries (but for elements below 2^-28
  * of their row's maximum) and taken with 22 bits of a 32-bit query; sums and
- * softmax statistics are 32-bit; the softmax weights are rounded to the query's precision before they meet the
- * values, and the normaliser sums the rounded weights. */
+ * softmax statistics are 32-bit; the softmax weights
+ * are rounded to the query's precision before they meet the values, and the
+ * normaliser sums the rounded weights.  Weights are held relative to a
+ * reference that the largest may pass by 2^48, so sums over values beyond
+ * about 2^60 can overflow. */
 int mds_cache_attend(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                      const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
                      float scale, int B, void* stream);
