@@ -162,6 +162,8 @@ int mds_cache_append(mds_cache* c, int layer, const int32_t* seqs, const int32_t
   if (rc != MDS_OK) return rc;
   if (layer < 0 || layer >= c->cfg.layers || n < 0 || n > MDS_CACHE_MAX_TOKENS) return MDS_ESHAPE;
   if (B == 0 || n == 0) return MDS_OK;
+  // one block of threads for eight blocks of tokens and heads
+  if ((int64_t)B * ((n + 30) / MDS_CACHE_BLOCK) * c->cfg.kv_heads / 4 >= INT32_MAX) return MDS_ESHAPE;
   const int es = esize_of(c->cfg.dtype);
   if (!rows_ok(k, k_strides, es) || !rows_ok(v, v_strides, es) || (counts && !aligned(counts, 4))) return MDS_EINVAL;
   DeviceGuard g(c->device);
