@@ -40,6 +40,10 @@ struct Params {
   int span;                // slots that one copy brings: a page, or a tile's part of it
   int g, rows, row_tiles, stages;
   int rows_per;            // rows of a row tile
+  // 1, in a form that the compiler does not know: it joins a packed product
+  // and a packed sum behind it into one fused operation, rounding modes or
+  // not, but not a product and a fused operation by this number.
+  float one = 1.f;
 };
 
 // A sequence's part of the call.

@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
 #pragma unroll
           for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) w[m][z] = (sc[0][m][z] + sc[1][m][z]) * (rc[m][z & 1] * ks);
+            for (int z = 0; z < 4; ++z)   // rounded: the largest, as a reference, leaves nothing of itself
+              w[m][z] = __fmul_rn(sc[0][m][z] + sc[1][m][z], rc[m][z & 1] * ks);
           if (!plain) {
 #pragma unroll
             for (int m = 0; m < NT; ++m)

@@ -135,14 +135,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
   return *reinterpret_cast<float2*>(&r);
 }
-__device__ __forceinline__ float2 mul2(float2 a, float b) {
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   unsigned long long r;
-  const float2 c{b, b};
   asm("mul.rn.f32x2 %0, %1, %2;"
       : "=l"(r)
-      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&c)));
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
   return *reinterpret_cast<float2*>(&r);
 }
+__device__ __forceinline__ float2 mul2(float2 a, float b) { return mul2(a, float2{b, b}); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -623,15 +623,21 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
           tmem_ld_frag(x, s_at + j * 8);
           tmem_ld_frag(x + 4, s_at + j * 8 + (16u << 16));
         };
-        auto scores = [&](int j, float* x) {   // less their references
+        // Scores in log2 units, rounded before a reference is taken from them:
+        // the reference is the largest of these numbers, so that no weight
+        // beside it passes 1 however large the scores are.  A fused product
+        // would leave its rounding in the exponent: beyond 2^6 for scores of
+        // 2^30.
+        auto scores = [&](int j, float* x) {
           const float4 y4 = my_cr[4 * j];
           const float2 c0 = mul2(float2{y4.x, y4.y}, ks0), c1 = mul2(float2{y4.x, y4.y}, ks1);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float2 y = fma2(float2{x[2 * k], x[2 * k + 1]}, k < 2 ? c0 : c1, float2{y4.z, y4.w});
+            const float2 y = mul2(float2{x[2 * k], x[2 * k + 1]}, k < 2 ? c0 : c1);
             x[2 * k] = y.x;
             x[2 * k + 1] = y.y;
           }
+          return float2{y4.z, y4.w};   // the references, negated
         };
         if (kb + 32 > len || (p.a.window > 0 && kb + 32 > p.a.sinks && kb <= len + min(p.a.L, p.a.n - 1) - p.a.window)) {
           // some slot is masked for some row: -inf in its place.  Dead columns
@@ -664,7 +670,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         // Weights first with the references as they are (0 before the first);
         // only where that gives a weight too large, or none that a first
         // reference could be judged by, the columns' maxima over the tile's
-        // slots become the references, and the tile is weighed again.
+        // slots become the references, and the tile is weighed once more: two
+        // passes at most.
         float2 part[kSteps];
         bool move = false, left = false;
         for (;;) {
@@ -699,19 +706,19 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
                 m.x = fmaxf(m.x, y.x);
                 m.y = fmaxf(m.y, y.y);
               }
-              // relative to the reference, which only moves up; a column that
-              // had none (relative to 0) takes the maximum
-              float2 up{fmaxf(m.x, 0.f), fmaxf(m.y, 0.f)};
+              // a reference only moves up; a column that had none takes the maximum
+              const float4 y4 = my_cr[4 * j];
+              float2 now{fmaxf(m.x, -y4.z), fmaxf(m.y, -y4.w)};
               if (unseen >> (2 * j) & 1u) {
-                up.x = m.x > kNone ? m.x : 0.f;
+                now.x = m.x > kNone ? m.x : 0.f;
                 if (m.x > kNone) unseen &= ~(1u << (2 * j));
               }
               if (unseen >> (2 * j) & 2u) {
-                up.y = m.y > kNone ? m.y : 0.f;
+                now.y = m.y > kNone ? m.y : 0.f;
                 if (m.y > kNone) unseen &= ~(2u << (2 * j));
               }
               // a first reference below 0 finds sums of 0
-              const float2 alpha{ex2(-fmaxf(up.x, 0.f)), ex2(-fmaxf(up.y, 0.f))};
+              const float2 alpha{ex2(fminf(-y4.z - now.x, 0.f)), ex2(fminf(-y4.w - now.y, 0.f))};
               if (again) {
                 float x[8];
                 const uint32_t o_at = t_o + col0 + j * 8 + lanes;
@@ -724,8 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
                 tmem_st_frag(o_at + (16u << 16), x + 4);
               }
               if (w4 == 0 && gr == 0) {
-                const float4 y4 = my_cr[4 * j];
-                *reinterpret_cast<float2*>(next + col) = float2{y4.z - up.x, y4.w - up.y};
+                *reinterpret_cast<float2*>(next + col) = float2{-now.x, -now.y};
                 *reinterpret_cast<float2*>(next + N + col) = alpha;
               }
             }
@@ -766,11 +772,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
               for (int j = 0; j < 2; ++j)
                 {
                   float* y = now[j];
-                  scores(j0 + j, y);
+                  const float2 less = scores(j0 + j, y);
                   unsigned w[4];
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {
-                    w[k] = pack_bf16(ex2(y[2 * k]), ex2(y[2 * k + 1]));
+                    const float2 z = fma2(float2{y[2 * k], y[2 * k + 1]}, float2{p.one, p.one}, less);
+                    w[k] = pack_bf16(ex2(z.x), ex2(z.y));
                     const float2 e{__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u)};
                     part[j0 + j] = k ? add2(part[j0 + j], e) : e;
                   }
@@ -791,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
                 if (unseen >> (2 * j) & 2u) low = fminf(low, part[j].y);
               }
           }
-          if (!third_any(third, top > kMostWeight || low < kLeastWeight)) break;
+          if (move || !third_any(third, top > kMostWeight || low < kLeastWeight)) break;
           move = true;
         }
         pending = pending && left;
