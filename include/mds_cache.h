@@ -160,7 +160,8 @@ int mds_cache_attend(mds_cache* cache, int layer, const int32_t* seqs, const int
  * ([B][K][L] int32) equal out_tokens ([B][L+1] int32), the arrays that
  * mds_verify read and wrote; both NULL: branch 0.  Tokens of no branch keep
  * branch 0 (MDS_ST_BADTOKEN); tokens that were not reserved, or would be
- * moved into a shared page, are not kept (MDS_ST_BADSEQ). */
+ * moved into a page that is shared when the call begins, are not kept
+ * (MDS_ST_BADSEQ), whichever of the call's sequences share it and keep what. */
 int mds_cache_commit(mds_cache* cache, const int32_t* seqs, const int32_t* accept_len, const int32_t* draft_tokens,
                      const int32_t* out_tokens, int K, int L, int B, void* stream);
 

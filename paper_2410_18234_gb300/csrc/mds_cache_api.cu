@@ -59,6 +59,7 @@ size_t carve(const mds_cache_config& c, char* base, State& s) {
   take(s.freemap, ((size_t)c.pages + 127) / 128 * 16);
   take(s.fresh, (size_t)c.pages * 4);
   take(s.copies, (size_t)c.pages * 12);
+  take(s.kept, (size_t)MDS_CACHE_MAX_BATCH * 8);
   take(s.arrive, (size_t)c.max_seqs * 4);
   take(s.joins, mds::cache::kJoins * 4);
   take(s.free_count, 64);

@@ -30,6 +30,7 @@ struct State {
   int32_t* fresh;     // [pages] workspace of reserve: the pages it hands out
   int32_t* copies;    // [pages][3] workspace of reserve: page, its copy, tokens
   int32_t* n_copies;
+  int32_t* kept;      // [MDS_CACHE_MAX_BATCH][2] workspace of commit: tokens kept behind the root, and how far they move
   uint32_t* arrive;   // [max_seqs] arrivals of commit's blocks, 0 between calls
   uint32_t* joins;    // [kJoins] arrivals of attend's pieces, 0 between calls
   float* part;        // attend's partial sums

@@ -455,47 +455,71 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) append_kernel(con
 
 // ------------------------------------------------------------------- commit
 
+// What a call keeps of sequence q (all the block's threads): the tokens behind
+// the root, -1 for nothing, and how many slots they move towards the front.
+__device__ int2 judge(const State& s, int q, int b, const int32_t* accept, const int32_t* drafts,
+                      const int32_t* out_tokens, int K, int L) {
+  __shared__ int branch_s;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int a = min(max(accept[b], -1), L);
+  int k = 0;
+  if (drafts && a > 0) {
+    if (tid == 0) branch_s = K;
+    __syncthreads();
+    const int32_t* out = out_tokens + (int64_t)b * (L + 1);
+    for (int i = tid >> 5; i < K; i += blockDim.x >> 5) {
+      const int32_t* d = drafts + ((int64_t)b * K + i) * L;
+      bool same = true;
+      for (int x = lane; x < a; x += 32) same = same && d[x] == out[x];
+      if (__all_sync(kFull, same) && lane == 0) atomicMin(&branch_s, i);
+    }
+    __syncthreads();
+    k = branch_s;
+    if (k >= K) {
+      if (tid == 0) atomicOr(s.status, MDS_ST_BADTOKEN);
+      k = 0;
+    }
+  }
+  const int len = s.lens[q];
+  const int64_t shift = a > 0 ? (int64_t)k * L : 0;
+  bool bad = len + 1 + (int64_t)a + shift > (int64_t)s.held[q] << s.page_log;
+  if (!bad && shift) {
+    const int32_t* table = s.table + (int64_t)q * s.max_pages;
+    for (int p = (len + 1) >> s.page_log; p <= (len + a) >> s.page_log; ++p) bad = bad || s.ref[table[p]] > 1;
+  }
+  if (bad && tid == 0) atomicOr(s.status, MDS_ST_BADSEQ);
+  return bad ? int2{-1, 0} : int2{a, (int)shift};
+}
+
+// A kernel of its own where tokens may move: whether a page is shared is
+// judged before any of the call's sequences gives one back.
+__global__ void __launch_bounds__(256) judge_kernel(const State s, const int32_t* seqs, const int32_t* accept,
+                                                    const int32_t* drafts, const int32_t* out_tokens, int K, int L) {
+  const int b = blockIdx.x, q = sequence(s, seqs, b);
+  if (q < 0) return;
+  const int2 keeps = judge(s, q, b, accept, drafts, out_tokens, K, L);
+  if (threadIdx.x == 0) reinterpret_cast<int2*>(s.kept)[b] = keeps;
+}
+
 // One block row per sequence.  Tokens move towards the front (branch k's
 // token i from slot len + 1 + k L + i to len + 1 + i), so a block of slots may
 // be rewritten once its own sources have been read: those of the blocks
 // behind it lie behind it.  One warp moves one tile's blocks in that order.
 // The last of a sequence's blocks of threads to finish shortens the sequence.
+// Without drafts (`judged` false) nothing moves and one block judges for itself.
 template <int U>
 __global__ void __launch_bounds__(256, 3) commit_kernel(const State s, const int32_t* seqs, const int32_t* accept,
-                                                     const int32_t* drafts, const int32_t* out_tokens, int K, int L) {
-  __shared__ int branch_s, last_s;
+                                                     bool judged, int L) {
+  __shared__ int last_s;
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int q = sequence(s, seqs, b);
-  if (q < 0) return;
+  const int q = seqs[b];
+  if (judged ? q < 0 || q >= s.max_seqs : sequence(s, seqs, b) < 0) return;
   const int len = s.lens[q], held = s.held[q];
-  int a = min(max(accept[b], -1), L);
-  if (tid == 0) branch_s = drafts && a > 0 ? K : 0;
-  __syncthreads();
-  if (drafts && a > 0) {
-    const int32_t* out = out_tokens + (int64_t)b * (L + 1);
-    for (int k = warp; k < K; k += 8) {
-      const int32_t* d = drafts + ((int64_t)b * K + k) * L;
-      bool same = true;
-      for (int i = lane; i < a; i += 32) same = same && d[i] == out[i];
-      if (__all_sync(kFull, same) && lane == 0) atomicMin(&branch_s, k);
-    }
-    __syncthreads();
-  }
-  int k = branch_s;
-  if (k >= K) {
-    if (tid == 0) atomicOr(s.status, MDS_ST_BADTOKEN);
-    k = 0;
-  }
+  const int2 keeps = judged ? reinterpret_cast<const int2*>(s.kept)[b]
+                            : judge(s, q, b, accept, nullptr, nullptr, 1, L);
+  const int a = keeps.x, shift = keeps.y;
   const int32_t* table = s.table + (int64_t)q * s.max_pages;
-  const int64_t shift = a > 0 ? (int64_t)k * L : 0;
-  bool bad = len + 1 + (int64_t)a + shift > (int64_t)held << s.page_log;
-  if (!bad && shift)
-    for (int p = (len + 1) >> s.page_log; p <= (len + a) >> s.page_log; ++p) bad = bad || s.ref[table[p]] > 1;
-  if (bad) {
-    if (tid == 0) atomicOr(s.status, MDS_ST_BADSEQ);
-    a = -1;
-  }
-  if (!bad && shift) {
+  if (shift) {
     using Blk = Block<__nv_bfloat16, U>;
     const int tiles = s.layers * 2 * s.kv_heads;
     const int row = lane / U, unit = lane % U;
@@ -512,7 +536,7 @@ __global__ void __launch_bounds__(256, 3) commit_kernel(const State s, const int
           bytes[i] = uint4{0, 0, 0, 0};
           sc[i] = 0.f;
           if (t <= len + a) {
-            const int from = t <= len ? t : t + (int)shift, fr = from & (s.page_tokens - 1);
+            const int from = t <= len ? t : t + shift, fr = from & (s.page_tokens - 1);
             const int64_t tile = tile_of(s, layer, table[from >> s.page_log], 0, kvh);
             sc[i] = s.scales[tile * per + fr / kBlock];
             bytes[i] = *reinterpret_cast<const uint4*>(s.pool + tile * tile_bytes + swizzled(fr * s.head_dim + unit * 16));
@@ -700,10 +724,11 @@ cudaError_t commit(const State& s, const int32_t* seqs, const int32_t* accept, c
   // for every 16 tiles, two a warp: a block's lookups cost more than a tile
   const int tiles = s.layers * 2 * s.kv_heads, want = drafts ? (tiles + 15) / 16 : 1;
   const dim3 grid((unsigned)min(want, 64), (unsigned)B);
+  if (drafts) judge_kernel<<<B, 256, 0, st>>>(s, seqs, accept, drafts, out_tokens, K, L);
   if (s.head_dim == 128)
-    commit_kernel<8><<<grid, 256, 0, st>>>(s, seqs, accept, drafts, out_tokens, K, L);
+    commit_kernel<8><<<grid, 256, 0, st>>>(s, seqs, accept, drafts != nullptr, L);
   else
-    commit_kernel<4><<<grid, 256, 0, st>>>(s, seqs, accept, drafts, out_tokens, K, L);
+    commit_kernel<4><<<grid, 256, 0, st>>>(s, seqs, accept, drafts != nullptr, L);
   return cudaGetLastError();
 }
 
