@@ -74,8 +74,8 @@ extern "C" {
  * infinite), MDS_ST_BADTOKEN (emitted tokens of no branch) and
  * MDS_ST_TIMEOUT. */
 #define MDS_ST_NOPAGES 128u /* too few free pages, or a page table too short: the
-                               sequence was given none, and its tokens behind
-                               what it holds are not stored                    */
+                               sequence was given none, and tokens that were
+                               not reserved before are not stored              */
 #define MDS_ST_BADSEQ 256u  /* a sequence id of max_seqs or more; a fork onto a
                                sequence that holds pages; tokens appended,
                                attended to or committed that were not reserved */
@@ -121,11 +121,17 @@ int mds_cache_state(const mds_cache* cache, const int32_t** lens, const int32_t*
  * from the page that holds slot len on (their tokens in front of slot
  * len + counts[b] are copied).  A sequence that the free pages do not reach,
  * counting those before it in the list, or whose page table is too short,
- * gets none (MDS_ST_NOPAGES). */
+ * gets none (MDS_ST_NOPAGES).
+ * Only reserved slots are stored to, attended to and committed.  They stay
+ * reserved until commit, truncate or free gives back their page (truncate and
+ * free: any slot behind the length).  A fork has what its source has reserved.
+ * Where pages are shared, a call that copies any ends what is reserved at
+ * len + counts[b], and one that gives none ends it in front of the first. */
 int mds_cache_reserve(mds_cache* cache, const int32_t* seqs, const int32_t* counts, int n, int B, void* stream);
 
 /* Store keys and values of layer `layer` in the slots len .. len + counts[b]
- * of each sequence (reserved before).  k and v are dtype: the element of
+ * of each sequence, as far as they are reserved (MDS_ST_BADSEQ where not, or
+ * where their page is shared).  k and v are dtype: the element of
  * sequence b of the list, token i, head h and dimension d is at
  * b * strides[0] + i * strides[1] + h * strides[2] + d, strides in elements,
  * multiples of 16 bytes, the bases aligned to 16 bytes (MDS_EINVAL

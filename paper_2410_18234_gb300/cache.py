@@ -198,7 +198,7 @@ class Cache:
 
     def append(self, layer, seqs, k, v, counts=None, stream=None):
         """Store keys and values [B][n][kv_heads][head_dim] (strided views with
-        16-byte rows) in the slots behind the committed tokens."""
+        16-byte rows) in the reserved slots behind the committed tokens."""
         ids, B = self._seqs(seqs)
         ks, vs = self._rows("k", k, B, self.kv_heads), self._rows("v", v, B, self.kv_heads)
         if k.shape != v.shape:

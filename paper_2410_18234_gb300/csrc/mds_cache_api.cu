@@ -55,6 +55,7 @@ size_t carve(const mds_cache_config& c, char* base, State& s) {
   take(s.table, (size_t)c.max_seqs * c.max_pages * 4);
   take(s.lens, (size_t)c.max_seqs * 4);
   take(s.held, (size_t)c.max_seqs * 4);
+  take(s.reach, (size_t)c.max_seqs * 4);
   take(s.ref, (size_t)c.pages * 4);
   take(s.freemap, ((size_t)c.pages + 127) / 128 * 16);
   take(s.fresh, (size_t)c.pages * 4);

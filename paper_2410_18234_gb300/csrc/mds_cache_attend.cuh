@@ -48,7 +48,7 @@ struct Params {
 
 // A sequence's part of the call.
 struct Seq {
-  int q, len, live, end;   // id, committed, live nodes, slots held (a slot behind it is not read)
+  int q, len, live, end;   // id, committed, live nodes, slots reserved (a slot behind them is not read)
 };
 
 // A group's key tiles: `sink` tiles from slot 0, then those from `first` on.
@@ -235,7 +235,7 @@ __device__ void plan(const Params& p, long long* prefix, Seq* seqs, int head_dim
       q.q = id;
       q.len = p.s.lens[id];
       q.live = p.a.counts ? min(max(p.a.counts[b], 0), p.a.n) : p.a.n;
-      q.end = p.s.held[id] << p.s.page_log;
+      q.end = p.s.reach[id];
       if (q.len + q.live > q.end && q.live > 0) {
         atomicOr(p.s.status, MDS_ST_BADSEQ);
         q.live = min(q.live, max(q.end - q.len, 0));   // rows without a slot of their own are zeros

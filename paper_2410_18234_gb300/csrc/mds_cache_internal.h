@@ -24,6 +24,7 @@ struct State {
   int32_t* table;     // [max_seqs][max_pages], -1 behind the held pages
   int32_t* lens;      // [max_seqs] committed tokens
   int32_t* held;      // [max_seqs] pages held
+  int32_t* reach;     // [max_seqs] slots reserved: lens <= reach <= held * page_tokens
   int32_t* ref;       // [pages] sequences that hold the page
   uint32_t* freemap;  // [ceil(pages / 128) * 4] bit set: the page is free
   int32_t* free_count;

@@ -28,7 +28,8 @@ __device__ __forceinline__ int64_t tile_of(const State& s, int layer, int page, 
   return (((int64_t)layer * s.pages + page) * 2 + kv) * s.kv_heads + h;
 }
 
-// Where slot t's rows are: page id, or -1 where the sequence holds none.
+// Where slot t's rows are: page id, or -1 where the sequence holds none.  (read:
+// the other calls go by what is reserved.)
 __device__ __forceinline__ int page_at(const State& s, int q, int t) {
   const int p = t >> s.page_log;
   return p < s.held[q] ? s.table[(int64_t)q * s.max_pages + p] : -1;
@@ -76,6 +77,15 @@ __device__ int2 block_scan(int2 x, int2* warp_sums) {
   return x;
 }
 
+// A reserve that gave sequence q nothing: of the slots reserved before, those
+// in shared pages, where the sequence cannot store, are not reserved any more.
+__device__ void got_none(const State& s, int q, int len, int held) {
+  const int32_t* row = s.table + (int64_t)q * s.max_pages;
+  int p = len >> s.page_log;
+  while (p < held && s.ref[row[p]] <= 1) ++p;
+  s.reach[q] = min(s.reach[q], max(len, p << s.page_log));
+}
+
 // One block plans the whole call: which page indices of which sequence need a
 // page (absent, or shared and about to be written behind), and which page
 // each gets.  The order is that of the list and of the indices, and pages are
@@ -99,10 +109,12 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const State 
       if (k > 0 && end > s.max_pages) {
         atomicOr(s.status, MDS_ST_NOPAGES);
         c.x = -1;
+        got_none(s, q, len, held);
       } else if (k > 0) {
         const int32_t* row = s.table + (int64_t)q * s.max_pages;
         for (int p = first; p < min(end, held); ++p) c.y += s.ref[row[p]] > 1;
         c.x = c.y + max(end - max(first, held), 0);
+        if (c.x == 0) s.reach[q] = max(s.reach[q], len + k);
       }
     }
     need[b] = c;
@@ -119,7 +131,10 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const State 
     const int off = before.x + inc.x - mine, coff = before.y + inc.y - own.y;
     if (b < B) {
       const bool fits = own.x > 0 && off + mine <= avail;
-      if (own.x > 0 && !fits) atomicOr(s.status, MDS_ST_NOPAGES);
+      if (own.x > 0 && !fits) {
+        atomicOr(s.status, MDS_ST_NOPAGES);
+        got_none(s, seqs[b], s.lens[seqs[b]], s.held[seqs[b]]);
+      }
       need[b] = int2{own.x == 0 ? 0 : fits ? off : -1, coff};
       if (own.x == 0) need[b].x = -2;   // nothing to hand out
       if (fits) {
@@ -176,6 +191,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const State 
       c[1] = fresh;
       c[2] = min(P, len + k - p * P);
     }
+    // behind a copy's tokens nothing is this sequence's own
+    s.reach[q] = off.y > need[b].y ? len + k : max(s.reach[q], len + k);
     need[b].x = off.x;
   }
   __syncthreads();
@@ -404,8 +421,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) append_kernel(con
   const int b = (int)(bj / nb), j = (int)(bj % nb);
   const int q = sequence(s, seqs, b);
   if (q < 0) return;
-  const int len = s.lens[q], c = live_count(counts, b, n);
+  const int len = s.lens[q], reach = s.reach[q], asked = live_count(counts, b, n), c = min(asked, reach - len);
   const int t0 = (len / kBlock + j) * kBlock;
+  if (asked == 0 || t0 >= len + asked) return;
+  if (c < asked && lane == 0) atomicOr(s.status, MDS_ST_BADSEQ);
   if (c == 0 || t0 >= len + c) return;
   using Blk = Block<T, U>;
   Blk blk;
@@ -418,8 +437,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) append_kernel(con
     if (t >= len && t < len + c) blk.v[i].load(src + (int64_t)(t - len) * st.y);
     else blk.v[i].zero();
   }
-  const int page = page_at(s, q, t0);
-  if (page < 0 || s.ref[page] > 1) {
+  const int page = s.table[(int64_t)q * s.max_pages + (t0 >> s.page_log)];
+  if (s.ref[page] > 1) {
     if (lane == 0) atomicOr(s.status, MDS_ST_BADSEQ);
     return;
   }
@@ -482,7 +501,7 @@ __device__ int2 judge(const State& s, int q, int b, const int32_t* accept, const
   }
   const int len = s.lens[q];
   const int64_t shift = a > 0 ? (int64_t)k * L : 0;
-  bool bad = len + 1 + (int64_t)a + shift > (int64_t)s.held[q] << s.page_log;
+  bool bad = len + 1 + (int64_t)a + shift > s.reach[q];
   if (!bad && shift) {
     const int32_t* table = s.table + (int64_t)q * s.max_pages;
     for (int p = (len + 1) >> s.page_log; p <= (len + a) >> s.page_log; ++p) bad = bad || s.ref[table[p]] > 1;
@@ -578,6 +597,7 @@ __global__ void __launch_bounds__(256, 3) commit_kernel(const State s, const int
     s.arrive[q] = 0;
     s.lens[q] = now;
     s.held[q] = min(keep, held);
+    s.reach[q] = min(s.reach[q], keep << s.page_log);
   }
 }
 
@@ -600,6 +620,7 @@ __global__ void __launch_bounds__(128) fork_kernel(const State s, const int32_t*
   if (threadIdx.x == 0) {
     s.lens[to] = s.lens[from];
     s.held[to] = held;
+    s.reach[to] = s.reach[from];
   }
 }
 
@@ -613,6 +634,7 @@ __global__ void __launch_bounds__(128) truncate_kernel(const State s, const int3
   if (threadIdx.x == 0) {
     s.lens[q] = now;
     s.held[q] = min(keep, held);
+    s.reach[q] = now;
   }
 }
 
