@@ -142,7 +142,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
   return *reinterpret_cast<float2*>(&r);
 }
-__device__ __forceinline__ float2 mul2(float2 a, float b) { return mul2(a, float2{b, b}); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -474,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
 #pragma unroll
         for (int d = 1; d < kUnits; d *= 2) bits = max(bits, __shfl_xor_sync(kFull, bits, d));
         const int e = bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23) - 127 - 14, -112);
-        // the coefficient is positive, so that a masked -inf stays one: the
+        // the coefficient is not negative, so that a masked -inf stays one: the
         // scale's sign, or 0, goes to the queries
         const float inv = p.a.scale == 0.f ? 0.f : copysignf(__uint_as_float((unsigned)(127 - e) << 23), p.a.scale);
         unsigned v[4];
@@ -487,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         if (unit == 0) {
           float* at_cr = reinterpret_cast<float*>(cr + (r >> 1)) + (r & 1);
           const float k = fabsf(p.a.scale) * dev::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
-          at_cr[0] = p.a.scale == 0.f ? 1.f : fmaxf(k, 0x1p-100f);
+          at_cr[0] = p.a.scale == 0.f ? 1.f : k;
           at_cr[2] = 0.f;
         }
       }
@@ -598,15 +597,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       float4* my_cr = cr + col0 / 2 + tq;   // step j's are 4 j further
       unsigned unseen = (1u << (2 * kSteps)) - 1u;   // this thread's columns that have no reference yet
       bool pending = true;                          // some column of the third has none
-      float least = 1.f;
 #pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        sum[j] = float2{0.f, 0.f};
-        least = fminf(least, fminf(my_cr[4 * j].x, my_cr[4 * j].y));
-      }
-      // a block's scale is taken as no less than this, so that its product
-      // with a coefficient is not 0 (scores that small are 0 by far)
-      const float scale_floor = 0x1p-120f / least;
+      for (int j = 0; j < kSteps; ++j) sum[j] = float2{0.f, 0.f};
       const Group grp = job.grp;
       const int off = job.off, end = off + job.cnt, len = job.len;
       for (int i = off; i < end; ++i, ++tile) {
@@ -616,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         after_sync();
         const float* sc = k_scales + (tile & (kScaleRing - 1)) * 8 + w4 * 2;
         const bool seen0 = block_seen(grp, kb), seen1 = block_seen(grp, kb + kBlock);
-        const float ks0 = seen0 ? fmaxf(sc[0], scale_floor) : 1.f, ks1 = seen1 ? fmaxf(sc[1], scale_floor) : 1.f;
+        const float ks0 = seen0 ? sc[0] : 1.f, ks1 = seen1 ? sc[1] : 1.f;
         const uint32_t s_at = t_s + b * N + col0 + lanes;
         // 8 columns: x[2 k], x[2 k + 1] of slot kb + 8 k + gr
         auto load = [&](int j, float* x) {
@@ -630,7 +622,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         // 2^30.
         auto scores = [&](int j, float* x) {
           const float4 y4 = my_cr[4 * j];
-          const float2 c0 = mul2(float2{y4.x, y4.y}, ks0), c1 = mul2(float2{y4.x, y4.y}, ks1);
+          // never 0, so that a masked -inf stays one; what 2^-120 adds to a score is below 2^-88
+          const float2 tiny{0x1p-120f, 0x1p-120f}, c0 = fma2(float2{y4.x, y4.y}, float2{ks0, ks0}, tiny),
+                       c1 = fma2(float2{y4.x, y4.y}, float2{ks1, ks1}, tiny);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float2 y = mul2(float2{x[2 * k], x[2 * k + 1]}, k < 2 ? c0 : c1);

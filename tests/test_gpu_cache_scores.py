@@ -93,3 +93,24 @@ def test_negative_scale(K, L, group, dtype):
         k, v = m.get(0, 0, 0, 333 + n)
         want, mag, big = attend(-wide(q[0]), k, v, visible(n, K, 333, window), 0.25)
         assert (np.abs(wide(a[0]) - want) <= bound(mag, big, want, 333 + n, 64, dtype)).all()
+
+
+@pytest.mark.parametrize("K,L,group", ROWS)
+def test_a_row_of_tiny_queries_changes_no_other(K, L, group):
+    """Keys of 2^-14 and queries of 2^18, with and without a node whose
+    queries are 2^-90: the other nodes' outputs are right either way."""
+    rng = np.random.default_rng(22)
+    D, n, T = 128, 1 + K * L, 200
+    c, m = both(kv_heads=1, head_dim=D, max_pages=20, page_tokens=16)
+    prompt(c, m, rng.standard_normal((T, D)) * 2.0 ** -14, rng.standard_normal((T, D)))
+    grow(c, m, rng, [0], [n], keep=False)
+    q = torch.tensor(rng.standard_normal((1, n, group, D)) * 2.0 ** 18, device=DEV).bfloat16()
+    first = c.attend(0, ints([0]), q, branches=K, window=100)
+    k, v = m.get(0, 0, 0, T + n)
+    want, mag, big = attend(wide(q[0]), k, v, visible(n, K, T, 100), D ** -0.5)
+    assert (np.abs(wide(first[0]) - want) <= bound(mag, big, want, T + n, D, "bf16")).all()
+    q[0, n // 2] *= 2.0 ** -108
+    again = c.attend(0, ints([0]), q, branches=K, window=100)
+    want, mag, big = attend(wide(q[0]), k, v, visible(n, K, T, 100), D ** -0.5)
+    assert (np.abs(wide(again[0]) - want) <= bound(mag, big, want, T + n, D, "bf16")).all()
+    assert c.status() == (0, "ok")
