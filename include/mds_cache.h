@@ -152,8 +152,9 @@ int mds_cache_append(mds_cache* cache, int layer, const int32_t* seqs, const int
  * softmax statistics are 32-bit; the softmax weights
  * are rounded to the query's precision before they meet the values, and the
  * normaliser sums the rounded weights.  Weights are held relative to a
- * reference that the largest may pass by 2^48, so sums over values beyond
- * about 2^60 can overflow. */
+ * reference that the largest may pass by 2^48 or miss by 2^20, so sums over
+ * values beyond about 2^60 can overflow and values below about 2^-100 lose
+ * bits.  Scores beyond 2^127 overflow. */
 int mds_cache_attend(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                      const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
                      float scale, int B, void* stream);

@@ -42,8 +42,10 @@ constexpr int kMaxN = 144;      // columns: three buffers of them and 64 of keys
 constexpr int kRingMax = 5;
 constexpr int kScaleRing = 8;   // tiles whose scales are held: kRingMax + 3
 // Weights are 2^(score - reference), and sums of floats lose nothing by a
-// reference that is not the maximum: it only has to keep them in range.
-constexpr float kMostWeight = 0x1p48f, kLeastWeight = 0x1p-60f;
+// reference that is not the maximum: it only has to keep them in range, 2^48
+// from the top and, so that a weight times a small value stays a normal
+// number, not far below 1 where a first reference (0) is judged.
+constexpr float kMostWeight = 0x1p48f, kLeastWeight = 0x1p-20f;
 
 enum Bar {
   kKFull = 0, kKEmpty = kKFull + kRingMax, kVFull = kKEmpty + kRingMax, kVEmpty = kVFull + kRingMax,

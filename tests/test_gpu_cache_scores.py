@@ -114,3 +114,30 @@ def test_a_row_of_tiny_queries_changes_no_other(K, L, group):
     want, mag, big = attend(wide(q[0]), k, v, visible(n, K, T, 100), D ** -0.5)
     assert (np.abs(wide(again[0]) - want) <= bound(mag, big, want, T + n, D, "bf16")).all()
     assert c.status() == (0, "ok")
+
+
+@pytest.mark.parametrize("score", [-12, -27, -38])
+@pytest.mark.parametrize("K,L,group", ROWS)
+def test_small_values_under_low_scores(K, L, group, score):
+    """Scores of about `score` (e^-38 is 2^-55) for every token, values of
+    2^-98: the weights' size must not push them out of 32 bits."""
+    rng = np.random.default_rng(23)
+    D, n, T = 64, 1 + K * L, 300
+    c, m = both(kv_heads=1, head_dim=D, max_pages=30, page_tokens=16)
+    k = 0.1 * rng.standard_normal((T + n, D))
+    k[:, 0] = score
+    v = rng.standard_normal((T + n, D)) * 2.0 ** -98
+    prompt(c, m, k[:T], v[:T])
+    kk, vv = (torch.tensor(x[None, T:, None], device=DEV).bfloat16() for x in (k, v))
+    m.reserve([0], [n])
+    c.reserve(ints([0]), n)
+    m.append(0, [0], [n], wide(kk), wide(vv))
+    c.append(0, ints([0]), kk, vv)
+    q = torch.tensor(0.1 * rng.standard_normal((1, n, group, D)), device=DEV)
+    q[..., 0] = 1.0
+    q = q.bfloat16()
+    o = c.attend(0, ints([0]), q, branches=K, scale=1.0)
+    kk, vv = m.get(0, 0, 0, T + n)
+    want, mag, big = attend(wide(q[0]), kk, vv, visible(n, K, T), 1.0)
+    assert (np.abs(wide(o[0]) - want) <= bound(mag, big, want, T + n, D, "bf16") - 1e-30).all()
+    assert c.status() == (0, "ok")
