@@ -13,6 +13,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cfloat>
+
 #include "mds_cache_internal.h"
 #include "mds_device.cuh"
 
@@ -30,7 +32,7 @@ using dev::smem_u32;
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kTile = 128;                 // slots of a key tile
-constexpr float kNone = -1e30f;            // reference of a row that has seen nothing
+constexpr float kNone = -FLT_MAX;          // reference of a row that has seen nothing: below every score
 constexpr float kSlack = 32.f;             // the reference moves when a weight passes 2^32
 constexpr unsigned kWaitTries = 1u << 18;
 

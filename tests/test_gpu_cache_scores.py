@@ -141,3 +141,28 @@ def test_small_values_under_low_scores(K, L, group, score):
     want, mag, big = attend(wide(q[0]), kk, vv, visible(n, K, T), 1.0)
     assert (np.abs(wide(o[0]) - want) <= bound(mag, big, want, T + n, D, "bf16") - 1e-30).all()
     assert c.status() == (0, "ok")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [50, 300])
+@pytest.mark.parametrize("K,L,group", ROWS)
+def test_scores_far_below_zero(K, L, group, T, dtype):
+    """Every score of a row is below -2^100: the largest of them picks its token."""
+    rng = np.random.default_rng(24)
+    D, n = 64, 1 + K * L
+    c, m = both(kv_heads=1, head_dim=D, max_pages=30, page_tokens=16, dtype=dtype)
+    u = rng.choice([-1.0, 1.0], D)
+    k = -u * 2.0 ** 50 * rng.choice([2.0, 3.0, 4.0], (T + n, 1))
+    k[T // 2] = -u * 2.0 ** 50
+    v = rng.standard_normal((T + n, D))
+    prompt(c, m, k[:T], v[:T])
+    kk, vv = (torch.tensor(x[None, T:, None], device=DEV).to(DT[dtype]) for x in (k, v))
+    m.reserve([0], [n])
+    c.reserve(ints([0]), n)
+    m.append(0, [0], [n], wide(kk), wide(vv))
+    c.append(0, ints([0]), kk, vv)
+    q = torch.tensor(u * np.exp2(rng.integers(50, 54, (1, n, group, 1))), device=DEV).to(DT[dtype])
+    o = c.attend(0, ints([0]), q, branches=K)
+    want = m.get(0, 0, T // 2, 1)[1][0]
+    np.testing.assert_array_equal(wide(o[0]), np.broadcast_to(want, (n, group, D)))
+    assert c.status() == (0, "ok")
