@@ -72,9 +72,18 @@ _lib = _bind(mds._lib)
 _I64x3 = ctypes.c_int64 * 3
 
 
+def _sizes(*given):
+    """`given` as integers that the C interface's 32 bits hold: ctypes would cut larger ones."""
+    out = [int(x) for x in given]
+    for x in out:
+        if not -1 << 31 <= x < 1 << 31:
+            raise MdsError(MDS_ESHAPE, f"a size of {x}")
+    return out
+
+
 def _config(layers, pages, kv_heads, head_dim, max_seqs, max_pages, page_tokens, dtype):
-    return CacheConfig(int(layers), int(pages), int(page_tokens), int(kv_heads), int(head_dim), int(max_seqs),
-                       int(max_pages), mds.DTYPES[dtype] if isinstance(dtype, str) else int(dtype))
+    return CacheConfig(*_sizes(layers, pages, page_tokens, kv_heads, head_dim, max_seqs, max_pages,
+                               mds.DTYPES[dtype] if isinstance(dtype, str) else dtype))
 
 
 def cache_bytes(layers, pages, kv_heads, head_dim, max_seqs, max_pages, page_tokens=64, dtype="bf16"):
@@ -161,7 +170,8 @@ class Cache:
         if t.dtype is not self.dtype or t.get_device() != self._index:
             raise MdsError(MDS_EINVAL, f"{name}: {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
         s = t.shape
-        if len(s) != 4 or s[0] != B or s[3] != self.head_dim or (heads is not None and s[2] != heads):
+        if len(s) != 4 or s[0] != B or s[3] != self.head_dim or (heads is not None and s[2] != heads) or \
+                max(s) >= 1 << 31:
             raise MdsError(MDS_ESHAPE, f"{name} has shape {tuple(s)}, expected ({B}, n, "
                                        f"{'q_heads' if heads is None else heads}, {self.head_dim})")
         st = t.stride()
@@ -192,7 +202,8 @@ class Cache:
     def reserve(self, seqs, n, counts=None, stream=None):
         """Room for counts (n) tokens behind the committed ones of every sequence."""
         ids, B = self._seqs(seqs)
-        rc = _lib.mds_cache_reserve(self.ctx, ids, self._ints("counts", counts, (B,)), int(n), B, self._stream(stream))
+        n, = _sizes(n)
+        rc = _lib.mds_cache_reserve(self.ctx, ids, self._ints("counts", counts, (B,)), n, B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_reserve")
 
@@ -203,7 +214,8 @@ class Cache:
         ks, vs = self._rows("k", k, B, self.kv_heads), self._rows("v", v, B, self.kv_heads)
         if k.shape != v.shape:
             raise MdsError(MDS_ESHAPE, f"k has shape {tuple(k.shape)}, v {tuple(v.shape)}")
-        rc = _lib.mds_cache_append(self.ctx, int(layer), ids, self._ints("counts", counts, (B,)), k.data_ptr(), ks,
+        layer, = _sizes(layer)
+        rc = _lib.mds_cache_append(self.ctx, layer, ids, self._ints("counts", counts, (B,)), k.data_ptr(), ks,
                                    v.data_ptr(), vs, k.shape[1], B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_append")
@@ -215,9 +227,10 @@ class Cache:
         the window off; ``scale`` defaults to head_dim ** -0.5."""
         ids, B = self._seqs(seqs)
         qs = self._rows("q", q, B)
+        layer, branches, window, sinks = _sizes(layer, branches, window, sinks)
         o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
-        rc = _lib.mds_cache_attend(self.ctx, int(layer), ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
-                                   o.data_ptr(), q.shape[2], q.shape[1], int(branches), int(window), int(sinks),
+        rc = _lib.mds_cache_attend(self.ctx, layer, ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
+                                   o.data_ptr(), q.shape[2], q.shape[1], branches, window, sinks,
                                    self.head_dim ** -0.5 if scale is None else float(scale), B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_attend")
@@ -228,7 +241,7 @@ class Cache:
         lowest branch whose draft_tokens [B][branches][length] are out_tokens
         [B][length + 1] (both None: branch 0); give the pages behind back."""
         ids, B = self._seqs(seqs)
-        K, L = int(branches), int(length)
+        K, L = _sizes(branches, length)
         rc = _lib.mds_cache_commit(self.ctx, ids, self._ints("accept_len", accept_len, (B,)),
                                    self._ints("draft_tokens", draft_tokens, (B, K, L)),
                                    self._ints("out_tokens", out_tokens, (B, L + 1)), K, L, B, self._stream(stream))
@@ -261,12 +274,13 @@ class Cache:
         [B][n][kv_heads][head_dim], with a leading [layers] for layer None;
         zeros beyond counts and beyond what a sequence holds."""
         ids, B = self._seqs(seqs)
-        shape = (B, int(n), self.kv_heads, self.head_dim)
+        n, at = _sizes(n, -1 if layer is None else layer)
+        shape = (B, n, self.kv_heads, self.head_dim)
         if layer is None:
             shape = (self.layers, *shape)
         k, v = self._outs(shape, stream, out, 2)
-        rc = _lib.mds_cache_read(self.ctx, -1 if layer is None else int(layer), ids, self._ints("start", start, (B,)),
-                                 self._ints("counts", counts, (B,)), k.data_ptr(), v.data_ptr(), int(n), B,
+        rc = _lib.mds_cache_read(self.ctx, at, ids, self._ints("start", start, (B,)),
+                                 self._ints("counts", counts, (B,)), k.data_ptr(), v.data_ptr(), n, B,
                                  self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_read")
