@@ -275,6 +275,8 @@ class Cache:
         zeros beyond counts and beyond what a sequence holds."""
         ids, B = self._seqs(seqs)
         n, at = _sizes(n, -1 if layer is None else layer)
+        if layer is not None and at < 0:   # -1 is the C entry's name for all layers
+            raise MdsError(MDS_ESHAPE, f"layer {at}")
         shape = (B, n, self.kv_heads, self.head_dim)
         if layer is None:
             shape = (self.layers, *shape)

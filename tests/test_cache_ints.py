@@ -51,3 +51,21 @@ def test_calls():
     assert c.status() == (0, "ok")
     with pytest.raises(cache.MdsError):
         cache.Cache(1, 20, 2, 64, 2 + WIDE, 10)
+
+
+@pytest.mark.gpu
+def test_read_of_no_layer():
+    """-1 means every layer at the C entry only: the binding's outputs are
+    one layer's, and the call is refused before anything is written."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    c = cache.Cache(3, 20, 2, 64, 2, 10, page_tokens=16)
+    seqs = torch.tensor([0], device="cuda", dtype=torch.int32)
+    out = tuple(torch.full((3, 1, 5, 2, 64), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    with pytest.raises(cache.MdsError) as e:
+        c.read(-1, seqs, None, 5, out=(out[0][0], out[1][0]))
+    assert e.value.code == cache.MDS_ESHAPE
+    assert all((x == 7.0).all() for x in out)
+    c.read(None, seqs, None, 5, out=out)
+    assert not any(x.any() for x in out)
+    assert c.status() == (0, "ok")
