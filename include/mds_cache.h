@@ -45,7 +45,7 @@
  * mds_cache_status), and a step can be captured in a CUDA graph.
  *
  * seqs lists the batch's sequences, ids in [0, max_seqs), no id twice in one
- * call.  An id below 0 marks an unused place of the batch: nothing is done
+ * call (but in the src of mds_cache_fork).  An id below 0 marks an unused place of the batch: nothing is done
  * for it, and its outputs are zeros.  An id of max_seqs or more is treated
  * the same and sets MDS_ST_BADSEQ.
  *
@@ -173,11 +173,12 @@ int mds_cache_commit(mds_cache* cache, const int32_t* seqs, const int32_t* accep
                      const int32_t* out_tokens, int K, int L, int B, void* stream);
 
 /* Let dst[b], which must be empty, share all of src[b]'s pages, tokens
- * behind the committed ones included.  No id of dst may be in src. */
+ * behind the committed ones included.  src may name a sequence several times;
+ * no id of dst may be in src. */
 int mds_cache_fork(mds_cache* cache, const int32_t* src, const int32_t* dst, int B, void* stream);
 
-/* Shorten each sequence to lens[b] tokens (no effect where it has fewer) and
- * give back the pages behind them. */
+/* Shorten each sequence to lens[b] tokens (to its length where it has fewer)
+ * and give back what is behind: pages, and the slots that were reserved. */
 int mds_cache_truncate(mds_cache* cache, const int32_t* seqs, const int32_t* lens, int B, void* stream);
 
 /* Empty the sequences and give back their pages. */

@@ -249,14 +249,14 @@ class Cache:
             raise MdsError(rc, "mds_cache_commit")
 
     def fork(self, src, dst, stream=None):
-        """Let the empty sequences dst share src's pages."""
+        """Let the empty sequences dst share src's pages (src may name one several times)."""
         ids, B = self._seqs(src)
         rc = _lib.mds_cache_fork(self.ctx, ids, self._ints("dst", dst, (B,)), B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_fork")
 
     def truncate(self, seqs, lens, stream=None):
-        """Shorten sequences to lens tokens and give the pages behind back."""
+        """Shorten sequences to lens tokens and give back what is behind, reserved slots too."""
         ids, B = self._seqs(seqs)
         rc = _lib.mds_cache_truncate(self.ctx, ids, self._ints("lens", lens, (B,)), B, self._stream(stream))
         if rc != MDS_OK:

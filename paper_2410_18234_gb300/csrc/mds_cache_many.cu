@@ -20,12 +20,14 @@
 // Pipeline, tile t: load K, V (bulk copies) | widen K(t + 1), V(t) | S(t + 1)
 // into one of two buffers | weights(t) | O += V(t) W(t).
 //
-// Bound by the weighing warps: about 50 instructions for 8 columns of 32
-// slots, half of them the exponentials and the sums of rounded weights, and
-// the ends of groups (references, normalisers, O) on the same warps.  256
-// sequences of 257 to 1537 tokens, 33 nodes, 32 heads on 8: 306 us, 2.1 TB/s
-// of cache and 407 TFLOP/s (626 MB and 125 GFLOP: 92 us at HBM's rate); two
-// prompts' chunks of 1021 tokens behind 4000 to 5000: 245 us, 673 TFLOP/s.
+// Bound by the weighing warps, which wait for scores 13 to 20 % of the time
+// (clock stamps by role), where the product warp and the widening warps wait
+// for 44 to 88 %.  256 sequences of 257 to 1537 tokens, 33 nodes, 32 heads on
+// 8: 300 us, 2.1 TB/s of cache and 415 TFLOP/s (626 MB and 125 GFLOP: 92 us at
+// HBM's rate), of the weighing warps' time 30 % weights, 13 % votes, 21 %
+// masks, references and waits for the weights' buffer, 18 % the ends of groups
+// of 8 tiles.  Two prompts' chunks of 1021 tokens behind 4000 to 5000: 249 us,
+// 663 TFLOP/s, 36 % weights, 9 % votes, 27 % masks and references, 8 % ends.
 // Code size counts here: before waits, schedule and loops were kept short the
 // instruction cache missed a third of its requests, and the same work took
 // 1.4 times as long.

@@ -1,5 +1,6 @@
-// Device helpers of the three kernels (mds_flow.cu, mds_kernel.cu,
-// mds_topk.cu): inline PTX wrappers, the counter-based random
+// Device helpers of the verification's three kernels (mds_flow.cu,
+// mds_kernel.cu, mds_topk.cu), some of which the cache's attention
+// (mds_cache_attend.cuh) uses too: inline PTX wrappers, the counter-based random
 // numbers, logit IO, the exponent convention of every probability, and the
 // stage maximum flow of the weighted scheme.  Not part of the public ABI.
 #pragma once
