@@ -6,7 +6,8 @@
  *
  *   mds_cache_reserve    room for the n = 1 + K * L tokens of a draft tree
  *   per model layer:
- *     mds_cache_append   their keys and values, quantised to 8 bits
+ *     mds_cache_append   their keys and values, quantised to 8 bits (_append_rotated:
+ *                        with rotary positions)
  *     mds_cache_attend   attention of every tree node over the cache
  *   mds_verify           the target logits of the nodes against the drafts
  *   mds_cache_commit     the root and the accepted branch stay, packed; the
@@ -138,6 +139,45 @@ int mds_cache_reserve(mds_cache* cache, const int32_t* seqs, const int32_t* coun
  * otherwise). */
 int mds_cache_append(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* k,
                      const int64_t* k_strides, const void* v, const int64_t* v_strides, int n, int B, void* stream);
+
+/* Rotary positions.  The first `dim` dimensions of a head are pairs, (i, i +
+ * dim / 2) or, interleaved, (2 i, 2 i + 1): pair i of a node at position p
+ * (len + depth) becomes
+ *   magnitude * (a cos(p f_i) - b sin(p f_i)), magnitude * (a sin(p f_i) + b cos(p f_i)).
+ * The other dimensions stay as they are. */
+typedef struct {
+  int dim;            /* a multiple of 16, at most head_dim                     */
+  int interleaved;    /* 0 or 1                                                 */
+  double magnitude;   /* 2^-20 .. 2^20                                          */
+  uint64_t turns[64]; /* [dim / 2]: f_i / (2 pi), as a 64-bit fraction of a turn */
+} mds_cache_rotary;
+
+/* Fill *rotary from the frequencies f_i, freqs[dim / 2] radians a position,
+ * each in [-pi, pi] (host memory; MDS_ESHAPE for a dim that is not 16, 32 ..
+ * 128, MDS_EINVAL for other values out of range). */
+int mds_cache_rotary_init(mds_cache_rotary* rotary, const double* freqs, int dim, int interleaved, double magnitude);
+
+/* x[b][i][h] rotated to the position of node i of sequence b's tree of n = 1 +
+ * branches * L nodes, whether or not its slot is reserved.  x has strides like
+ * k above; out is [B][n][heads][head_dim] dtype, contiguous, aligned to 16
+ * bytes, and may be x itself (contiguous), but no other memory that x has.
+ * Angles are off by at most p * 2^-64 of a turn and a rounding to 32 bits;
+ * products and sums are 32-bit.  *rotary is read before the call returns. */
+int mds_cache_rotate(mds_cache* cache, const int32_t* seqs, const int32_t* counts, const mds_cache_rotary* rotary,
+                     const void* x, const int64_t* x_strides, void* out, int heads, int n, int branches, int B,
+                     void* stream);
+
+/* mds_cache_append with the keys rotated to their nodes' positions on the way,
+ * n = 1 + branches * L.  The quantiser Q takes the rotated keys as they are
+ * before any rounding (to about 2^-38 of the pair).  A pair with a number that
+ * is not finite, or whose rotation passes the largest float, is stored like
+ * numbers that are not finite.
+ * With q (NULL: none) the queries of the same nodes are rotated into q_out in
+ * the same launch, as by mds_cache_rotate. */
+int mds_cache_append_rotated(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts,
+                             const mds_cache_rotary* rotary, const void* k, const int64_t* k_strides, const void* v,
+                             const int64_t* v_strides, const void* q, const int64_t* q_strides, void* q_out,
+                             int q_heads, int n, int branches, int B, void* stream);
 
 /* Attention of the n = 1 + branches * L nodes of each sequence's tree over
  * layer `layer` of the cache (their own keys and values appended before):

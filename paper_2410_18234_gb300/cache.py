@@ -8,7 +8,7 @@ one given.  A step of multi-draft decoding:
     c = cache.Cache(layers, pages, kv_heads, head_dim, max_seqs, max_pages)
     c.reserve(seqs, 1 + K * L)
     for layer in range(layers):
-        c.append(layer, seqs, k, v)                    # [B][1 + K * L][kv_heads][head_dim]
+        c.append(layer, seqs, k, v)                    # [B][1 + K * L][kv_heads][head_dim]; append_rotated: with positions
         o = c.attend(layer, seqs, q, branches=K)       # [B][1 + K * L][q_heads][head_dim]
     out_tokens, accept_len, _ = verifier.verify(...)   # mds.Verifier
     c.commit(seqs, accept_len, branches=K, length=L, draft_tokens=tokens, out_tokens=out_tokens)
@@ -31,7 +31,7 @@ MAX_GROUP = 64          # MDS_CACHE_MAX_GROUP
 
 # every symbol include/mds_cache.h declares
 EXPORTS = ("mds_cache_bytes", "mds_cache_create", "mds_cache_state", "mds_cache_reserve", "mds_cache_append",
-           "mds_cache_attend", "mds_cache_commit", "mds_cache_fork", "mds_cache_truncate", "mds_cache_free",
+           "mds_cache_rotary_init", "mds_cache_rotate", "mds_cache_append_rotated", "mds_cache_attend", "mds_cache_commit", "mds_cache_fork", "mds_cache_truncate", "mds_cache_free",
            "mds_cache_read", "mds_cache_status", "mds_cache_destroy")
 
 
@@ -41,15 +41,23 @@ class CacheConfig(ctypes.Structure):
                 ("max_pages", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
+class RotaryStruct(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("magnitude", ctypes.c_double),
+                ("turns", ctypes.c_uint64 * 64)]
+
+
 def _bind(lib):
-    vp, i, i64p = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(ctypes.c_int64)
-    cfg = ctypes.POINTER(CacheConfig)
+    vp, i, i64p, f64 = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(ctypes.c_int64), ctypes.c_double
+    cfg, rot = ctypes.POINTER(CacheConfig), ctypes.POINTER(RotaryStruct)
     types = {
         "mds_cache_bytes": [cfg],
         "mds_cache_create": [ctypes.POINTER(vp), cfg, i, vp, vp],
         "mds_cache_state": [vp, ctypes.POINTER(vp), ctypes.POINTER(vp)],
         "mds_cache_reserve": [vp, vp, vp, i, i, vp],
         "mds_cache_append": [vp, i, vp, vp, vp, i64p, vp, i64p, i, i, vp],
+        "mds_cache_rotary_init": [rot, ctypes.POINTER(f64), i, i, f64],
+        "mds_cache_rotate": [vp, vp, vp, rot, vp, i64p, vp, i, i, i, i, vp],
+        "mds_cache_append_rotated": [vp, i, vp, vp, rot, vp, i64p, vp, i64p, vp, i64p, vp, i, i, i, i, vp],
         "mds_cache_attend": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, i, ctypes.c_float, i, vp],
         "mds_cache_commit": [vp, vp, vp, vp, vp, i, i, i, vp],
         "mds_cache_fork": [vp, vp, vp, i, vp],
@@ -93,6 +101,44 @@ def cache_bytes(layers, pages, kv_heads, head_dim, max_seqs, max_pages, page_tok
     if n == 0:
         raise MdsError(MDS_ESHAPE, "mds_cache_bytes")
     return n
+
+
+class Rotary:
+    """Rotary positions of the first ``dim`` (a multiple of 16) dimensions of a
+    head, for `Cache.rotate` and `Cache.append_rotated`: pairs of dimensions
+    (i, i + dim / 2), or (2 i, 2 i + 1) where ``interleaved``, turned by
+    position * f_i and scaled by ``magnitude``.
+
+    f_i is ``freqs[i]`` radians a position where ``freqs`` is given, else
+    base ** (-2 i / dim), for contexts longer than the model was trained on
+    divided by ``factor``: all alike, or, with ``original`` (tokens) above 0,
+    wholly where a pair turns ``slow`` times or less in that many tokens, not
+    where it turns ``fast`` times or more, and by a line in between.  It holds
+    no device memory, and any cache may use it.
+    """
+
+    def __init__(self, dim, base=10000.0, interleaved=False, factor=1.0, original=0, fast=32.0, slow=1.0,
+                 magnitude=1.0, freqs=None):
+        dim, = _sizes(dim)
+        if not 16 <= dim <= 128 or dim % 16:
+            raise MdsError(MDS_ESHAPE, f"dim {dim}: a multiple of 16 up to 128")
+        if freqs is None:
+            if not (1 <= base < math.inf and 0 < factor < math.inf and 0 <= original < math.inf and slow < fast):
+                raise MdsError(MDS_EINVAL, f"base {base}, factor {factor}, original {original}, slow {slow}, fast {fast}")
+            freqs = []
+            for i in range(dim // 2):
+                f = float(base) ** (-2 * i / dim)
+                keep = min(max((original * f / (2 * math.pi) - slow) / (fast - slow), 0.0), 1.0) if original else 0.0
+                freqs.append(f * (keep + (1 - keep) / factor))
+        #: radians a position of each pair
+        self.freqs = [float(f) for f in freqs]
+        if len(self.freqs) != dim // 2:
+            raise MdsError(MDS_ESHAPE, f"{len(self.freqs)} frequencies for {dim // 2} pairs")
+        self.struct = RotaryStruct()
+        rc = _lib.mds_cache_rotary_init(ctypes.byref(self.struct), (ctypes.c_double * (dim // 2))(*self.freqs), dim,
+                                        int(bool(interleaved)), float(magnitude))
+        if rc != MDS_OK:
+            raise MdsError(rc, "mds_cache_rotary_init")
 
 
 class Cache:
@@ -197,6 +243,18 @@ class Cache:
                 t.record_stream(torch.cuda.ExternalStream(int(stream), device=self.device))
         return got
 
+    def _apart(self, out, same, others=()):
+        """Refuse a given output that shares memory with an input: `same` may
+        be the output itself, element for element."""
+        def span(t):
+            return t.data_ptr(), t.data_ptr() + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+        a, b = span(out)
+        for t in (same, *others):
+            c, d = span(t)
+            if a < d and c < b and not (t is same and t.data_ptr() == out.data_ptr() and t.is_contiguous()):
+                raise MdsError(MDS_EINVAL, "out shares memory with an input")
+
     # ------------------------------------------------------------- calls
 
     def reserve(self, seqs, n, counts=None, stream=None):
@@ -219,6 +277,51 @@ class Cache:
                                    v.data_ptr(), vs, k.shape[1], B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_append")
+
+    def rotate(self, seqs, x, rotary, branches=1, counts=None, out=None, stream=None):
+        """Heads x [B][1 + branches * L][heads][head_dim] (a strided view with
+        16-byte rows) rotated to the positions of the sequences' tree nodes.
+        ``out`` may be x itself."""
+        ids, B = self._seqs(seqs)
+        xs = self._rows("x", x, B)
+        branches, = _sizes(branches)
+        o, = self._outs(tuple(x.shape), stream, None if out is None else (out,))
+        if out is not None and x.numel():
+            self._apart(out, x)
+        rc = _lib.mds_cache_rotate(self.ctx, ids, self._ints("counts", counts, (B,)), ctypes.byref(rotary.struct),
+                                   x.data_ptr(), xs, o.data_ptr(), x.shape[2], x.shape[1], branches, B,
+                                   self._stream(stream))
+        if rc != MDS_OK:
+            raise MdsError(rc, "mds_cache_rotate")
+        return o
+
+    def append_rotated(self, layer, seqs, k, v, rotary, branches=1, q=None, counts=None, out=None, stream=None):
+        """`append` with the keys rotated to their nodes' positions on the way
+        (n = 1 + branches * L).  With q [B][n][q_heads][head_dim] the same
+        launch rotates the queries, as `rotate` does; returns them, or None."""
+        ids, B = self._seqs(seqs)
+        ks, vs = self._rows("k", k, B, self.kv_heads), self._rows("v", v, B, self.kv_heads)
+        if k.shape != v.shape:
+            raise MdsError(MDS_ESHAPE, f"k has shape {tuple(k.shape)}, v {tuple(v.shape)}")
+        layer, branches = _sizes(layer, branches)
+        qs = o = None
+        if q is not None:
+            qs = self._rows("q", q, B)
+            if q.shape[1] != k.shape[1]:
+                raise MdsError(MDS_ESHAPE, f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
+            o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
+            if out is not None and q.numel():
+                self._apart(out, q, (k, v))
+        elif out is not None:
+            raise MdsError(MDS_EINVAL, "out without q")
+        rc = _lib.mds_cache_append_rotated(self.ctx, layer, ids, self._ints("counts", counts, (B,)),
+                                           ctypes.byref(rotary.struct), k.data_ptr(), ks, v.data_ptr(), vs,
+                                           None if q is None else q.data_ptr(), qs, None if q is None else o.data_ptr(),
+                                           0 if q is None else q.shape[2], k.shape[1], branches, B,
+                                           self._stream(stream))
+        if rc != MDS_OK:
+            raise MdsError(rc, "mds_cache_append_rotated")
+        return o
 
     def attend(self, layer, seqs, q, branches=1, counts=None, window=0, sinks=0, scale=None, out=None, stream=None):
         """Attention of the nodes of every sequence's tree: q is

@@ -1,5 +1,6 @@
 // Entry points of the key/value cache (include/mds_cache.h): argument checks,
 // the layout of the caller's memory, and the launches.
+#include <cmath>
 #include <new>
 #include <type_traits>
 
@@ -97,6 +98,11 @@ bool rows_ok(const void* p, const int64_t* strides, int es) {
   return true;
 }
 
+bool rotary_ok(const mds_cache_rotary* r) {
+  return r && (r->interleaved == 0 || r->interleaved == 1) && r->magnitude >= 0x1p-20 && r->magnitude <= 0x1p20;
+}
+bool dim_ok(int dim, int head_dim) { return dim >= 16 && dim <= head_dim && dim % 16 == 0; }
+
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 
 }  // namespace
@@ -171,6 +177,65 @@ int mds_cache_append(mds_cache* c, int layer, const int32_t* seqs, const int32_t
   DeviceGuard g(c->device);
   return done(mds::cache::append(c->s, layer, seqs, counts, k, k_strides, v, v_strides, n, B, stream_of(stream)),
               "mds_cache_append");
+}
+
+int mds_cache_rotary_init(mds_cache_rotary* rotary, const double* freqs, int dim, int interleaved, double magnitude) {
+  if (!rotary || !freqs) return MDS_EINVAL;
+  if (!dim_ok(dim, 128)) return MDS_ESHAPE;
+  mds_cache_rotary r{dim, interleaved, magnitude, {}};
+  if (!rotary_ok(&r)) return MDS_EINVAL;
+  // 1 / (2 pi) in two parts: the turn is off by 2^-64, not by the 2^-53 of one product
+  constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;
+  for (int i = 0; i < dim / 2; ++i) {
+    const double f = freqs[i];
+    if (!(std::fabs(f) <= 3.14159265358979312)) return MDS_EINVAL;
+    const double h = f * kHigh, l = std::fma(f, kHigh, -h) + f * kLow;
+    // either part in units of 2^-64 modulo 2^64; |h| may be a half, 2^63 units
+    r.turns[i] = 2 * (uint64_t)(int64_t)std::llrint(std::ldexp(h, 63)) +
+                 (uint64_t)(int64_t)std::llrint(std::ldexp(h, 64) - 2 * (double)std::llrint(std::ldexp(h, 63)) + std::ldexp(l, 64));
+  }
+  *rotary = r;
+  return MDS_OK;
+}
+
+int mds_cache_rotate(mds_cache* c, const int32_t* seqs, const int32_t* counts, const mds_cache_rotary* rotary,
+                     const void* x, const int64_t* x_strides, void* out, int heads, int n, int branches, int B,
+                     void* stream) {
+  const int rc = batch(c, seqs, B);
+  if (rc != MDS_OK) return rc;
+  if (!rotary_ok(rotary)) return MDS_EINVAL;
+  if (!dim_ok(rotary->dim, c->cfg.head_dim) || n < 0 || n > MDS_CACHE_MAX_TOKENS || branches < 1 || heads < 1 ||
+      heads > 65536 || (n > 0 && (n - 1) % branches))
+    return MDS_ESHAPE;
+  if (B == 0 || n == 0) return MDS_OK;
+  const int es = esize_of(c->cfg.dtype);
+  if (!rows_ok(x, x_strides, es) || !out || !aligned(out, 16) || (counts && !aligned(counts, 4))) return MDS_EINVAL;
+  DeviceGuard g(c->device);
+  mds::cache::Rotate a{rotary, seqs, counts, nullptr, nullptr, nullptr, nullptr, x, x_strides, out, 0, heads, n,
+                       (n - 1) / branches, B};
+  return done(mds::cache::rotate(c->s, a, stream_of(stream)), "mds_cache_rotate");
+}
+
+int mds_cache_append_rotated(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts,
+                             const mds_cache_rotary* rotary, const void* k, const int64_t* k_strides, const void* v,
+                             const int64_t* v_strides, const void* q, const int64_t* q_strides, void* q_out,
+                             int q_heads, int n, int branches, int B, void* stream) {
+  const int rc = batch(c, seqs, B);
+  if (rc != MDS_OK) return rc;
+  if (!rotary_ok(rotary)) return MDS_EINVAL;
+  if (!dim_ok(rotary->dim, c->cfg.head_dim) || layer < 0 || layer >= c->cfg.layers || n < 0 ||
+      n > MDS_CACHE_MAX_TOKENS || branches < 1 || (n > 0 && (n - 1) % branches) ||
+      (q && (q_heads < 1 || q_heads > 65536)))
+    return MDS_ESHAPE;
+  if (B == 0 || n == 0) return MDS_OK;
+  const int es = esize_of(c->cfg.dtype);
+  if (!rows_ok(k, k_strides, es) || !rows_ok(v, v_strides, es) || (counts && !aligned(counts, 4)) ||
+      (q && (!rows_ok(q, q_strides, es) || !q_out || !aligned(q_out, 16))))
+    return MDS_EINVAL;
+  DeviceGuard g(c->device);
+  mds::cache::Rotate a{rotary, seqs, counts, k, k_strides, v, v_strides, q, q_strides, q_out, layer, q ? q_heads : 0, n,
+                       (n - 1) / branches, B};
+  return done(mds::cache::rotate(c->s, a, stream_of(stream)), "mds_cache_append_rotated");
 }
 
 int mds_cache_attend(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,

@@ -1,6 +1,7 @@
 // Internal interface of the key/value cache (declared in
 // include/mds_cache.h) between its entry points (mds_cache_api.cu) and its
-// kernels (mds_cache_pages.cu, mds_cache_few.cu, mds_cache_many.cu).
+// kernels (mds_cache_pages.cu, mds_cache_rotary.cu, mds_cache_few.cu,
+// mds_cache_many.cu).
 #pragma once
 #include <cuda_runtime.h>
 
@@ -53,6 +54,22 @@ cudaError_t truncate(const State& s, const int32_t* seqs, const int32_t* lens, i
 cudaError_t read(const State& s, int layer, const int32_t* seqs, const int32_t* start, const int32_t* counts, void* k,
                  void* v, int n, int B, cudaStream_t st);
 cudaError_t clear(const State& s, cudaStream_t st);
+
+// Heads rotated by their nodes' positions; with k, keys and values stored.
+struct Rotate {
+  const mds_cache_rotary* rotary;
+  const int32_t* seqs;
+  const int32_t* counts;
+  const void* k;
+  const int64_t* ks;
+  const void* v;
+  const int64_t* vs;
+  const void* q;
+  const int64_t* qs;
+  void* out;
+  int layer, heads, n, L, B;
+};
+cudaError_t rotate(const State& s, const Rotate& a, cudaStream_t st);   // mds_cache_rotary.cu
 
 struct Attend {
   const int32_t* seqs;
