@@ -31,7 +31,8 @@ MAX_GROUP = 64          # MDS_CACHE_MAX_GROUP
 
 # every symbol include/mds_cache.h declares
 EXPORTS = ("mds_cache_bytes", "mds_cache_create", "mds_cache_state", "mds_cache_reserve", "mds_cache_append",
-           "mds_cache_rotary_init", "mds_cache_rotate", "mds_cache_append_rotated", "mds_cache_attend", "mds_cache_commit", "mds_cache_fork", "mds_cache_truncate", "mds_cache_free",
+           "mds_cache_rotary_init", "mds_cache_rotate", "mds_cache_append_rotated", "mds_cache_attend",
+           "mds_cache_attend_shared", "mds_cache_commit", "mds_cache_fork", "mds_cache_truncate", "mds_cache_free",
            "mds_cache_read", "mds_cache_status", "mds_cache_destroy")
 
 
@@ -59,6 +60,7 @@ def _bind(lib):
         "mds_cache_rotate": [vp, vp, vp, rot, vp, i64p, vp, i, i, i, i, vp],
         "mds_cache_append_rotated": [vp, i, vp, vp, rot, vp, i64p, vp, i64p, vp, i64p, vp, i, i, i, i, vp],
         "mds_cache_attend": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, i, ctypes.c_float, i, vp],
+        "mds_cache_attend_shared": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, ctypes.c_float, i, vp],
         "mds_cache_commit": [vp, vp, vp, vp, vp, i, i, i, vp],
         "mds_cache_fork": [vp, vp, vp, i, vp],
         "mds_cache_truncate": [vp, vp, vp, i, vp],
@@ -337,6 +339,24 @@ class Cache:
                                    self.head_dim ** -0.5 if scale is None else float(scale), B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_attend")
+        return o
+
+    def attend_shared(self, layer, seqs, q, group, branches=1, counts=None, scale=None, out=None, stream=None):
+        """`attend` (without a window) for sequences that share a prefix: each
+        ``group`` (a divisor of B) sequences of the list in turn, such as the
+        forks of one prompt; unused places pad a smaller group.  The pages
+        that all of a group hold, as far as they are committed, are read once
+        for all of them."""
+        ids, B = self._seqs(seqs)
+        qs = self._rows("q", q, B)
+        layer, branches, group = _sizes(layer, branches, group)
+        o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
+        rc = _lib.mds_cache_attend_shared(self.ctx, layer, ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
+                                          o.data_ptr(), q.shape[2], q.shape[1], branches, group,
+                                          self.head_dim ** -0.5 if scale is None else float(scale), B,
+                                          self._stream(stream))
+        if rc != MDS_OK:
+            raise MdsError(rc, "mds_cache_attend_shared")
         return o
 
     def commit(self, seqs, accept_len, branches=1, length=0, draft_tokens=None, out_tokens=None, stream=None):

@@ -64,6 +64,7 @@ size_t carve(const mds_cache_config& c, char* base, State& s) {
   take(s.kept, (size_t)MDS_CACHE_MAX_BATCH * 8);
   take(s.arrive, (size_t)c.max_seqs * 4);
   take(s.joins, mds::cache::kJoins * 4);
+  take(s.share, (size_t)MDS_CACHE_MAX_BATCH * 8);
   take(s.free_count, 64);
   s.n_copies = s.free_count + 1;
   s.status = reinterpret_cast<uint32_t*>(s.free_count + 2);
@@ -238,13 +239,13 @@ int mds_cache_append_rotated(mds_cache* c, int layer, const int32_t* seqs, const
   return done(mds::cache::rotate(c->s, a, stream_of(stream)), "mds_cache_append_rotated");
 }
 
-int mds_cache_attend(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
-                     const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
-                     float scale, int B, void* stream) {
+static int attend_call(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
+                       const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
+                       float scale, int group, int B, void* stream, const char* name) {
   const int rc = batch(c, seqs, B);
   if (rc != MDS_OK) return rc;
   if (layer < 0 || layer >= c->cfg.layers || n < 0 || n > MDS_CACHE_MAX_NODES || branches < 1 || q_heads < 1 ||
-      q_heads % c->cfg.kv_heads || q_heads / c->cfg.kv_heads > MDS_CACHE_MAX_GROUP)
+      q_heads % c->cfg.kv_heads || q_heads / c->cfg.kv_heads > MDS_CACHE_MAX_GROUP || group < 1 || B % group)
     return MDS_ESHAPE;
   if (n > 0 && (n - 1) % branches) return MDS_ESHAPE;
   if (window < 0 || sinks < 0 || !(scale - scale == 0.f)) return MDS_EINVAL;
@@ -254,7 +255,22 @@ int mds_cache_attend(mds_cache* c, int layer, const int32_t* seqs, const int32_t
   DeviceGuard g(c->device);
   mds::cache::Attend a{seqs, counts, q, q_strides[0], q_strides[1], q_strides[2], out, layer, B, n,
                        (n - 1) / branches, q_heads, window, sinks, scale};
-  return done(mds::cache::attend(c->s, a, c->sms, stream_of(stream)), "mds_cache_attend");
+  return done(group > 1 ? mds::cache::attend_shared(c->s, a, group, c->sms, stream_of(stream))
+                        : mds::cache::attend(c->s, a, c->sms, stream_of(stream)), name);
+}
+
+int mds_cache_attend(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
+                     const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
+                     float scale, int B, void* stream) {
+  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, window, sinks, scale, 1, B, stream,
+                     "mds_cache_attend");
+}
+
+int mds_cache_attend_shared(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
+                            const int64_t* q_strides, void* out, int q_heads, int n, int branches, int group,
+                            float scale, int B, void* stream) {
+  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, 0, 0, scale, group, B, stream,
+                     "mds_cache_attend_shared");
 }
 
 int mds_cache_commit(mds_cache* c, const int32_t* seqs, const int32_t* accept_len, const int32_t* draft_tokens,

@@ -9,11 +9,18 @@
 // per SM) share evenly, so ragged lengths and few sequences load every SM.  A
 // group cut between blocks is joined by the last of them to finish, which
 // adds the pieces in their order: results do not depend on timing.
+//
+// Parts.  A call is one launch (kAll), or two where sequences share a prefix:
+// kPrefix takes every group of sequences as one of `members` times as many
+// nodes over the prefix's tiles, and leaves each row's reference, normaliser
+// and sums in `prior`; kRest takes the sequences over the tiles behind it, and
+// joins what it finds there like one more piece.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <cfloat>
+#include <climits>
 
 #include "mds_cache_internal.h"
 #include "mds_device.cuh"
@@ -36,9 +43,11 @@ constexpr float kNone = -FLT_MAX;          // reference of a row that has seen n
 constexpr float kSlack = 32.f;             // the reference moves when a weight passes 2^32
 constexpr unsigned kWaitTries = 1u << 18;
 
+enum Part { kAll, kPrefix, kRest };
+
 struct Params {
   State s;
-  Attend a;
+  Attend a;                // kPrefix: a.B groups of a.n nodes of all members together
   int span;                // slots that one copy brings: a page, or a tile's part of it
   int g, rows, row_tiles, stages;
   int rows_per;            // rows of a row tile
@@ -46,12 +55,25 @@ struct Params {
   // and a packed sum behind it into one fused operation, rounding modes or
   // not, but not a product and a fused operation by this number.
   float one = 1.f;
+  int members = 1, nodes = 0;      // sequences of a group, and nodes of one
+  float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
 };
 
 // A sequence's part of the call.
+template <int kPart>
 struct Seq {
   int q, len, live, end;   // id, committed, live nodes, slots reserved (a slot behind them is not read)
 };
+template <>
+struct Seq<kRest> {
+  int q, len, live, end;
+  int from;                // the prefix's tokens
+};
+// Bytes of B of them, in whole units of 16.
+template <int kPart>
+__host__ __device__ constexpr int seq_bytes(int B) {
+  return (B * (int)sizeof(Seq<kPart>) + 15) / 16 * 16;
+}
 
 // A group's key tiles: `sink` tiles from slot 0, then those from `first` on.
 struct Group {
@@ -59,7 +81,8 @@ struct Group {
   int sink_tiles, first, tiles;
 };
 
-__device__ __forceinline__ Group group_of(const Params& p, const Seq& q, int rt) {
+template <int kPart>
+__device__ __forceinline__ Group group_of(const Params& p, const Seq<kPart>& q, int rt) {
   Group r;
   const int i0 = rt * p.rows_per / p.g, i1 = min((rt * p.rows_per + p.rows_per - 1) / p.g, q.live - 1);
   r.tiles = 0;
@@ -72,6 +95,7 @@ __device__ __forceinline__ Group group_of(const Params& p, const Seq& q, int rt)
     r.lo = (int)min(max(pos - p.a.window + 1, (int64_t)0), (int64_t)q.len);
     r.sinks = min(p.a.sinks, r.lo);
   }
+  if constexpr (kPart == kRest) r.lo = q.from;   // a multiple of kTile
   r.first = r.lo / kTile;
   r.sink_tiles = min((r.sinks + kTile - 1) / kTile, r.first);
   r.tiles = r.sink_tiles + max((r.hi + kTile - 1) / kTile - r.first, 0);
@@ -161,7 +185,8 @@ struct Cursor {
 };
 
 // The group and tile of unit u (whole warp).
-__device__ Cursor locate(const Params& p, const long long* prefix, const Seq* seqs, long long u) {
+template <int kPart>
+__device__ Cursor locate(const Params& p, const long long* prefix, const Seq<kPart>* seqs, long long u) {
   const int lane = threadIdx.x & 31;
   int lo = 0, hi = p.a.B - 1;
   while (lo < hi) {   // the last b with prefix[b] <= u
@@ -175,7 +200,7 @@ __device__ Cursor locate(const Params& p, const long long* prefix, const Seq* se
   const long long rem = u - prefix[lo];
   c.h = (int)(rem / per);
   long long in = rem % per;
-  const Seq q = seqs[lo];
+  const Seq<kPart> q = seqs[lo];
   for (int r0 = 0;; r0 += 32) {
     const int rt = r0 + lane;
     int t = rt < p.row_tiles ? group_of(p, q, rt).tiles : 0;
@@ -196,7 +221,8 @@ __device__ Cursor locate(const Params& p, const long long* prefix, const Seq* se
 }
 
 // The next group that has tiles.  False past the end.
-__device__ bool advance(const Params& p, const Seq* seqs, Cursor& c, Group& grp) {
+template <int kPart>
+__device__ bool advance(const Params& p, const Seq<kPart>* seqs, Cursor& c, Group& grp) {
   c.off = 0;
   for (;;) {
     if (++c.rt >= p.row_tiles || c.rt * p.rows_per / p.g >= seqs[c.b].live) {
@@ -224,30 +250,85 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* out, float4
   *reinterpret_cast<uint2*>(out) = uint2{pack_bf16(x.x, x.y), pack_bf16(x.z, x.w)};
 }
 
+// Sequence b of the list, whose live nodes end with its reserved slots.
+// True where the call asks for what is not there.
+__device__ __forceinline__ bool find(const State& s, const int32_t* seqs, const int32_t* counts, int b, int n, int* q,
+                                     int* len, int* live, int* end) {
+  const int id = seqs[b];
+  *q = -1;
+  *len = *live = *end = 0;
+  if (id < 0 || id >= s.max_seqs) return id >= 0;
+  *q = id;
+  *len = s.lens[id];
+  *live = counts ? min(max(counts[b], 0), n) : n;
+  *end = s.reach[id];
+  const bool bad = *len + *live > *end && *live > 0;
+  if (bad) *live = min(*live, max(*end - *len, 0));   // rows without a slot of their own are zeros
+  return bad;
+}
+
+// What the live sequences of a group share: at the group's first place of
+// `least` the fewest tokens, and how many sequences there are.  (All threads.)
+__device__ __forceinline__ void common(const Params& p, int b, int* least, int* count) {
+  const int2 x = __ldg(p.s.share + b);
+  if (x.y <= 0) return;
+  atomicMin(least, x.x);
+  atomicAdd(count, 1);
+}
+
 // The plan, by all of the block's threads: seqs and the exclusive sums of
 // their tiles, and zeros in the rows of nodes that are not live.
-template <typename T>
-__device__ void plan(const Params& p, long long* prefix, Seq* seqs, int head_dim) {
+template <typename T, int kPart>
+__device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int head_dim) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  for (int b = tid; b < p.a.B; b += blockDim.x) {
-    const int id = p.a.seqs[b];
-    Seq q{-1, 0, 0, 0};
-    if (id >= p.s.max_seqs) atomicOr(p.s.status, MDS_ST_BADSEQ);
-    else if (id >= 0) {
-      q.q = id;
-      q.len = p.s.lens[id];
-      q.live = p.a.counts ? min(max(p.a.counts[b], 0), p.a.n) : p.a.n;
-      q.end = p.s.reach[id];
-      if (q.len + q.live > q.end && q.live > 0) {
-        atomicOr(p.s.status, MDS_ST_BADSEQ);
-        q.live = min(q.live, max(q.end - q.len, 0));   // rows without a slot of their own are zeros
+  if constexpr (kPart == kPrefix) {
+    // q: the place of the group's first live sequence; len: what is shared;
+    // end: live sequences; live: nodes up to the last live sequence
+    for (int g = tid; g < p.a.B; g += blockDim.x) seqs[g] = Seq<kPart>{INT_MAX, INT_MAX, 0, 0};
+    __syncthreads();
+    for (int b = tid; b < p.a.B * p.members; b += blockDim.x) {
+      Seq<kPart>& q = seqs[b / p.members];
+      common(p, b, &q.len, &q.end);
+      if (__ldg(p.s.share + b).y > 0) {
+        atomicMin(&q.q, b);
+        atomicMax(&q.live, (b % p.members + 1) * p.nodes);
       }
     }
-    seqs[b] = q;
+    __syncthreads();
+    for (int g = tid; g < p.a.B; g += blockDim.x) {
+      const Seq<kPart> q = seqs[g];
+      const bool any = q.end > 1 && q.len > 0;
+      seqs[g] = any ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
+    }
+  } else {
+    if constexpr (kPart == kRest) {
+      // a group's first place holds what is shared, and in q how many are live
+      for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = INT_MAX, seqs[b].q = 0;
+      __syncthreads();
+      for (int b = tid; b < p.a.B; b += blockDim.x) {
+        Seq<kPart>& first = seqs[b / p.members * p.members];
+        common(p, b, &first.from, &first.q);
+      }
+      __syncthreads();
+      for (int b = tid; b < p.a.B; b += blockDim.x) {
+        const Seq<kPart>& first = seqs[b / p.members * p.members];
+        if (b % p.members) seqs[b].from = first.q > 1 ? first.from : 0;
+      }
+      __syncthreads();
+      for (int b = tid; b < p.a.B; b += blockDim.x)
+        if (b % p.members == 0 && seqs[b].q < 2) seqs[b].from = 0;
+      __syncthreads();
+    }
+    for (int b = tid; b < p.a.B; b += blockDim.x) {
+      Seq<kPart>& q = seqs[b];
+      int id, len, live, end;
+      if (find(p.s, p.a.seqs, p.a.counts, b, p.a.n, &id, &len, &live, &end)) atomicOr(p.s.status, MDS_ST_BADSEQ);
+      q.q = id, q.len = len, q.live = live, q.end = end;
+    }
   }
   __syncthreads();
   for (int b = warp; b < p.a.B; b += warps) {
-    const Seq q = seqs[b];
+    const Seq<kPart> q = seqs[b];
     long long t = 0;
     const int tiles = min(p.row_tiles, (q.live * p.g + p.rows_per - 1) / p.rows_per);
     for (int rt = lane; rt < tiles; rt += 32) t += group_of(p, q, rt).tiles;
@@ -270,7 +351,7 @@ __device__ void plan(const Params& p, long long* prefix, Seq* seqs, int head_dim
     }
   }
   T* out = static_cast<T*>(p.a.out);
-  for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {
+  for (int b = blockIdx.x; b < (kPart == kPrefix ? 0 : p.a.B); b += gridDim.x) {
     const int64_t row = (int64_t)p.a.heads * head_dim;
     const int64_t from = ((int64_t)b * p.a.n + seqs[b].live) * row, to = (int64_t)(b + 1) * p.a.n * row;
     for (int64_t i = from + tid * 4; i < to; i += blockDim.x * 4) store4(out + i, float4{0.f, 0.f, 0.f, 0.f});
@@ -296,7 +377,8 @@ struct Job {
 };
 
 // The scheduler warp: c is the place of unit u0.
-__device__ __forceinline__ void schedule(const Params& p, const Seq* seqs, Cursor c, long long per, long long u0,
+template <int kPart>
+__device__ __forceinline__ void schedule(const Params& p, const Seq<kPart>* seqs, Cursor c, long long per, long long u0,
                                          long long u1, Job* jobs, uint64_t* ready, uint64_t* taken, int* abort) {
   const int lane = threadIdx.x & 31;
   Group grp = group_of(p, seqs[c.b], c.rt);
@@ -309,7 +391,7 @@ __device__ __forceinline__ void schedule(const Params& p, const Seq* seqs, Curso
       Job& j = jobs[slot];
       j.cnt = cnt;
       if (cnt) {
-        const Seq q = seqs[c.b];
+        const Seq<kPart> q = seqs[c.b];
         j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
         j.q = q.q, j.len = q.len, j.live = q.live;
         j.first_block = (int)((u - c.off) / per);
@@ -339,27 +421,57 @@ __device__ __forceinline__ float* piece_of(const Params& p, int block, bool begi
   return p.s.part + ((int64_t)block * 2 + (begins ? 1 : 0)) * p.rows_per * kPieceRow<D>;
 }
 
+// Where node `node` of sequence b of the list (kPrefix: of group b) has its
+// queries, from the call's first; -1 for a node that is not live.
+template <int kPart>
+__device__ __forceinline__ int64_t query_at(const Params& p, int b, int node, int live) {
+  if constexpr (kPart == kPrefix) {
+    if (node >= live) return -1;
+    const int m = b * p.members + node / p.nodes, i = node % p.nodes;
+    return i < __ldg(p.s.share + m).y ? m * p.a.q_seq + i * p.a.q_tok : -1;
+  } else {
+    return node < live ? b * p.a.q_seq + node * p.a.q_tok : -1;
+  }
+}
+
+// A row's place in the call, rows of heads of nodes of sequences.
+__device__ __forceinline__ int64_t row_at(const Params& p, int b, int h, int row) {
+  return ((int64_t)b * p.a.n + row / p.g) * p.a.heads + h * p.g + row % p.g;
+}
+template <int D>
+__device__ __forceinline__ float* prior_of(const Params& p, int64_t row) {
+  return p.prior + row * kPieceRow<D>;
+}
+
 // Where row `row` of head group h of sequence b of the list goes.
 template <typename T>
 __device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, int head_dim) {
-  const int64_t node = (int64_t)b * p.a.n + row / p.g;
-  return static_cast<T*>(p.a.out) + (node * p.a.heads + h * p.g + row % p.g) * head_dim;
+  return static_cast<T*>(p.a.out) + row_at(p, b, h, row) * head_dim;
 }
 
 // Add the pieces that blocks c0..c1 left of a row tile, in their order.  First
 // the rows' references and normalisers (into `stat`, shared memory of
 // rows_per), then the dimensions, four a thread, kItems such and kAhead pieces
 // at a time: a join is a wait for memory at the end of a block, so loads are
-// issued together (many rows have few pieces, few rows many).
-template <typename T, int D, int kItems, int kAhead>
-__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, float2* stat, int tid,
-                            int threads) {
+// issued together (many rows have few pieces, few rows many).  kPrefix: the
+// sums go to `prior` as they are; kRest with `prior`: what is there is the
+// last piece.
+template <typename T, int D, int kItems, int kAhead, int kPart>
+__device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, bool prior, float2* stat,
+                            int tid, int threads) {
   constexpr int R = kPieceRow<D>;
-  const int lane = tid & 31, pieces = c1 - c0 + 1;
+  const int lane = tid & 31, blocks = c1 - c0 + 1, pieces = blocks + (kPart == kRest && prior);
   const int64_t stride = 2 * (int64_t)p.rows_per * R;
   const float* first = piece_of<D>(p, c0, true);
   const float* later = piece_of<D>(p, c0, false);   // + stride for each block further
-  auto at = [&](int cc, int r) { return (cc ? later + cc * stride : first) + r * R; };
+  auto at = [&](int cc, int r) -> const float* {
+    if constexpr (kPart == kRest) {
+      // a row that is not live has none there, and is not stored: any piece will do
+      if (cc == blocks && (row0 + r) / p.g < live) return prior_of<D>(p, row_at(p, b, h, row0 + r));
+      if (cc == blocks) cc = 0;
+    }
+    return (cc ? later + cc * stride : first) + r * R;
+  };
   if (pieces <= 8 && p.rows_per <= threads) {   // a thread a row
     if (tid < p.rows_per) {
       float2 y[8];
@@ -370,7 +482,7 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
       for (int cc = 0; cc < 8; ++cc) top = fmaxf(top, y[cc].x);
 #pragma unroll
       for (int cc = 0; cc < 8; ++cc) l += y[cc].y * ex2(y[cc].x - top);
-      stat[tid] = float2{top, 1.f / l};
+      stat[tid] = float2{top, kPart == kPrefix ? l : 1.f / l};
     }
   } else {   // a warp a row, a lane a piece
     for (int r = tid >> 5; r < p.rows_per; r += threads >> 5) {
@@ -384,7 +496,7 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
       }
 #pragma unroll
       for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
-      if (lane == 0) stat[r] = float2{top, 1.f / l};
+      if (lane == 0) stat[r] = float2{top, kPart == kPrefix ? l : 1.f / l};
     }
   }
   asm volatile("bar.sync 15, %0;" ::"r"(threads) : "memory");
@@ -408,6 +520,13 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
     for (int i = 0; i < kItems; ++i) {
       const int x = x0 + i * threads, r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
       if (x >= items || row / p.g >= live) continue;
+      if constexpr (kPart == kPrefix) {
+        if (query_at<kPart>(p, b, row / p.g, live) < 0) continue;
+        float* to = prior_of<D>(p, row_at(p, b, h, row));
+        __stcg(reinterpret_cast<float4*>(to + 4 + d), o[i]);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(to), stat[r]);
+        continue;
+      }
       const float inv = stat[r].y;
       store4(out_row<T>(p, b, h, row, D) + d, float4{o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv});
     }

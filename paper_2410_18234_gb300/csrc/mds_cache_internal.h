@@ -35,13 +35,15 @@ struct State {
   int32_t* kept;      // [MDS_CACHE_MAX_BATCH][2] workspace of commit: tokens kept behind the root, and how far they move
   uint32_t* arrive;   // [max_seqs] arrivals of commit's blocks, 0 between calls
   uint32_t* joins;    // [kJoins] arrivals of attend's pieces, 0 between calls
-  float* part;        // attend's partial sums
+  int2* share;        // [MDS_CACHE_MAX_BATCH] attend over prefixes: tokens shared with the group's first, live nodes
+  float* part;        // attend's partial sums; the second half: rows' sums over a prefix
   uint32_t* status;
   int layers, pages, page_tokens, page_log, kv_heads, head_dim, max_seqs, max_pages, dtype;
 };
 
 constexpr int kJoins = 1024;            // blocks of attend's grid at most
 constexpr size_t kPartFloats = 16u << 20;
+constexpr size_t kPieceFloats = kPartFloats / 2;   // of it, for pieces where sums over a prefix take the rest
 
 cudaError_t reserve(const State& s, const int32_t* seqs, const int32_t* counts, int n, int B, cudaStream_t st);
 cudaError_t append(const State& s, int layer, const int32_t* seqs, const int32_t* counts, const void* k,
@@ -82,10 +84,22 @@ struct Attend {
 };
 cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st);        // mds_cache_few.cu
 cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st);   // mds_cache_many.cu
+// Groups of `members` sequences of the list, over their common prefix and each
+// over its rest (mds_cache_shared.cu; the launches: _shared_few.cu, _shared_many.cu).
+cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms, cudaStream_t st);
+struct Shared {
+  int members, nodes;
+  bool prefix;     // the prefix's launch; else the rest's
+  float* prior;
+};
+cudaError_t shared_few(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
+cudaError_t shared_many(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
 cudaError_t configure_many();
+cudaError_t configure_shared_few();
+cudaError_t configure_shared_many();
 // Blocks of an attention kernel: one per SM, as far as the partial sums reach.
-inline int attend_grid(int sms, int rows, int head_dim) {
-  const size_t most = kPartFloats / (2 * (size_t)rows * (head_dim + 4));
+inline int attend_grid(int sms, int rows, int head_dim, size_t floats = kPartFloats) {
+  const size_t most = floats / (2 * (size_t)rows * (head_dim + 4));
   const int grid = sms < kJoins ? sms : kJoins;
   return (size_t)grid < most ? grid : (int)most;
 }
