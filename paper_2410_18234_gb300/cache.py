@@ -80,6 +80,8 @@ def _bind(lib):
 
 _lib = _bind(mds._lib)
 _I64x3 = ctypes.c_int64 * 3
+# the current stream's address without a stream object around it, where torch has CUDA
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _sizes(*given):
@@ -137,6 +139,7 @@ class Rotary:
         if len(self.freqs) != dim // 2:
             raise MdsError(MDS_ESHAPE, f"{len(self.freqs)} frequencies for {dim // 2} pairs")
         self.struct = RotaryStruct()
+        self._ref = ctypes.byref(self.struct)
         rc = _lib.mds_cache_rotary_init(ctypes.byref(self.struct), (ctypes.c_double * (dim // 2))(*self.freqs), dim,
                                         int(bool(interleaved)), float(magnitude))
         if rc != MDS_OK:
@@ -194,7 +197,7 @@ class Cache:
 
     def _stream(self, stream):
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return _raw_stream(self._index) if _raw_stream else torch.cuda.current_stream(self.device).cuda_stream
         return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
     def _ints(self, name, t, shape):
@@ -225,7 +228,8 @@ class Cache:
         st = t.stride()
         if st[3] != 1:
             raise MdsError(MDS_EINVAL, f"{name}: the last axis must be contiguous")
-        return _I64x3(*(st[i] if s[i] > 1 else 0 for i in range(3)))   # an axis of one has any stride
+        # an axis of one has any stride
+        return _I64x3(st[0] if s[0] > 1 else 0, st[1] if s[1] > 1 else 0, st[2] if s[2] > 1 else 0)
 
     def _outs(self, shape, stream, given, n=1):
         """`given`, checked, or new tensors, allocated on the stream that writes them."""
@@ -236,13 +240,14 @@ class Cache:
                 if t.dtype is not self.dtype or t.get_device() != self._index or not t.is_contiguous():
                     raise MdsError(MDS_EINVAL, f"out: contiguous {self.dtype} on {self.device}")
             return given
+        if stream is None:
+            return [torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(n)]
         if isinstance(stream, torch.cuda.Stream):
             with torch.cuda.stream(stream):
                 return tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(n))
         got = tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(n))
-        if stream is not None:
-            for t in got:
-                t.record_stream(torch.cuda.ExternalStream(int(stream), device=self.device))
+        for t in got:
+            t.record_stream(torch.cuda.ExternalStream(int(stream), device=self.device))
         return got
 
     def _apart(self, out, same, others=()):
@@ -290,7 +295,7 @@ class Cache:
         o, = self._outs(tuple(x.shape), stream, None if out is None else (out,))
         if out is not None and x.numel():
             self._apart(out, x)
-        rc = _lib.mds_cache_rotate(self.ctx, ids, self._ints("counts", counts, (B,)), ctypes.byref(rotary.struct),
+        rc = _lib.mds_cache_rotate(self.ctx, ids, self._ints("counts", counts, (B,)), rotary._ref,
                                    x.data_ptr(), xs, o.data_ptr(), x.shape[2], x.shape[1], branches, B,
                                    self._stream(stream))
         if rc != MDS_OK:
@@ -317,7 +322,7 @@ class Cache:
         elif out is not None:
             raise MdsError(MDS_EINVAL, "out without q")
         rc = _lib.mds_cache_append_rotated(self.ctx, layer, ids, self._ints("counts", counts, (B,)),
-                                           ctypes.byref(rotary.struct), k.data_ptr(), ks, v.data_ptr(), vs,
+                                           rotary._ref, k.data_ptr(), ks, v.data_ptr(), vs,
                                            None if q is None else q.data_ptr(), qs, None if q is None else o.data_ptr(),
                                            0 if q is None else q.shape[2], k.shape[1], branches, B,
                                            self._stream(stream))

@@ -119,15 +119,23 @@ struct Lane16<float> {
   __device__ __forceinline__ float at(int i) const { return v[i]; }
 };
 
+// The scale: the least e in [-117, 119] with max <= 448 * 2^e, from the
+// maximum's exponent x and mantissa m: 448 = 1.75 * 2^8, so e = x - 8 if
+// m <= 1.75, else x - 7.  Returns 2^e and sets inv to 2^-e.
+__device__ __forceinline__ float block_scale(unsigned bits, float* inv) {
+  int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = bits == 0 ? 0 : min(max(e, -117), 119);
+  *inv = __uint_as_float((unsigned)(127 - e) << 23);
+  return __uint_as_float((unsigned)(127 + e) << 23);
+}
+
 template <typename T, int U>
 struct Block {
   static constexpr int kPasses = U / 2;
   static constexpr int kRows = 32 / U;
   Lane16<T> v[kPasses];
 
-  // The scale: the least e in [-117, 119] with max <= 448 * 2^e, from the
-  // maximum's exponent x and mantissa m: 448 = 1.75 * 2^8, so e = x - 8 if
-  // m <= 1.75, else x - 7.  Lane-uniform.  Returns 2^e and sets inv to 2^-e.
+  // The block's scale; lane-uniform.
   __device__ __forceinline__ float scale(float* inv, bool* odd) {
     unsigned m = 0;
 #pragma unroll
@@ -140,40 +148,40 @@ struct Block {
       for (int i = 0; i < kPasses; ++i) m = max(m, v[i].template largest<true>());
       bits = __reduce_max_sync(kFull, m);
     }
-    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = bits == 0 ? 0 : min(max(e, -117), 119);
-    *inv = __uint_as_float((unsigned)(127 - e) << 23);
-    return __uint_as_float((unsigned)(127 + e) << 23);
+    return block_scale(bits, inv);
   }
 };
 
+__device__ __forceinline__ void decode4(unsigned w, float scale, float* v) {
+  unsigned lo, hi;
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+  const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  v[0] = a.x * scale, v[1] = a.y * scale, v[2] = b.x * scale, v[3] = b.y * scale;
+}
 __device__ __forceinline__ void decode16(const uint4& x, float scale, float* v) {
-  const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    unsigned lo, hi;
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi)
-        : "r"(w[i]));
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-    v[4 * i] = a.x * scale;
-    v[4 * i + 1] = a.y * scale;
-    v[4 * i + 2] = b.x * scale;
-    v[4 * i + 3] = b.y * scale;
-  }
+  decode4(x.x, scale, v);
+  decode4(x.y, scale, v + 4);
+  decode4(x.z, scale, v + 8);
+  decode4(x.w, scale, v + 12);
 }
 
+__device__ __forceinline__ unsigned encode4(float a, float b, float c, float d) {
+  unsigned w;
+  asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
+      "mov.b32 %0, {a, b};\n\t}"
+      : "=r"(w)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return w;
+}
 template <typename T>
 __device__ __forceinline__ uint4 encode16(const Lane16<T>& v, float inv) {
   unsigned w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
-        "mov.b32 %0, {a, b};\n\t}"
-        : "=r"(w[i])
-        : "f"(v.at(4 * i) * inv), "f"(v.at(4 * i + 1) * inv), "f"(v.at(4 * i + 2) * inv), "f"(v.at(4 * i + 3) * inv));
-  }
+  for (int i = 0; i < 4; ++i)
+    w[i] = encode4(v.at(4 * i) * inv, v.at(4 * i + 1) * inv, v.at(4 * i + 2) * inv, v.at(4 * i + 3) * inv);
   return uint4{w[0], w[1], w[2], w[3]};
 }
 

@@ -11,13 +11,15 @@
 // at position 2^20 as at 1.  Sine and cosine are Taylor sums on an eighth of a turn either way,
 // in pairs of floats for the terms that matter (2^-40 absolute).
 //
-// Rounding.  Queries take the leading floats and are rounded to their type
-// once.  A key is rounded to 8 bits behind the rotation, where an error of
-// 2^-24 would turn one number in half a million into its neighbour, a
-// sixteenth away: its products and sum are kept in two floats, and their sum
-// goes to one float by rounding to odd (of the two floats around it the one
-// whose last bit is set), which a second rounding cannot tell from the sum
-// itself.  What is stored is the quantiser's answer on the exact rotation.
+// Rounding.  Queries are rotated in 32 bits and rounded to their type once.  A
+// key is rounded to 8 bits behind the rotation, where an error of 2^-24 would
+// turn one number in half a million into its neighbour, a sixteenth away.  So
+// each is quantised as the two ends of its error's interval; where they differ
+// (a lane in some thousands, and the ties of position 0), it is computed again
+// with products and sum in two floats and angles to 2^-40, and the sum goes to
+// one float by rounding to odd (of the two floats around it the one whose last
+// bit is set), which a second rounding cannot tell from the sum itself.  What
+// is stored is the quantiser's answer on the exact rotation.
 #include <cfloat>
 
 #include "mds_cache_quant.cuh"
@@ -47,7 +49,8 @@ struct Call {
   T* out;
   longlong3 ks, vs, qs;
   int layer, n, L, chunks;     // chunks of 16 nodes a sequence
-  int q_heads, q_each, q_parts;   // heads a block turns; blocks for them
+  int q_heads, q_each;         // heads that a block turns
+  int kv_parts;                // blocks for the keys and values of a chunk
 };
 
 // ------------------------------------------------------- pairs of floats
@@ -99,6 +102,21 @@ __device__ __forceinline__ void turn_cos_sin(uint64_t f, float2& c, float2& s) {
   if (quarter & 2u) s = float2{-s.x, -s.y};
 }
 
+// The same in one float each, for what is rounded to its type once: an eighth
+// of a turn either way as a float is off by 2^-24 of itself, a sum by about
+// 1.5 * 2^-24 of its largest term.
+__device__ __forceinline__ void turn_cos_sin(uint64_t f, float& c, float& s) {
+  const unsigned quarter = (unsigned)((f + (1ull << 61)) >> 62) & 3u;
+  const int64_t r = (int64_t)(f - ((uint64_t)quarter << 62));
+  const float a = __ll2float_rn(r) * (float)(6.283185307179586476925286766559 / 18446744073709551616.0), z = a * a;
+  const float sine = fmaf(a * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), a);
+  const float cosine = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  c = quarter & 1u ? sine : cosine;
+  s = quarter & 1u ? cosine : sine;
+  if (quarter == 1u || quarter == 2u) c = -c;
+  if (quarter & 2u) s = -s;
+}
+
 // x c + y s to one float, rounded to odd.  A sum that is not finite stays as it
 // is: what rounding left of it is not a number.
 __device__ __forceinline__ float odd_sum(float x, float ch, float cl, float y, float sh, float sl) {
@@ -115,35 +133,70 @@ __device__ __forceinline__ float odd_sum(float x, float ch, float cl, float y, f
 // ----------------------------------------------------------- the lanes' part
 
 // U = head_dim / 16 lanes a row, two chunks of 8 dimensions a lane, chosen so
-// that a lane holds both parts of its pairs, 8 unit .. 8 unit + 7.
-template <int U>
+// that a lane holds both parts of its eight pairs and the lanes' chunks lie
+// next to one another: kI (interleaved) chunks u and u + U, pairs 4 u .. + 3
+// and 4 (u + U) .. + 3; else chunks u and u + dim / 16, pairs 8 u .. + 7.  The
+// pairs are taken in two quads: a quad's 8 numbers are two words of a block's
+// bytes, and `turns` says of each quad whether it is turned.
+template <int U, bool kI>
 struct Lane {
-  int first, second;   // chunks
-  bool turns;
-  __device__ __forceinline__ Lane(const Turns& t, int unit) {
+  int unit, first, second;   // chunks
+  bool turns[2];
+  __device__ __forceinline__ Lane(const Turns& t, int u) : unit(u) {
     const int half = t.dim >> 4;
-    turns = unit < half;
-    first = !t.interleaved && turns ? unit : 2 * unit;
-    second = !t.interleaved && turns ? unit + half : 2 * unit + 1;
+    if (kI) {
+      first = u, second = u + U;
+      turns[0] = u * 8 < t.dim, turns[1] = (u + U) * 8 < t.dim;
+    } else {
+      turns[0] = turns[1] = u < half;
+      first = u < half ? u : 2 * u;
+      second = u < half ? u + half : 2 * u + 1;
+    }
+  }
+  __device__ __forceinline__ int pair(int i) const { return kI ? 4 * (unit + (i >> 2) * U) + (i & 3) : 8 * unit + i; }
+};
+// Where pair p of a row stands in a table's row: what the lanes of a row read
+// together, a quad each, is contiguous.
+template <bool kI>
+__device__ __forceinline__ int place(int p, int pairs) {
+  return kI ? p : ((p >> 2) & 1) * (pairs >> 1) + (p >> 3) * 4 + (p & 3);
+}
+template <int U, bool kI>
+__device__ __forceinline__ float4 quad_of(const float* row, int unit, int q, int pairs) {
+  return *reinterpret_cast<const float4*>(row + unit * 4 + (q ? (kI ? 4 * U : pairs >> 1) : 0));
+}
+// The words (of four numbers) of quad q: its two halves' places in a lane's 16.
+template <bool kI>
+__device__ __forceinline__ constexpr int word_of(int q, int half) { return kI ? 2 * q + half : q + 2 * half; }
+
+// A lane's 16 numbers of a row as they are loaded.
+template <typename T>
+struct Raw {
+  static constexpr int kWords = (int)sizeof(T) * 4;
+  unsigned w[kWords];
+  __device__ __forceinline__ void load(const T* first, const T* second) {
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) {
+      const uint4 y = reinterpret_cast<const uint4*>(i < kWords / 8 ? first : second)[i % (kWords / 8)];
+      w[4 * i] = y.x, w[4 * i + 1] = y.y, w[4 * i + 2] = y.z, w[4 * i + 3] = y.w;
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  // numbers of quad q
+  template <bool kI>
+  __device__ __forceinline__ void quad(int q, float* x) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = at(word_of<kI>(q, i >> 2) * 4 + (i & 3));
   }
 };
 
-__device__ __forceinline__ void load8(float* x, const __nv_bfloat16* p) {
-  const uint4 y = *reinterpret_cast<const uint4*>(p);
-  const unsigned w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8(float* x, const float* p) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float4 y = reinterpret_cast<const float4*>(p)[i];
-    x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
-  }
-}
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   unsigned w[4];
 #pragma unroll
@@ -158,150 +211,242 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
   for (int i = 0; i < 2; ++i) reinterpret_cast<float4*>(p)[i] = float4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
 }
 
-// Where pair p of a row stands in a table's row of `pairs`: what the lanes of
-// a row read together, four pairs each, is contiguous.
-__device__ __forceinline__ int place(int p, int pairs) { return ((p >> 2) & 1) * (pairs >> 1) + (p >> 3) * 4 + (p & 3); }
-
-// A lane's eight pairs of one table.
-__device__ __forceinline__ void pairs8(float* x, const float* row, int unit, int pairs) {
-  const float4 a = *reinterpret_cast<const float4*>(row + unit * 4), b = *reinterpret_cast<const float4*>(row + (pairs >> 1) + unit * 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+// The largest magnitude of three; no number where one is none.
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
-// Element indices of pair i's two parts in a lane's 16 values.
-template <bool kInterleaved>
-__device__ __forceinline__ constexpr int part_a(int i) { return kInterleaved ? 2 * i : i; }
-template <bool kInterleaved>
-__device__ __forceinline__ constexpr int part_b(int i) { return kInterleaved ? 2 * i + 1 : i + 8; }
+// Pair i of a quad's numbers.
+template <bool kI>
+__device__ __forceinline__ constexpr int part_a(int i) { return kI ? 2 * i : i; }
+template <bool kI>
+__device__ __forceinline__ constexpr int part_b(int i) { return kI ? 2 * i + 1 : i + 4; }
 
-template <bool kInterleaved>
-__device__ __forceinline__ void turn_query(float* x, const float* c, const float* s) {
+template <bool kI>
+__device__ __forceinline__ void turn(float* x, const float4& cos4, const float4& sin4) {
+  const float c[4] = {cos4.x, cos4.y, cos4.z, cos4.w}, s[4] = {sin4.x, sin4.y, sin4.z, sin4.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float &a = x[part_a<kInterleaved>(i)], &b = x[part_b<kInterleaved>(i)];
+  for (int i = 0; i < 4; ++i) {
+    float &a = x[part_a<kI>(i)], &b = x[part_b<kI>(i)];
     const float y = fmaf(a, c[i], -(b * s[i]));
     b = fmaf(a, s[i], b * c[i]);
     a = y;
   }
 }
-template <bool kInterleaved>
-__device__ __forceinline__ void turn_key(float* x, const float* c, const float* cl, const float* s, const float* sl) {
+
+__device__ __forceinline__ int depth_of(int node, int L) { return node <= L ? max(node, 0) : (node - 1) % L + 1; }
+
+// ------------------------------------------------------------- exact blocks
+
+// A head's rows of a block as the exact path takes them, from memory again.
+template <typename T>
+struct Rows {
+  const T* src;             // row 0's numbers (of which rows [from, to) are there)
+  int64_t stride;
+  uint8_t* base;            // row 0's bytes
+  const Turns* t;
+  int from, to, position;   // position: of depth 0
+  int node0, L;             // row 0's node
+  bool key;
+};
+
+// The numbers of quad q of row r, turned to floats rounded to odd; 0 for what
+// is no number.  Whether any is not finite.
+template <typename T, int D, bool kI>
+__device__ bool exact_quad(const Rows<T>& w, const Lane<D / 16, kI>& at, int r, int q, float* x) {
 #pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int word = word_of<kI>(q, half), d = (word < 2 ? at.first : at.second) * 8 + (word & 1) * 4;
+    const T* from = w.src + r * w.stride + d;
+    for (int i = 0; i < 4; ++i) x[half * 4 + i] = (float)from[i];
+  }
+  if (w.key && at.turns[q]) {
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      float &a = x[part_a<kI>(i)], &b = x[part_b<kI>(i)];
+      float2 c, s;
+      turn_cos_sin(w.t->turn[at.pair(4 * q + i)] * (uint64_t)(w.position + depth_of(w.node0 + r, w.L)), c, s);
+      c = product(c, w.t->magnitude);
+      s = product(s, w.t->magnitude);
+      const float y = odd_sum(a, c.x, c.y, -b, s.x, s.y);
+      b = odd_sum(a, s.x, s.y, b, c.x, c.y);
+      a = y;
+    }
+  }
+  bool odd = false;
   for (int i = 0; i < 8; ++i) {
-    float &a = x[part_a<kInterleaved>(i)], &b = x[part_b<kInterleaved>(i)];
-    const float y = odd_sum(a, c[i], cl[i], -b, s[i], sl[i]);
-    b = odd_sum(a, s[i], sl[i], b, c[i], cl[i]);
-    a = y;
+    odd = odd || !(fabsf(x[i]) <= FLT_MAX);
+    x[i] = x[i] == x[i] ? x[i] : 0.f;
+  }
+  return odd;
+}
+// The bits of the largest finite magnitude of a lane's rows; the highest bit is
+// set where one is not finite.
+template <typename T, int D, bool kI>
+__device__ __noinline__ unsigned exact_largest(const Rows<T>& w, int lane) {
+  constexpr int U = D / 16;
+  const Lane<U, kI> at(*w.t, lane % U);
+  unsigned m = 0;
+  bool odd = false;
+#pragma unroll 1
+  for (int r = lane / U; r < w.to; r += 32 / U)
+#pragma unroll 1
+    for (int q = 0; q < 2; ++q) {
+      if (r < w.from) continue;
+      float x[8];
+      odd = exact_quad<T, D, kI>(w, at, r, q, x) || odd;
+      for (int i = 0; i < 8; ++i) {
+        const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu;
+        m = max(m, a >= kInf ? 0u : a);
+      }
+    }
+  return odd ? m | 0x80000000u : m;
+}
+// Store the quads of `mask` (bit 2 i + q of a lane's i-th row).
+template <typename T, int D, bool kI>
+__device__ __noinline__ void exact_store(const Rows<T>& w, int lane, unsigned mask, float inv) {
+  constexpr int U = D / 16;
+  const Lane<U, kI> at(*w.t, lane % U);
+#pragma unroll 1
+  for (; mask; mask &= mask - 1) {
+    const int bit = __ffs(mask) - 1, r = (bit >> 1) * (32 / U) + lane / U, q = bit & 1;
+    if (r < w.from || r >= w.to) continue;
+    float x[8];
+    exact_quad<T, D, kI>(w, at, r, q, x);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int word = word_of<kI>(q, half), d = (word < 2 ? at.first : at.second) * 8 + (word & 1) * 4;
+      *reinterpret_cast<unsigned*>(w.base + swizzled(r * D + d)) =
+          encode4(x[4 * half] * inv, x[4 * half + 1] * inv, x[4 * half + 2] * inv, x[4 * half + 3] * inv);
+    }
   }
 }
 
-// One block of threads takes 16 nodes of one sequence (kStore: the 16 slots of
-// a block of the cache), and some of its heads: it fills a table of their cosines and
-// sines once, and turns the heads by it.  With kStore the blocks behind those
-// of the queries take a key's or a value's head a warp, like append's.
-template <typename T, int D, bool kStore>
-__global__ void __launch_bounds__(kThreads, 2) rotary_kernel(const __grid_constant__ Call<T> p) {
-  constexpr int U = D / 16, P = D / 2;
-  __shared__ __align__(16) float table[kStore ? 4 : 2][16 * P];
+
+// Cosines and sines of rows [from, to) of the chunk whose first row is node
+// `node0`, by all the block's threads, a pair each.
+template <int P, bool kI>
+__device__ __forceinline__ void fill(float (*table)[16 * P], const Turns& t, int from, int to, int node0, int len, int L) {
+  const int i = threadIdx.x % P, pairs = t.dim >> 1;
+  if (i >= pairs) return;
+  const uint64_t turn = t.turn[i];
+  const int at = place<kI>(i, pairs);
+  for (int r = from + threadIdx.x / P; r < to; r += kThreads / P) {
+    float c, s;
+    turn_cos_sin(turn * (uint64_t)(len + depth_of(node0 + r, L)), c, s);
+    table[0][r * P + at] = c * t.magnitude.x, table[1][r * P + at] = s * t.magnitude.x;
+  }
+}
+
+// One block of threads takes 16 nodes of one sequence and some of its heads
+// (kStore: or the 16 slots of a block of the cache, a key's or a value's head a
+// warp, like append's; those blocks come first, as they take longest).  It
+// starts its loads, fills a table of the rows' cosines and sines while they
+// are under way, and turns the heads by it.
+template <typename T, int D, bool kStore, bool kI>
+__global__ void __launch_bounds__(kThreads, !kStore ? 4 : sizeof(T) * D <= 256 ? 3 : 2)
+    rotary_kernel(const __grid_constant__ Call<T> p) {
+  constexpr int U = D / 16, P = D / 2, kItems = sizeof(T) == 4 ? 1 : 2;
+  __shared__ __align__(16) float table[2][16 * P];
   const State& s = p.s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int b = (int)(blockIdx.x / p.chunks), j = (int)(blockIdx.x % p.chunks), part = blockIdx.y;
-  const bool stores = kStore && part >= p.q_parts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pairs = p.t.dim >> 1;
+  const int b = (int)(blockIdx.x / p.chunks), j = (int)(blockIdx.x % p.chunks);
   int id = p.seqs[b];
   if (id >= s.max_seqs) {
     if (tid == 0) atomicOr(s.status, MDS_ST_BADSEQ);
     id = -1;
   }
-  const int len = id >= 0 ? s.lens[id] : 0, asked = id >= 0 ? live_count(p.counts, b, p.n) : 0;
-  const int t0 = kStore ? (len / kBlock + j) * kBlock : len + j * kBlock;   // the chunk's first slot
-  if (t0 >= len + (stores ? asked : p.n)) return;
-  const int from = max(len - t0, 0), to = min(len + asked - t0, kBlock);    // its rows that turn
-  const int units0 = (part - p.q_parts) * (kThreads / 32);                  // keys' heads, then values'
-  const int pairs = p.t.dim >> 1;
-  if (!stores || units0 < s.kv_heads) {
-    for (int x = from * pairs + tid; x < to * pairs; x += kThreads) {
-      const int r = x / pairs, i = x - r * pairs, node = t0 + r - len;
-      const int depth = node > 0 ? (node - 1) % p.L + 1 : 0;
-      float2 c, sn;
-      turn_cos_sin(p.t.turn[i] * (uint64_t)(len + depth), c, sn);
-      c = product(c, p.t.magnitude);
-      sn = product(sn, p.t.magnitude);
-      const int at = r * P + place(i, pairs);
-      if constexpr (kStore) {
-        if (stores) {
-          c = quick_sum(c.x, c.y);
-          sn = quick_sum(sn.x, sn.y);
-          table[2][at] = c.y;
-          table[3][at] = sn.y;
-        }
-      }
-      table[0][at] = c.x;
-      table[1][at] = sn.x;
-    }
-    __syncthreads();
-  }
+  const int asked = id >= 0 ? live_count(p.counts, b, p.n) : 0;
+  const Lane<U, kI> at(p.t, tid % U);
 
-  if (!stores) {
-    // ---- queries: rows that are not live become zeros
-    const int h0 = part * p.q_each, heads = min(p.q_each, p.q_heads - h0);
-    const int end = min(len + p.n - t0, kBlock), unit = tid % U;
-    const Lane<U> at(p.t, unit);
-    const T* src = p.q + b * p.qs.x + h0 * p.qs.z;
-    T* dst = p.out + (((int64_t)b * p.n) * p.q_heads + h0) * D;
-#pragma unroll 2
-    for (int x = from * heads + tid / U; x < end * heads; x += kThreads / U) {
-      const int r = x / heads, h = x - r * heads;
-      const int64_t node = t0 + r - len;
-      float v[16];
-      if (r < to) {
-        const T* y = src + node * p.qs.y + h * p.qs.z;
-        load8(v, y + at.first * 8);
-        load8(v + 8, y + at.second * 8);
-        if (at.turns) {
-          float c[8], sn[8];
-          pairs8(c, table[0] + r * P, unit, pairs);
-          pairs8(sn, table[1] + r * P, unit, pairs);
-          if (p.t.interleaved) turn_query<true>(v, c, sn);
-          else turn_query<false>(v, c, sn);
-        }
-      } else {
+  if (!kStore || (int)blockIdx.y >= p.kv_parts) {
+    // ---- queries, a row a thread: rows that are not live become zeros
+    const int node0 = j * kBlock, end = min(p.n - node0, kBlock), to = min(asked - node0, end);
+    if (end <= 0) return;
+    const int h0 = ((int)blockIdx.y - p.kv_parts) * p.q_each, heads = min(p.q_each, p.q_heads - h0);
+    const int log = 32 - __clz(end - 1);   // of the rows, rounded up to a power of two
+    const int r = (tid / U) & ((1 << log) - 1), first = tid / U >> log, step = kThreads / U >> log;
+    const bool live = r < to;
+    const T* src = p.q + b * p.qs.x + (node0 + r) * p.qs.y + h0 * p.qs.z;
+    T* dst = p.out + (((int64_t)b * p.n + node0 + r) * p.q_heads + h0) * D;
+    Raw<T> raw[kItems];
+    auto load = [&](int g) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+      for (int i = 0; i < kItems; ++i) {
+        const int h = g + i * step;
+        if (live && h < heads) raw[i].load(src + h * p.qs.z + at.first * 8, src + h * p.qs.z + at.second * 8);
+        else raw[i].zero();
       }
-      T* o = dst + (node * p.q_heads + h) * D;
-      store8(o + at.first * 8, v);
-      store8(o + at.second * 8, v + 8);
+    };
+    load(first);
+    if (to > 0) fill<P, kI>(table, p.t, 0, to, node0, s.lens[id], p.L);
+    __syncthreads();
+    if (r >= end) return;
+    float4 c[2], sn[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      c[q] = float4{1.f, 1.f, 1.f, 1.f}, sn[q] = float4{0.f, 0.f, 0.f, 0.f};
+      if (at.turns[q] && live) {
+        c[q] = quad_of<U, kI>(table[0] + r * P, at.unit, q, pairs);
+        sn[q] = quad_of<U, kI>(table[1] + r * P, at.unit, q, pairs);
+      }
+    }
+    for (int g = first; g < heads; g += kItems * step) {
+      if (g != first) load(g);
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int h = g + i * step;
+        if (h >= heads) break;
+        float v[2][8];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          raw[i].template quad<kI>(q, v[q]);
+          if (at.turns[q]) turn<kI>(v[q], c[q], sn[q]);
+        }
+        float x[16];
+#pragma unroll
+        for (int y = 0; y < 16; ++y) x[word_of<kI>(y >> 3, (y >> 2) & 1) * 4 + (y & 3)] = v[y >> 3][y & 7];
+        store8(dst + h * D + at.first * 8, x);
+        store8(dst + h * D + at.second * 8, x + 8);
+      }
     }
     return;
   }
 
   if constexpr (kStore) {
     // ---- a head of keys or of values a warp: quantised with the tokens in front
-    const int u = units0 + warp, kv = u >= s.kv_heads, h = u - kv * s.kv_heads;
-    if (u >= 2 * s.kv_heads) return;
-    const int c = min(asked, s.reach[id] - len);
-    if (c < asked && lane == 0) atomicOr(s.status, MDS_ST_BADSEQ);
+    if (asked == 0) return;
+    const int len = s.lens[id], c = min(asked, s.reach[id] - len);
+    const int t0 = (len / kBlock + j) * kBlock, from = max(len - t0, 0), to = min(len + c - t0, kBlock);   // new rows
+    if (t0 >= len + asked) return;
+    if (c < asked && tid == 0) atomicOr(s.status, MDS_ST_BADSEQ);
     if (c == 0 || t0 >= len + c) return;
-    using Blk = Block<float, U>;
-    Blk blk;
-    const int row = lane / U, unit = lane % U;
-    const Lane<U> at(p.t, unit);
+    const int units0 = blockIdx.y * (kThreads / 32), u = units0 + warp;   // keys' heads, then values'
+    const bool mine = u < 2 * s.kv_heads;
+    const int kv = u >= s.kv_heads, h = u - kv * s.kv_heads;
+    constexpr int kPasses = U / 2, kRows = 32 / U;
+    const int row = lane / U;
+    const int page = s.table[(int64_t)id * s.max_pages + (t0 >> s.page_log)];
     const longlong3 st = kv ? p.vs : p.ks;
-    const T* src = (kv ? p.v : p.k) + b * st.x + h * st.z;
+    const T* src = (kv ? p.v : p.k) + b * st.x + h * st.z + (int64_t)(t0 - len) * st.y;
+    Raw<T> raw[kPasses];
+    if (mine) {
 #pragma unroll
-    for (int i = 0; i < Blk::kPasses; ++i) {
-      const int t = t0 + i * Blk::kRows + row;
-      float* v = blk.v[i].v;
-      if (t >= len && t < len + c) {
-        const T* y = src + (int64_t)(t - len) * st.y;
-        load8(v, y + at.first * 8);
-        load8(v + 8, y + at.second * 8);
-      } else {
-        blk.v[i].zero();
+      for (int i = 0; i < kPasses; ++i) {
+        const int r = i * kRows + row;
+        if (r >= from && r < to) raw[i].load(src + r * st.y + at.first * 8, src + r * st.y + at.second * 8);
+        else raw[i].zero();
       }
     }
-    const int page = s.table[(int64_t)id * s.max_pages + (t0 >> s.page_log)];
-    if (s.ref[page] > 1) {
+    const bool shared = s.ref[page] > 1;
+    if (units0 < s.kv_heads) {
+      fill<P, kI>(table, p.t, from, to, t0 - len, len, p.L);
+      __syncthreads();
+    }
+    if (!mine) return;
+    if (shared) {
       if (lane == 0) atomicOr(s.status, MDS_ST_BADSEQ);
       return;
     }
@@ -309,48 +454,116 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_kernel(const __grid_consta
     const int r0 = t0 & (s.page_tokens - 1);
     uint8_t* base = s.pool + tile * (s.page_tokens * D) + r0 * D;
     float* scale_at = s.scales + tile * (s.page_tokens / kBlock) + r0 / kBlock;
-    if (!kv && at.turns) {
-#pragma unroll
-      for (int i = 0; i < Blk::kPasses; ++i) {
-        const int r = i * Blk::kRows + row;
-        if (r >= from && t0 + r < len + c) {
-          float cs[8], cl[8], sn[8], sl[8];
-          pairs8(cs, table[0] + r * P, unit, pairs);
-          pairs8(sn, table[1] + r * P, unit, pairs);
-          pairs8(cl, table[2] + r * P, unit, pairs);
-          pairs8(sl, table[3] + r * P, unit, pairs);
-          if (p.t.interleaved) turn_key<true>(blk.v[i].v, cs, cl, sn, sl);
-          else turn_key<false>(blk.v[i].v, cs, cl, sn, sl);
-        }
-      }
-    }
     float was = 0.f;
     if (t0 < len) {
       was = *scale_at;
 #pragma unroll
-      for (int i = 0; i < Blk::kPasses; ++i) {
-        const int r = i * Blk::kRows + row;
-        if (r < from) {
+      for (int i = 0; i < kPasses; ++i) {
+        const int r = i * kRows + row;
+        if (r < from) {   // bytes in the place of new numbers
           const uint2 lo = *reinterpret_cast<const uint2*>(base + swizzled(r * D + at.first * 8));
           const uint2 hi = *reinterpret_cast<const uint2*>(base + swizzled(r * D + at.second * 8));
-          decode16(uint4{lo.x, lo.y, hi.x, hi.y}, was, blk.v[i].v);
+          raw[i].w[0] = lo.x, raw[i].w[1] = lo.y, raw[i].w[2] = hi.x, raw[i].w[3] = hi.y;
         }
       }
     }
-    float inv;
-    bool odd;
-    const float scale = blk.scale(&inv, &odd);
-    if (odd && lane == 0) atomicOr(s.status, MDS_ST_NONFINITE);
-    if (lane == 0) *scale_at = scale;
+    const Rows<T> rows{src, st.y, base, &p.t, from, to, len, t0 - len, p.L, !kv};
+    // Quad q of the lane's i-th row, from what was loaded: bytes of tokens in
+    // front, new numbers, turned or not.
+    auto numbers = [&](int i, int q, float* v, float* mag) {
+      const int r = i * kRows + row;
+      if (r < from) {
+        decode4(raw[i].w[word_of<kI>(q, 0)], was, v);
+        decode4(raw[i].w[word_of<kI>(q, 1)], was, v + 4);
+        return false;
+      }
+      raw[i].template quad<kI>(q, v);
+      if (kv || !at.turns[q] || r >= to) return false;
 #pragma unroll
-    for (int i = 0; i < Blk::kPasses; ++i) {
-      const int r = i * Blk::kRows + row, t = t0 + r;
-      if (t < len + c && (t >= len || scale != was)) {
-        const uint4 y = encode16(blk.v[i], inv);
-        *reinterpret_cast<uint2*>(base + swizzled(r * D + at.first * 8)) = uint2{y.x, y.y};
-        *reinterpret_cast<uint2*>(base + swizzled(r * D + at.second * 8)) = uint2{y.z, y.w};
+      for (int x = 0; x < 4; ++x) mag[x] = fabsf(v[part_a<kI>(x)]) + fabsf(v[part_b<kI>(x)]);
+      turn<kI>(v, quad_of<U, kI>(table[0] + r * P, at.unit, q, pairs), quad_of<U, kI>(table[1] + r * P, at.unit, q, pairs));
+      return true;
+    };
+    // The block's maximum and scale.  A turned number is off by less than
+    // 2^-21 of its pair's |a| + |b| (times the magnitude), of which the larger
+    // of the pair's two is at least half, so the maximum is off by less than
+    // 2^-20 of itself, 16 steps of a float: where those decide the scale, or it
+    // is not finite, the numbers are computed exactly.
+    auto step_of = [](unsigned bits) { return (bits + 0x1fffffu) >> 23; };   // goes up behind 1.75 * 2^x
+    float top[2] = {0.f, 0.f};   // of numbers that are as they are, and of turned ones
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      if (i * kRows >= to) break;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float v[8], mag[4];
+        const bool turned = numbers(i, q, v, mag);
+        float m = largest3(v[0], v[1], v[2]);
+        m = largest3(m, v[3], v[4]);
+        m = largest3(m, v[5], v[6]);
+        if (turned) top[1] = largest3(top[1], m, v[7]);
+        else top[0] = largest3(top[0], m, v[7]);
       }
     }
+    unsigned known = __reduce_max_sync(kFull, __float_as_uint(top[0]) & 0x7fffffffu);
+    const unsigned most = __reduce_max_sync(kFull, __float_as_uint(top[1]) & 0x7fffffffu);
+    bool exact = false;
+    if (max(known, most) >= kInf || step_of(max(known, most - min(most, 16u))) != step_of(max(known, most + 16u))) {
+      exact = true;
+      const unsigned m = exact_largest<T, D, kI>(rows, lane);
+      if (__any_sync(kFull, m >> 31) && lane == 0) atomicOr(s.status, MDS_ST_NONFINITE);
+      unsigned held = 0;   // tokens in front are finite
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        if (i * kRows + row >= from) break;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float v[8], mag[4];
+          numbers(i, q, v, mag);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) held = max(held, __float_as_uint(v[x]) & 0x7fffffffu);
+        }
+      }
+      known = __reduce_max_sync(kFull, max(held, m & 0x7fffffffu));
+    }
+    float inv;
+    const float scale = block_scale(exact ? known : max(known, most), &inv);
+    if (lane == 0) *scale_at = scale;
+    const float off = inv * p.t.magnitude.x * 0x1p-21f;
+    unsigned unsure = exact ? (1u << (2 * kPasses)) - 1u : 0u;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      if (i * kRows >= to) break;
+      const int r = i * kRows + row;
+      if (r < to && (r >= from || scale != was)) {
+        unsigned w[4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float v[8], mag[4];
+          unsigned &lo = w[word_of<kI>(q, 0)], &hi = w[word_of<kI>(q, 1)];
+          if (numbers(i, q, v, mag)) {
+            // either end of each number's error: the same but where a rounding border lies between
+            float x[8], y[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z) {
+              const float e = mag[kI ? z >> 1 : z & 3] * off;
+              x[z] = fmaf(v[z], inv, -e);
+              y[z] = fmaf(v[z], inv, e);
+            }
+            lo = encode4(x[0], x[1], x[2], x[3]);
+            hi = encode4(x[4], x[5], x[6], x[7]);
+            if (lo != encode4(y[0], y[1], y[2], y[3]) || hi != encode4(y[4], y[5], y[6], y[7])) unsure |= 1u << (2 * i + q);
+          } else {
+            lo = encode4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            hi = encode4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+          }
+        }
+        *reinterpret_cast<uint2*>(base + swizzled(r * D + at.first * 8)) = uint2{w[0], w[1]};
+        *reinterpret_cast<uint2*>(base + swizzled(r * D + at.second * 8)) = uint2{w[2], w[3]};
+      }
+    }
+    unsure = __reduce_or_sync(kFull, unsure);
+    if (unsure) exact_store<T, D, kI>(rows, lane, unsure, inv);
   }
 }
 
@@ -379,13 +592,15 @@ cudaError_t launch(const State& s, const Rotate& a, cudaStream_t st) {
   p.L = a.L > 0 ? a.L : 1;
   p.chunks = a.k ? (a.n + 2 * kBlock - 2) / kBlock : (a.n + kBlock - 1) / kBlock;
   p.q_heads = a.heads;
-  // about four items a thread
-  const int rows = a.n < kBlock ? a.n : kBlock, each = 4 * kThreads / (D / 16) / rows;
+  // heads for which a table is filled: eight times a thread's 16 numbers
+  const int rows = a.n < kBlock ? a.n : kBlock, each = 8 * kThreads / (D / 16) / rows;
   p.q_each = a.heads < each ? a.heads : each;
-  p.q_parts = a.q ? (a.heads + p.q_each - 1) / p.q_each : 0;
-  const dim3 grid(a.B * p.chunks, p.q_parts + (a.k ? (2 * s.kv_heads + 7) / 8 : 0));
-  if (a.k) rotary_kernel<T, D, true><<<grid, kThreads, 0, st>>>(p);
-  else rotary_kernel<T, D, false><<<grid, kThreads, 0, st>>>(p);
+  p.kv_parts = a.k ? (2 * s.kv_heads + 7) / 8 : 0;
+  const dim3 grid(a.B * p.chunks, p.kv_parts + (a.q ? (a.heads + p.q_each - 1) / p.q_each : 0));
+  if (a.k && p.t.interleaved) rotary_kernel<T, D, true, true><<<grid, kThreads, 0, st>>>(p);
+  else if (a.k) rotary_kernel<T, D, true, false><<<grid, kThreads, 0, st>>>(p);
+  else if (p.t.interleaved) rotary_kernel<T, D, false, true><<<grid, kThreads, 0, st>>>(p);
+  else rotary_kernel<T, D, false, false><<<grid, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 
