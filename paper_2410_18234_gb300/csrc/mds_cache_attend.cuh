@@ -42,6 +42,7 @@ constexpr int kTile = 128;                 // slots of a key tile
 constexpr float kNone = -FLT_MAX;          // reference of a row that has seen nothing: below every score
 constexpr float kSlack = 32.f;             // the reference moves when a weight passes 2^32
 constexpr unsigned kWaitTries = 1u << 18;
+constexpr int kRestExtra = 3;              // what a group costs beside its blocks, in blocks (mds_cache_rest.cu)
 
 enum Part { kAll, kPrefix, kRest };
 
@@ -267,29 +268,22 @@ __device__ __forceinline__ bool find(const State& s, const int32_t* seqs, const 
   return bad;
 }
 
-// What the live sequences of a group share: at the group's first place of
-// `least` the fewest tokens, and how many sequences there are.  (All threads.)
-__device__ __forceinline__ void common(const Params& p, int b, int* least, int* count) {
-  const int2 x = __ldg(p.s.share + b);
-  if (x.y <= 0) return;
-  atomicMin(least, x.x);
-  atomicAdd(count, 1);
-}
-
 // The plan, by all of the block's threads: seqs and the exclusive sums of
-// their tiles, and zeros in the rows of nodes that are not live.
-template <typename T, int kPart>
+// their tiles (kFine: of blocks of 16 slots, and kRestExtra), and zeros in the rows of nodes
+// that are not live.
+template <typename T, int kPart, bool kFine = false>
 __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int head_dim) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  // what a group's live sequences share is the least of what each shares with the first
   if constexpr (kPart == kPrefix) {
-    // q: the place of the group's first live sequence; len: what is shared;
-    // end: live sequences; live: nodes up to the last live sequence
+    // q: the place of the first live sequence; live: nodes up to the last one
     for (int g = tid; g < p.a.B; g += blockDim.x) seqs[g] = Seq<kPart>{INT_MAX, INT_MAX, 0, 0};
     __syncthreads();
     for (int b = tid; b < p.a.B * p.members; b += blockDim.x) {
+      const int2 x = __ldg(p.s.share + b);
       Seq<kPart>& q = seqs[b / p.members];
-      common(p, b, &q.len, &q.end);
-      if (__ldg(p.s.share + b).y > 0) {
+      if (x.y > 0) {
+        atomicMin(&q.len, x.x);
         atomicMin(&q.q, b);
         atomicMax(&q.live, (b % p.members + 1) * p.nodes);
       }
@@ -297,57 +291,80 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
     __syncthreads();
     for (int g = tid; g < p.a.B; g += blockDim.x) {
       const Seq<kPart> q = seqs[g];
-      const bool any = q.end > 1 && q.len > 0;
-      seqs[g] = any ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
+      seqs[g] = q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
     }
   } else {
     if constexpr (kPart == kRest) {
-      // a group's first place holds what is shared, and in q how many are live
-      for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = INT_MAX, seqs[b].q = 0;
-      __syncthreads();
-      for (int b = tid; b < p.a.B; b += blockDim.x) {
-        Seq<kPart>& first = seqs[b / p.members * p.members];
-        common(p, b, &first.from, &first.q);
-      }
-      __syncthreads();
-      for (int b = tid; b < p.a.B; b += blockDim.x) {
-        const Seq<kPart>& first = seqs[b / p.members * p.members];
-        if (b % p.members) seqs[b].from = first.q > 1 ? first.from : 0;
-      }
-      __syncthreads();
-      for (int b = tid; b < p.a.B; b += blockDim.x)
-        if (b % p.members == 0 && seqs[b].q < 2) seqs[b].from = 0;
+      for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = INT_MAX;
       __syncthreads();
     }
     for (int b = tid; b < p.a.B; b += blockDim.x) {
       Seq<kPart>& q = seqs[b];
+      int2 x{0, 0};
+      if constexpr (kPart == kRest) x = __ldg(p.s.share + b);
       int id, len, live, end;
       if (find(p.s, p.a.seqs, p.a.counts, b, p.a.n, &id, &len, &live, &end)) atomicOr(p.s.status, MDS_ST_BADSEQ);
       q.q = id, q.len = len, q.live = live, q.end = end;
+      if constexpr (kPart == kRest)
+        if (x.y > 0) atomicMin(&seqs[b / p.members * p.members].from, x.x);   // its first place has the group's
+    }
+    if constexpr (kPart == kRest) {
+      __syncthreads();
+      for (int b = tid; b < p.a.B; b += blockDim.x)
+        if (b % p.members) seqs[b].from = seqs[b / p.members * p.members].from;
     }
   }
   __syncthreads();
-  for (int b = warp; b < p.a.B; b += warps) {
-    const Seq<kPart> q = seqs[b];
-    long long t = 0;
-    const int tiles = min(p.row_tiles, (q.live * p.g + p.rows_per - 1) / p.rows_per);
-    for (int rt = lane; rt < tiles; rt += 32) t += group_of(p, q, rt).tiles;
-    for (int d = 16; d; d /= 2) t += __shfl_xor_sync(kFull, t, d);
-    if (lane == 0) prefix[b + 1] = t * p.s.kv_heads;
+  auto tiles_of = [&](const Seq<kPart>& q, int rt) {
+    const Group grp = group_of(p, q, rt);
+    return !kFine ? grp.tiles : grp.tiles ? (grp.hi - grp.lo + kBlock - 1) / kBlock + kRestExtra : 0;
+  };
+  // A thread a sequence where it has few row tiles, else a warp.
+  if (p.row_tiles <= 4) {
+    for (int b = tid; b < p.a.B; b += blockDim.x) {
+      const Seq<kPart> q = seqs[b];
+      long long t = 0;
+      for (int rt = 0; rt < p.row_tiles; ++rt) t += tiles_of(q, rt);
+      prefix[b + 1] = t * p.s.kv_heads;
+    }
+  } else {
+    for (int b = warp; b < p.a.B; b += warps) {
+      const Seq<kPart> q = seqs[b];
+      long long t = 0;
+      const int tiles = min(p.row_tiles, (q.live * p.g + p.rows_per - 1) / p.rows_per);
+      for (int rt = lane; rt < tiles; rt += 32) t += tiles_of(q, rt);
+      for (int d = 16; d; d /= 2) t += __shfl_xor_sync(kFull, t, d);
+      if (lane == 0) prefix[b + 1] = t * p.s.kv_heads;
+    }
   }
   __syncthreads();
-  if (warp == 0) {
-    long long run = 0;
-    if (lane == 0) prefix[0] = 0;
-    for (int b0 = 0; b0 < p.a.B; b0 += 32) {
-      const int b = b0 + lane;
-      long long x = b < p.a.B ? prefix[b + 1] : 0;
-      for (int d = 1; d < 32; d *= 2) {
-        const long long y = __shfl_up_sync(kFull, x, d);
-        if (lane >= d) x += y;
-      }
-      if (b < p.a.B) prefix[b + 1] = run + x;
-      run += __shfl_sync(kFull, x, 31);
+  // sums within 32 sequences by a warp, then a thread adds the 32s in front of its own
+  for (int b0 = warp * 32; b0 < p.a.B; b0 += warps * 32) {
+    const int b = b0 + lane;
+    long long x = b < p.a.B ? prefix[b + 1] : 0;
+    for (int d = 1; d < 32; d *= 2) {
+      const long long y = __shfl_up_sync(kFull, x, d);
+      if (lane >= d) x += y;
+    }
+    if (b < p.a.B) prefix[b + 1] = x;
+  }
+  if (tid == 0) prefix[0] = 0;
+  __syncthreads();
+  if (p.a.B > 32) {
+    constexpr int kMost = MDS_CACHE_MAX_BATCH / 256;   // sequences of a thread
+    long long in_front[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      const int b = tid + i * (int)blockDim.x;
+      in_front[i] = 0;
+      if (b < p.a.B)
+        for (int c = 32; c <= b; c += 32) in_front[i] += prefix[c];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      const int b = tid + i * (int)blockDim.x;
+      if (b < p.a.B) prefix[b + 1] += in_front[i];
     }
   }
   T* out = static_cast<T*>(p.a.out);

@@ -10,6 +10,7 @@ cudaError_t configure() {
   if (e == cudaSuccess) e = configure_many();
   if (e == cudaSuccess) e = configure_shared_few();
   if (e == cudaSuccess) e = configure_shared_many();
+  if (e == cudaSuccess) e = configure_rest();
   return e;
 }
 

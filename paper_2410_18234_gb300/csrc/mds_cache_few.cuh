@@ -85,6 +85,170 @@ struct Few {
   }
 };
 
+// Where a lane's parts of a block of 16 slots lie in its bytes.
+template <int D>
+struct Places {
+  unsigned k[2][D / 64], v[D / 32];
+  __device__ __forceinline__ explicit Places(int lane) {
+    const int gr = lane >> 2, tq = lane & 3;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) k[j][x] = swizzled((j * 8 + gr) * D + (tq + 4 * x) * 16);
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+      const int key = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * x + (lane >> 4);
+      v[x] = swizzled(key * D + chunk * 16);
+    }
+  }
+};
+
+// A warp's running references, normalisers and sums: of rows 2 (lane % 4) and
+// + 1 of each tile of 8.
+template <int D, int NT>
+struct Sums {
+  float ref[NT][2], sum[NT][2], acc[NT][D / 16][4];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        ref[m][x] = kNone;
+        sum[m][x] = 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) acc[m][x][z] = 0.f;
+    }
+  }
+};
+
+// One block of 16 slots from t0 on, its keys at kb and its values at vb
+// (shared memory), for a warp's rows.  query(i) is fragment i of the rows'
+// queries; node and own are the rows' nodes and their branches' first nodes.
+template <typename T, int D, int NT, typename Query>
+__device__ __forceinline__ void few_block(const Params& p, const char* kb, unsigned vb, float ks, float vs, const Places<D>& at,
+                                          Query query, const int (&node)[NT][2], const int (&own)[NT][2],
+                                          const float (&rc)[NT][2], int t0, int len, int hi, Sums<D, NT>& s) {
+  using F = Few<T, D, NT>;
+  const int gr = (threadIdx.x & 31) >> 2;
+  // scores: x[m][2 h + r] of slot t0 + gr + 8 h and row 2 tq + r; even and
+  // odd steps into sums of their own, for shorter chains of products
+  float sc[2][NT][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) sc[h][m][z] = 0.f;
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) {
+    const uint4 k0 = *reinterpret_cast<const uint4*>(kb + at.k[0][x]);
+    const uint4 k1 = *reinterpret_cast<const uint4*>(kb + at.k[1][x]);
+    const unsigned w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      unsigned a[4];
+      to_f16(w0[y], a[0], a[2]);
+      to_f16(w1[y], a[1], a[3]);
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int term = 0; term < F::kQ; ++term)
+          mma_f16(sc[y & 1][m], a, query((m * F::kQ + term) * F::kSteps + x * 4 + y));
+    }
+  }
+  // in log2 units, masked
+  const bool plain = t0 + kBlock <= len &&
+                     (p.a.window <= 0 || t0 + kBlock <= p.a.sinks || t0 > len + min(p.a.L, p.a.n - 1) - p.a.window);
+  float w[NT][4];
+  bool moves = false;
+#pragma unroll
+  for (int m = 0; m < NT; ++m)
+#pragma unroll
+    for (int z = 0; z < 4; ++z)   // rounded: the largest, as a reference, leaves nothing of itself
+      w[m][z] = __fmul_rn(sc[0][m][z] + sc[1][m][z], rc[m][z & 1] * ks);
+  if (!plain) {
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const int t = t0 + (z >> 1) * 8 + gr, at_node = t - len, i_row = node[m][z & 1], b0 = own[m][z & 1];
+        bool see = at_node <= i_row && (at_node <= 0 || at_node >= b0) && t < hi;
+        if (p.a.window > 0) {
+          const int pos = at_node <= 0 ? t : len + at_node - b0 + 1;
+          const int mine = len + (i_row > 0 ? i_row - b0 + 1 : 0);
+          see = see && (pos < p.a.sinks || pos > mine - p.a.window);
+        }
+        if (!see) w[m][z] = dev::kNegInf;
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < NT; ++m)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) moves |= fmaxf(w[m][r], w[m][2 + r]) > s.ref[m][r] + kSlack;
+  if (__any_sync(kFull, moves)) {
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+      float alpha[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float top = fmaxf(w[m][r], w[m][2 + r]);
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+        top = fmaxf(top, s.ref[m][r]);
+        alpha[r] = ex2(s.ref[m][r] - top);
+        s.ref[m][r] = top;
+        s.sum[m][r] *= alpha[r];
+      }
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) s.acc[m][x][z] *= alpha[z & 1];
+    }
+  }
+  // weights; the values' scale goes to the values
+  uint2 b[NT][F::kW];
+#pragma unroll
+  for (int m = 0; m < NT; ++m)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float w0 = ex2(w[m][2 * h] - s.ref[m][0]), w1 = ex2(w[m][2 * h + 1] - s.ref[m][1]);
+      if constexpr (F::kW > 1) s.sum[m][0] += w0, s.sum[m][1] += w1;
+#pragma unroll
+      for (int term = 0; term < F::kW; ++term) {
+        const unsigned pk = pack_bf16(w0, w1);
+        const float r0 = __uint_as_float(pk << 16), r1 = __uint_as_float(pk & 0xffff0000u);
+        if constexpr (F::kW == 1) s.sum[m][0] += r0, s.sum[m][1] += r1;
+        w0 -= r0;
+        w1 -= r1;
+        (h ? b[m][term].y : b[m][term].x) = transposed(pk);
+      }
+    }
+  unsigned rest;
+  const unsigned factor = value_factor(vs, rest);
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x) {
+    unsigned v[4];
+    ldmatrix_x4_trans(v, vb + at.v[x]);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      unsigned a[4];   // even and odd dimensions of 8 slots, then of the other 8
+      to_bf16(v[2 * y], factor, a[0], a[1]);
+      to_bf16(v[2 * y + 1], factor, a[2], a[3]);
+      if (rest != 0x3f803f80u) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z) times_rest(a[z], rest);
+      }
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int term = 0; term < F::kW; ++term) mma_bf16(s.acc[m][2 * x + y], a, b[m][term]);
+    }
+  }
+}
+
 template <typename T, int D, int NT, int kPart>
 __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(const __grid_constant__ Params p) {
   using F = Few<T, D, NT>;
@@ -199,16 +363,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
   // ---- consumers
   auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(F::kThreads) : "memory"); };
   const int gr = lane >> 2, tq = lane & 3, set = warp >> 3, blk = warp & 7;
-  unsigned k_at[2][D / 64], v_at[D / 32];
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int x = 0; x < D / 64; ++x) k_at[j][x] = swizzled((j * 8 + gr) * D + (tq + 4 * x) * 16);
-#pragma unroll
-  for (int x = 0; x < D / 32; ++x) {
-    const int key = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * x + (lane >> 4);
-    v_at[x] = swizzled(key * D + chunk * 16);
-  }
+  const Places<D> places(lane);
   int stage = 0, turn = 0;
   unsigned phase = 0;
   for (int n = 0;; ++n) {
@@ -267,21 +422,13 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         own[m][x] = i > 0 && p.a.L > 0 ? 1 + (i - 1) / p.a.L * p.a.L : 1;
       }
     consumers_sync();
-    float rc[NT][2], ref[NT][2], sum[NT][2], acc[NT][D / 16][4];
+    float rc[NT][2];
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        rc[m][x] = coef[m * 8 + tq * 2 + x];
-        ref[m][x] = kNone;
-        sum[m][x] = 0.f;
-      }
-#pragma unroll
-    for (int m = 0; m < NT; ++m)
-#pragma unroll
-      for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-        for (int z = 0; z < 4; ++z) acc[m][x][z] = 0.f;
+      for (int r = 0; r < 2; ++r) rc[m][r] = coef[m * 8 + tq * 2 + r];
+    Sums<D, NT> x;
+    x.clear();
 
     const Group grp = job.grp;
     const int off = job.off, end = off + job.cnt, len = job.len;
@@ -291,122 +438,8 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         wait(full + stage, phase, abort);
         if (block_seen(grp, t0)) {
           const char* kb = stage_mem + stage * F::kStageBytes + blk * kBlock * D;
-          const unsigned vb = smem_u32(kb + kTile * D);
-          const float ks = stage_scales[stage * 16 + blk], vs = stage_scales[stage * 16 + 8 + blk];
-          // scores: x[m][2 h + r] of slot t0 + gr + 8 h and row 2 tq + r; even and
-          // odd steps into sums of their own, for shorter chains of products
-          float sc[2][NT][4];
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-              for (int z = 0; z < 4; ++z) sc[h][m][z] = 0.f;
-#pragma unroll
-          for (int x = 0; x < D / 64; ++x) {
-            const uint4 k0 = *reinterpret_cast<const uint4*>(kb + k_at[0][x]);
-            const uint4 k1 = *reinterpret_cast<const uint4*>(kb + k_at[1][x]);
-            const unsigned w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              unsigned a[4];
-              to_f16(w0[y], a[0], a[2]);
-              to_f16(w1[y], a[1], a[3]);
-#pragma unroll
-              for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int term = 0; term < F::kQ; ++term)
-                  mma_f16(sc[y & 1][m], a, qf[((m * F::kQ + term) * F::kSteps + x * 4 + y) * 32 + lane]);
-            }
-          }
-          // in log2 units, masked
-          const bool plain = t0 + kBlock <= len &&
-                             (p.a.window <= 0 || t0 + kBlock <= p.a.sinks || t0 > len + min(p.a.L, p.a.n - 1) - p.a.window);
-          float w[NT][4];
-          bool moves = false;
-#pragma unroll
-          for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int z = 0; z < 4; ++z)   // rounded: the largest, as a reference, leaves nothing of itself
-              w[m][z] = __fmul_rn(sc[0][m][z] + sc[1][m][z], rc[m][z & 1] * ks);
-          if (!plain) {
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-              for (int z = 0; z < 4; ++z) {
-                const int t = t0 + (z >> 1) * 8 + gr, at_node = t - len, i_row = node[m][z & 1], b0 = own[m][z & 1];
-                bool see = at_node <= i_row && (at_node <= 0 || at_node >= b0) && t < grp.hi;
-                if (p.a.window > 0) {
-                  const int pos = at_node <= 0 ? t : len + at_node - b0 + 1;
-                  const int mine = len + (i_row > 0 ? i_row - b0 + 1 : 0);
-                  see = see && (pos < p.a.sinks || pos > mine - p.a.window);
-                }
-                if (!see) w[m][z] = dev::kNegInf;
-              }
-          }
-#pragma unroll
-          for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) moves |= fmaxf(w[m][r], w[m][2 + r]) > ref[m][r] + kSlack;
-          if (__any_sync(kFull, moves)) {
-#pragma unroll
-            for (int m = 0; m < NT; ++m) {
-              float alpha[2];
-#pragma unroll
-              for (int r = 0; r < 2; ++r) {
-                float top = fmaxf(w[m][r], w[m][2 + r]);
-#pragma unroll
-                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-                top = fmaxf(top, ref[m][r]);
-                alpha[r] = ex2(ref[m][r] - top);
-                ref[m][r] = top;
-                sum[m][r] *= alpha[r];
-              }
-#pragma unroll
-              for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) acc[m][x][z] *= alpha[z & 1];
-            }
-          }
-          // weights; the values' scale goes to the values
-          uint2 b[NT][F::kW];
-#pragma unroll
-          for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float w0 = ex2(w[m][2 * h] - ref[m][0]), w1 = ex2(w[m][2 * h + 1] - ref[m][1]);
-              if constexpr (F::kW > 1) sum[m][0] += w0, sum[m][1] += w1;
-#pragma unroll
-              for (int term = 0; term < F::kW; ++term) {
-                const unsigned pk = pack_bf16(w0, w1);
-                const float r0 = __uint_as_float(pk << 16), r1 = __uint_as_float(pk & 0xffff0000u);
-                if constexpr (F::kW == 1) sum[m][0] += r0, sum[m][1] += r1;
-                w0 -= r0;
-                w1 -= r1;
-                (h ? b[m][term].y : b[m][term].x) = transposed(pk);
-              }
-            }
-          unsigned rest;
-          const unsigned factor = value_factor(vs, rest);
-#pragma unroll
-          for (int x = 0; x < D / 32; ++x) {
-            unsigned v[4];
-            ldmatrix_x4_trans(v, vb + v_at[x]);
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              unsigned a[4];   // even and odd dimensions of 8 slots, then of the other 8
-              to_bf16(v[2 * y], factor, a[0], a[1]);
-              to_bf16(v[2 * y + 1], factor, a[2], a[3]);
-              if (rest != 0x3f803f80u) {
-#pragma unroll
-                for (int z = 0; z < 4; ++z) times_rest(a[z], rest);
-              }
-#pragma unroll
-              for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int term = 0; term < F::kW; ++term) mma_bf16(acc[m][2 * x + y], a, b[m][term]);
-            }
-          }
+          few_block<T, D, NT>(p, kb, smem_u32(kb + kTile * D), stage_scales[stage * 16 + blk], stage_scales[stage * 16 + 8 + blk],
+                              places, [&](int i) { return qf[i * 32 + lane]; }, node, own, rc, t0, len, grp.hi, x);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + stage);
@@ -419,10 +452,10 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
     for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        float l = sum[m][r];
+        float l = x.sum[m][r];
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l += __shfl_xor_sync(kFull, l, d);
-        if (gr == 0) ml[warp * F::kRows + m * 8 + tq * 2 + r] = float2{ref[m][r], l};
+        if (gr == 0) ml[warp * F::kRows + m * 8 + tq * 2 + r] = float2{x.ref[m][r], l};
       }
     consumers_sync();
     const bool whole = job.whole(), prior = kPart == kRest && grp.lo > 0;
@@ -435,7 +468,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         float top = kNone;
 #pragma unroll
         for (int wq = 0; wq < F::kWarps; ++wq) top = fmaxf(top, ml[wq * F::kRows + m * 8 + tq * 2 + r].x);
-        f[r] = ex2(ref[m][r] - top);
+        f[r] = ex2(x.ref[m][r] - top);
       }
 #pragma unroll
       for (int hd = 0; hd < D / 64; ++hd) {
@@ -447,11 +480,11 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
             for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
               for (int r = 0; r < 2; ++r) {
-                const float* ac = acc[m][hd * 4 + ch];
-                float2* at = reinterpret_cast<float2*>(join + (blk * 8 + tq * 2 + r) * kJoinStride + ch * 16 + gr * 2);
-                float2 x{ac[r] * f[r], ac[2 + r] * f[r]};
-                if (st < F::kSets - 1) x.x += at->x, x.y += at->y;
-                *at = x;
+                const float* ac = x.acc[m][hd * 4 + ch];
+                float2* to = reinterpret_cast<float2*>(join + (blk * 8 + tq * 2 + r) * kJoinStride + ch * 16 + gr * 2);
+                float2 y{ac[r] * f[r], ac[2 + r] * f[r]};
+                if (st < F::kSets - 1) y.x += to->x, y.y += to->y;
+                *to = y;
               }
           }
           consumers_sync();

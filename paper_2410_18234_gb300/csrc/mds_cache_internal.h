@@ -94,6 +94,8 @@ struct Shared {
 };
 cudaError_t shared_few(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
 cudaError_t shared_many(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
+cudaError_t shared_rest(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);   // mds_cache_rest.cu
+cudaError_t configure_rest();
 cudaError_t configure_many();
 cudaError_t configure_shared_few();
 cudaError_t configure_shared_many();

@@ -13,17 +13,18 @@ namespace cache {
 namespace {
 
 // One block of threads a sequence: the tokens that it shares with the first
-// live sequence of its group, and its live nodes.
+// live sequence of its group (none if it is the only one), and its live nodes.
 __global__ void __launch_bounds__(256) share_kernel(const State s, const int32_t* seqs, const int32_t* counts, int n,
                                                     int members) {
-  __shared__ int first_s, differ_s;
+  __shared__ int first_s, differ_s, others_s;
   const int tid = threadIdx.x, b = blockIdx.x, g0 = b / members * members;
-  if (tid == 0) first_s = INT_MAX, differ_s = INT_MAX;
+  if (tid == 0) first_s = INT_MAX, differ_s = INT_MAX, others_s = 0;
   __syncthreads();
   int id, len, live, end, q0, len0, live0;
-  for (int i = g0 + tid; i <= b; i += 256) {
+  for (int i = g0 + tid; i < g0 + members; i += 256) {
     find(s, seqs, counts, i, n, &q0, &len0, &live0, &end);
     if (live0 > 0) atomicMin(&first_s, i);
+    if (live0 > 0 && i != b) others_s = 1;
   }
   find(s, seqs, counts, b, n, &id, &len, &live, &end);
   __syncthreads();
@@ -37,7 +38,7 @@ __global__ void __launch_bounds__(256) share_kernel(const State s, const int32_t
     atomicMin(&differ_s, differ);
   }
   __syncthreads();
-  if (tid == 0) s.share[b] = live > 0 ? int2{(differ_s << s.page_log) & -kTile, live} : int2{INT_MAX, 0};
+  if (tid == 0) s.share[b] = live <= 0 ? int2{INT_MAX, 0} : others_s ? int2{(differ_s << s.page_log) & -kTile, live} : int2{0, live};
 }
 
 }  // namespace
@@ -68,7 +69,9 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms,
       e = s.dtype != MDS_F32 && (int64_t)y.n * g > 16 ? shared_many(s, y, z, sms, st) : shared_few(s, y, z, sms, st);
     z.prefix = false;
     if (e == cudaSuccess)
-      e = s.dtype != MDS_F32 && (int64_t)a.n * g > 16 ? shared_many(s, x, z, sms, st) : shared_few(s, x, z, sms, st);
+      e = s.dtype == MDS_F32 ? shared_few(s, x, z, sms, st)
+          : (int64_t)a.n * g <= 8 ? shared_rest(s, x, z, sms, st)
+          : (int64_t)a.n * g <= 16 ? shared_few(s, x, z, sms, st) : shared_many(s, x, z, sms, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

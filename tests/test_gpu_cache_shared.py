@@ -176,6 +176,22 @@ def test_wide_groups(G):
         check(c, m, rng, list(range(G)), G, 8, K, L, only=some)
 
 
+@pytest.mark.parametrize("D,H,Hq", [(128, 2, 8), (64, 5, 5), (64, 1, 7)])
+def test_long_rests(D, H, Hq):
+    """Rests of one block to thousands of slots: cut within a block of threads,
+    between two, and over many."""
+    rng = np.random.default_rng(D + H)
+    c, m = both(700, H, D, 8, 200, 64)
+    grow(c, m, rng, [0, 4], [200, 140])
+    fork(c, m, [0, 0, 0, 4, 4, 4], [1, 2, 3, 5, 6, 7])
+    grow(c, m, rng, list(range(8)), [9000, 0, 3001, 15, 4000, 1, 700, 64])
+    for K, L in [(1, 0), (1, 1), (2, 2)]:
+        if (1 + K * L) * (Hq // H) <= 8:
+            check(c, m, rng, list(range(8)), 4, Hq, K, L)
+    check(c, m, rng, [3, 1, 7, 5], 2, Hq, 1, 0)
+    check(c, m, rng, [0, 2], 2, Hq, 1, 0)
+
+
 @pytest.mark.parametrize("factor,scale", [(1e4, None), (1e-4, None), (1.5, -0.125), (1.5, 0.0), (3e4, -1.0)])
 def test_scores_of_any_size(factor, scale):
     """One side may hold all of a row's weight."""
