@@ -20,7 +20,8 @@ FLAGS = ["-cudart", "static", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-
 SOURCES = ["mds_kernel.cu", "mds_flow.cu", "mds_topk.cu", "mds_api.cu", "mds_noalloc.cu",
            "mds_cache_api.cu", "mds_cache_pages.cu", "mds_cache_rotary.cu",
            "mds_cache_few.cu", "mds_cache_many.cu",
-           "mds_cache_shared.cu", "mds_cache_shared_few.cu", "mds_cache_shared_many.cu", "mds_cache_rest.cu"]
+           "mds_cache_shared.cu", "mds_cache_shared_few.cu", "mds_cache_shared_many.cu", "mds_cache_rest.cu",
+           "mds_cache_wide.cu"]
 
 
 def nvcc():

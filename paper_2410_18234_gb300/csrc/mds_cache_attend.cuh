@@ -13,7 +13,9 @@
 // Parts.  A call is one launch (kAll), or two where sequences share a prefix:
 // kPrefix takes every group of sequences as one of `members` times as many
 // nodes over the prefix's tiles, and leaves each row's reference, normaliser
-// and sums in `prior`; kRest takes the sequences over the tiles behind it, and
+// and sums in `prior`, or in pieces that a launch of its own joins (a few
+// groups may be cut into many pieces, which one block each would be long
+// over); kRest takes the sequences over the tiles behind it, and
 // joins what it finds there like one more piece.
 #pragma once
 #include <cuda_bf16.h>
@@ -376,55 +378,7 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
   __syncthreads();
 }
 
-// ------------------------------------------------------------- the schedule
-//
-// One warp walks the block's part of the line and publishes its groups, kJobs
-// ahead: the divisions and searches stay out of the other warps' code and
-// registers.
-
-constexpr int kJobs = 4;
-
-// A group, or the block's piece of one, as the scheduler publishes it.
-struct Job {
-  int b, h, row0, off, cnt, tiles;             // cnt 0: the end
-  int q, len, live;                            // of the sequence
-  int first_block, last_block;                 // blocks of the grid that hold the group
-  Group grp;
-  __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
-};
-
-// The scheduler warp: c is the place of unit u0.
-template <int kPart>
-__device__ __forceinline__ void schedule(const Params& p, const Seq<kPart>* seqs, Cursor c, long long per, long long u0,
-                                         long long u1, Job* jobs, uint64_t* ready, uint64_t* taken, int* abort) {
-  const int lane = threadIdx.x & 31;
-  Group grp = group_of(p, seqs[c.b], c.rt);
-  long long u = u0;
-  for (int n = 0;; ++n) {
-    const int slot = n & (kJobs - 1);
-    wait(taken + slot, ((n / kJobs) & 1) ^ 1, abort);
-    const int cnt = u < u1 ? (int)min((long long)(grp.tiles - c.off), u1 - u) : 0;
-    if (lane == 0) {
-      Job& j = jobs[slot];
-      j.cnt = cnt;
-      if (cnt) {
-        const Seq<kPart> q = seqs[c.b];
-        j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
-        j.q = q.q, j.len = q.len, j.live = q.live;
-        j.first_block = (int)((u - c.off) / per);
-        j.last_block = (int)((u - c.off + grp.tiles - 1) / per);
-        j.grp = grp;
-      }
-      mbar_arrive(ready + slot);
-    }
-    __syncwarp();
-    if (!cnt) break;
-    u += cnt;
-    if (u < u1) advance(p, seqs, c, grp);
-  }
-}
-
-// ---------------------------------------------------------- joining pieces
+// ------------------------------------------------------- rows and pieces
 //
 // A piece's partial sums: per row its reference, its normaliser, two unused
 // places, and D sums.  A block has two: of the group that it continues, and of
@@ -466,13 +420,65 @@ __device__ __forceinline__ T* out_row(const Params& p, int b, int h, int row, in
   return static_cast<T*>(p.a.out) + row_at(p, b, h, row) * head_dim;
 }
 
+// ------------------------------------------------------------- the schedule
+//
+// One warp walks the block's part of the line and publishes its groups, kJobs
+// ahead: the divisions and searches stay out of the other warps' code and
+// registers.
+
+constexpr int kJobs = 4;
+
+// A group, or the block's piece of one, as the scheduler publishes it.
+struct Job {
+  int b, h, row0, off, cnt, tiles;             // cnt 0: the end
+  int q, len, live;                            // of the sequence
+  int first_block, last_block;                 // blocks of the grid that hold the group
+  Group grp;
+  __device__ __forceinline__ bool whole() const { return off == 0 && cnt == tiles; }
+};
+
+// The scheduler warp: c is the place of unit u0.
+template <int D, int kPart>
+__device__ __forceinline__ void schedule(const Params& p, const Seq<kPart>* seqs, Cursor c, long long per, long long u0,
+                                         long long u1, Job* jobs, uint64_t* ready, uint64_t* taken, int* abort) {
+  const int lane = threadIdx.x & 31;
+  Group grp = group_of(p, seqs[c.b], c.rt);
+  long long u = u0;
+  for (int n = 0;; ++n) {
+    const int slot = n & (kJobs - 1);
+    wait(taken + slot, ((n / kJobs) & 1) ^ 1, abort);
+    const int cnt = u < u1 ? (int)min((long long)(grp.tiles - c.off), u1 - u) : 0;
+    if (lane == 0) {
+      Job& j = jobs[slot];
+      j.cnt = cnt;
+      if (cnt) {
+        const Seq<kPart> q = seqs[c.b];
+        j.b = c.b, j.h = c.h, j.row0 = c.rt * p.rows_per, j.off = c.off, j.tiles = grp.tiles;
+        j.q = q.q, j.len = q.len, j.live = q.live;
+        j.first_block = (int)((u - c.off) / per);
+        j.last_block = (int)((u - c.off + grp.tiles - 1) / per);
+        j.grp = grp;
+        // a cut prefix's blocks, for the launch that joins them
+        if (kPart == kPrefix && c.off == 0 && cnt < grp.tiles)
+          *reinterpret_cast<int2*>(prior_of<D>(p, row_at(p, c.b, c.h, j.row0)) + 2) = int2{j.first_block, j.last_block};
+      }
+      mbar_arrive(ready + slot);
+    }
+    __syncwarp();
+    if (!cnt) break;
+    u += cnt;
+    if (u < u1) advance(p, seqs, c, grp);
+  }
+}
+
+// ---------------------------------------------------------- joining pieces
+
 // Add the pieces that blocks c0..c1 left of a row tile, in their order.  First
 // the rows' references and normalisers (into `stat`, shared memory of
 // rows_per), then the dimensions, four a thread, kItems such and kAhead pieces
 // at a time: a join is a wait for memory at the end of a block, so loads are
-// issued together (many rows have few pieces, few rows many).  kPrefix: the
-// sums go to `prior` as they are; kRest with `prior`: what is there is the
-// last piece.
+// issued together (many rows have few pieces, few rows many).  kRest with
+// `prior`: what is there is the last piece.
 template <typename T, int D, int kItems, int kAhead, int kPart>
 __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, int c0, int c1, bool prior, float2* stat,
                             int tid, int threads) {
@@ -499,7 +505,7 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
       for (int cc = 0; cc < 8; ++cc) top = fmaxf(top, y[cc].x);
 #pragma unroll
       for (int cc = 0; cc < 8; ++cc) l += y[cc].y * ex2(y[cc].x - top);
-      stat[tid] = float2{top, kPart == kPrefix ? l : 1.f / l};
+      stat[tid] = float2{top, 1.f / l};
     }
   } else {   // a warp a row, a lane a piece
     for (int r = tid >> 5; r < p.rows_per; r += threads >> 5) {
@@ -513,7 +519,7 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
       }
 #pragma unroll
       for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
-      if (lane == 0) stat[r] = float2{top, kPart == kPrefix ? l : 1.f / l};
+      if (lane == 0) stat[r] = float2{top, 1.f / l};
     }
   }
   asm volatile("bar.sync 15, %0;" ::"r"(threads) : "memory");
@@ -537,13 +543,6 @@ __device__ void join_pieces(const Params& p, int b, int h, int row0, int live, i
     for (int i = 0; i < kItems; ++i) {
       const int x = x0 + i * threads, r = x / (D / 4), d = x % (D / 4) * 4, row = row0 + r;
       if (x >= items || row / p.g >= live) continue;
-      if constexpr (kPart == kPrefix) {
-        if (query_at<kPart>(p, b, row / p.g, live) < 0) continue;
-        float* to = prior_of<D>(p, row_at(p, b, h, row));
-        __stcg(reinterpret_cast<float4*>(to + 4 + d), o[i]);
-        if (d == 0) __stcg(reinterpret_cast<float2*>(to), stat[r]);
-        continue;
-      }
       const float inv = stat[r].y;
       store4(out_row<T>(p, b, h, row, D) + d, float4{o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv});
     }

@@ -11,6 +11,7 @@ cudaError_t configure() {
   if (e == cudaSuccess) e = configure_shared_few();
   if (e == cudaSuccess) e = configure_shared_many();
   if (e == cudaSuccess) e = configure_rest();
+  if (e == cudaSuccess) e = configure_wide();
   return e;
 }
 

@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
   if (u0 >= u1) return;
 
   if (warp == F::kWarps + 1) {
-    schedule(p, seqs, locate(p, prefix, seqs, u0), per, u0, u1, jobs, ready, taken, abort);
+    schedule<D>(p, seqs, locate(p, prefix, seqs, u0), per, u0, u1, jobs, ready, taken, abort);
     return;
   }
   auto job_at = [&](int n) -> const Job& {
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         consumers_sync();
       }
     }
-    if (!whole) {
+    if (!whole && kPart != kPrefix) {
       // the last piece of the group to arrive adds them all, in order
       __threadfence();
       consumers_sync();

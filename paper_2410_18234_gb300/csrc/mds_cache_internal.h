@@ -36,14 +36,14 @@ struct State {
   uint32_t* arrive;   // [max_seqs] arrivals of commit's blocks, 0 between calls
   uint32_t* joins;    // [kJoins] arrivals of attend's pieces, 0 between calls
   int2* share;        // [MDS_CACHE_MAX_BATCH] attend over prefixes: tokens shared with the group's first, live nodes
-  float* part;        // attend's partial sums; the second half: rows' sums over a prefix
+  float* part;        // attend's partial sums; from kPieceFloats on rows' sums over a prefix
   uint32_t* status;
   int layers, pages, page_tokens, page_log, kv_heads, head_dim, max_seqs, max_pages, dtype;
 };
 
 constexpr int kJoins = 1024;            // blocks of attend's grid at most
 constexpr size_t kPartFloats = 16u << 20;
-constexpr size_t kPieceFloats = kPartFloats / 2;   // of it, for pieces where sums over a prefix take the rest
+constexpr size_t kPieceFloats = kPartFloats / 8 * 5;   // of it, for pieces where sums over a prefix take the rest
 
 cudaError_t reserve(const State& s, const int32_t* seqs, const int32_t* counts, int n, int B, cudaStream_t st);
 cudaError_t append(const State& s, int layer, const int32_t* seqs, const int32_t* counts, const void* k,
@@ -92,10 +92,18 @@ struct Shared {
   bool prefix;     // the prefix's launch; else the rest's
   float* prior;
 };
+// Rows of a tile of rows in the prefix's launch, by the kernel that it is.
+inline int even_rows(int64_t rows, int most) {   // as even as it goes
+  const int64_t tiles = (rows + most - 1) / most;
+  return (int)((rows + tiles - 1) / tiles);
+}
+constexpr int kFewRows = 16, kManyRows = 144, kWideRows = 256;
 cudaError_t shared_few(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
 cudaError_t shared_many(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);
 cudaError_t shared_rest(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);   // mds_cache_rest.cu
 cudaError_t configure_rest();
+cudaError_t shared_wide(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st);   // mds_cache_wide.cu
+cudaError_t configure_wide();
 cudaError_t configure_many();
 cudaError_t configure_shared_few();
 cudaError_t configure_shared_many();

@@ -1,6 +1,7 @@
 // Attention for sequences that share a prefix: what is shared is found from
 // the page tables, the prefix is attended to once for all of a group's rows,
-// then every sequence attends to its own tokens and joins the two.
+// its pieces are joined, then every sequence attends to its own tokens and
+// joins the two.
 //
 // Pages that several sequences hold are the same memory at the same slots, so
 // a prefix is the page indices at which the tables of all of a group's live
@@ -12,12 +13,21 @@ namespace cache {
 
 namespace {
 
+constexpr int kNarrow = 48;
+
 // One block of threads a sequence: the tokens that it shares with the first
 // live sequence of its group (none if it is the only one), and its live nodes.
-__global__ void __launch_bounds__(256) share_kernel(const State s, const int32_t* seqs, const int32_t* counts, int n,
-                                                    int members) {
+// A group's first block marks its tiles of rows as not cut.
+template <int D>
+__global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Params p) {
+  const State& s = p.s;
+  const int32_t *seqs = p.a.seqs, *counts = p.a.counts;
+  const int n = p.nodes, members = p.members;
   __shared__ int first_s, differ_s, others_s;
   const int tid = threadIdx.x, b = blockIdx.x, g0 = b / members * members;
+  if (b == g0)
+    for (int x = tid; x < s.kv_heads * p.row_tiles; x += 256)
+      *reinterpret_cast<int2*>(prior_of<D>(p, row_at(p, b / members, x / p.row_tiles, x % p.row_tiles * p.rows_per)) + 2) = int2{-1, -1};
   if (tid == 0) first_s = INT_MAX, differ_s = INT_MAX, others_s = 0;
   __syncthreads();
   int id, len, live, end, q0, len0, live0;
@@ -41,6 +51,51 @@ __global__ void __launch_bounds__(256) share_kernel(const State s, const int32_t
   if (tid == 0) s.share[b] = live <= 0 ? int2{INT_MAX, 0} : others_s ? int2{(differ_s << s.page_log) & -kTile, live} : int2{0, live};
 }
 
+// A row a warp: the pieces of its tile of rows, where that was cut, in their order.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params p) {
+  constexpr int R = kPieceRow<D>, kEach = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int per = (p.rows_per + 7) / 8, r = blockIdx.x % per * 8 + (threadIdx.x >> 5);
+  const int rt = blockIdx.x / per % p.row_tiles, h = blockIdx.x / per / p.row_tiles % p.s.kv_heads;
+  const int b = blockIdx.x / per / p.row_tiles / p.s.kv_heads, row = rt * p.rows_per + r;
+  if (r >= p.rows_per || row >= p.rows) return;
+  const int2 cut = *reinterpret_cast<const int2*>(prior_of<D>(p, row_at(p, b, h, rt * p.rows_per)) + 2);
+  if (cut.x < 0 || query_at<kPrefix>(p, b, row / p.g, p.a.n) < 0) return;
+  const int64_t stride = 2 * (int64_t)p.rows_per * R;
+  const float* first = piece_of<D>(p, cut.x, true) + r * R;
+  const float* later = piece_of<D>(p, cut.x, false) + r * R;   // + stride for each block further
+  const int pieces = cut.y - cut.x + 1;
+  auto at = [&](int c) { return c ? later + c * stride : first; };
+  float top = kNone;
+  for (int c = lane; c < pieces; c += 32) top = fmaxf(top, __ldcg(at(c)));
+#pragma unroll
+  for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+  float l = 0.f, o[kEach] = {};
+  for (int c0 = 0; c0 < pieces; c0 += 32) {
+    float2 y{kNone, 0.f};
+    if (c0 + lane < pieces) y = __ldcg(reinterpret_cast<const float2*>(at(c0 + lane)));
+    const float mine = ex2(y.x - top);
+    l += y.y * mine;
+#pragma unroll 8
+    for (int c = c0; c < min(c0 + 32, pieces); ++c) {
+      const float f = __shfl_sync(kFull, mine, c - c0);
+      const float* x = at(c) + 4 + lane * kEach;
+#pragma unroll
+      for (int i = 0; i < kEach; i += 2) {
+        const float2 z = __ldcg(reinterpret_cast<const float2*>(x + i));
+        o[i] += f * z.x, o[i + 1] += f * z.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d; d /= 2) l += __shfl_xor_sync(kFull, l, d);
+  float* to = prior_of<D>(p, row_at(p, b, h, row));
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) __stcg(reinterpret_cast<float2*>(to + 4 + lane * kEach + i), float2{o[i], o[i + 1]});
+  if (lane == 0) __stcg(reinterpret_cast<float2*>(to), float2{top, l});
+}
+
 }  // namespace
 
 cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms, cudaStream_t st) {
@@ -58,15 +113,31 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms,
     x.counts = a.counts ? a.counts + b0 : nullptr;
     x.q = static_cast<const char*>(a.q) + b0 * a.q_seq * es;
     x.out = static_cast<char*>(a.out) + (int64_t)b0 * a.n * a.heads * s.head_dim * es;
-    share_kernel<<<x.B, 256, 0, st>>>(s, x.seqs, x.counts, a.n, members);
-    cudaError_t e = cudaGetLastError();
     Attend y = x;
     y.B = some;
     y.n = a.n * members;
     y.L = y.n - 1;
     Shared z{members, a.n, true, s.part + kPieceFloats};
+    const int64_t rows = (int64_t)y.n * g;
+    const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
+    Params p{s, y, 0, g, (int)rows, 0, 0, 0};
+    // as the launch of the prefix cuts them
+    p.rows_per = few ? (rows > 8 ? 16 : 8) : even_rows(rows, many ? kManyRows : kWideRows);
+    p.row_tiles = (int)((rows + p.rows_per - 1) / p.rows_per);
+    p.members = members;
+    p.nodes = a.n;
+    p.prior = z.prior;
+    if (s.head_dim == 64) share_kernel<64><<<x.B, 256, 0, st>>>(p);
+    else share_kernel<128><<<x.B, 256, 0, st>>>(p);
+    cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess)
-      e = s.dtype != MDS_F32 && (int64_t)y.n * g > 16 ? shared_many(s, y, z, sms, st) : shared_few(s, y, z, sms, st);
+      e = few ? shared_few(s, y, z, sms, st) : many ? shared_many(s, y, z, sms, st) : shared_wide(s, y, z, sms, st);
+    if (e == cudaSuccess) {
+      const int blocks = some * s.kv_heads * p.row_tiles * ((p.rows_per + 7) / 8);
+      if (s.head_dim == 64) join_kernel<64><<<blocks, 256, 0, st>>>(p);
+      else join_kernel<128><<<blocks, 256, 0, st>>>(p);
+      e = cudaGetLastError();
+    }
     z.prefix = false;
     if (e == cudaSuccess)
       e = s.dtype == MDS_F32 ? shared_few(s, x, z, sms, st)
