@@ -404,7 +404,7 @@ def _own_shared(s, tokens, pre, lens):
     s.cache.reserve(root, pk.shape[1], counts=pre)
     s.cache.append(0, root, pk, pv, counts=pre)
     s.cache.commit(root, pre - 1, length=pk.shape[1] - 1)
-    s.cache.fork(root.repeat_interleave(G - 1), s.seqs.view(-1, G)[:, 1:].flatten())
+    s.cache.fork(root.repeat_interleave(G - 1), s.seqs.view(-1, G)[:, 1:].contiguous().flatten())
     s.cache.reserve(s.seqs, tk.shape[1], counts=lens)
     s.cache.append(0, s.seqs, tk, tv, counts=lens)
     s.cache.commit(s.seqs, lens - 1, length=tk.shape[1] - 1)
