@@ -204,12 +204,14 @@ int mds_cache_attend(mds_cache* cache, int layer, const int32_t* seqs, const int
  * group, and the pages that all of its live sequences hold at the same places,
  * as far as their tokens are committed, are read once for all of them instead
  * of once for each (in whole tiles of 128 tokens).  What is shared is found on
- * the device; a group that shares nothing is attended to all the same.  The
+ * the device; a group that shares nothing is attended to all the same, and so
+ * are all where sharing would save less than least_saved bytes of keys and
+ * values (below 0: a default, at which it pays; 0: shared in any case).  The
  * result is mds_cache_attend's but for the order of 32-bit sums and the
  * references that weights are rounded at. */
 int mds_cache_attend_shared(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                             const int64_t* q_strides, void* out, int q_heads, int n, int branches, int group,
-                            float scale, int B, void* stream);
+                            float scale, int64_t least_saved, int B, void* stream);
 
 /* Keep, of the 1 + K * L tokens behind the committed ones, the root and the
  * first accept_len[b] tokens of one branch (accept_len clamped to [-1, L];

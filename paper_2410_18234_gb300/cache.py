@@ -60,7 +60,7 @@ def _bind(lib):
         "mds_cache_rotate": [vp, vp, vp, rot, vp, i64p, vp, i, i, i, i, vp],
         "mds_cache_append_rotated": [vp, i, vp, vp, rot, vp, i64p, vp, i64p, vp, i64p, vp, i, i, i, i, vp],
         "mds_cache_attend": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, i, ctypes.c_float, i, vp],
-        "mds_cache_attend_shared": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, ctypes.c_float, i, vp],
+        "mds_cache_attend_shared": [vp, i, vp, vp, vp, i64p, vp, i, i, i, i, ctypes.c_float, ctypes.c_int64, i, vp],
         "mds_cache_commit": [vp, vp, vp, vp, vp, i, i, i, vp],
         "mds_cache_fork": [vp, vp, vp, i, vp],
         "mds_cache_truncate": [vp, vp, vp, i, vp],
@@ -346,20 +346,23 @@ class Cache:
             raise MdsError(rc, "mds_cache_attend")
         return o
 
-    def attend_shared(self, layer, seqs, q, group, branches=1, counts=None, scale=None, out=None, stream=None):
+    def attend_shared(self, layer, seqs, q, group, branches=1, counts=None, scale=None, least_saved=None, out=None,
+                      stream=None):
         """`attend` (without a window) for sequences that share a prefix: each
         ``group`` (a divisor of B) sequences of the list in turn, such as the
         forks of one prompt; unused places pad a smaller group.  The pages
         that all of a group hold, as far as they are committed, are read once
-        for all of them."""
+        for all of them, unless that would save less than ``least_saved``
+        bytes of keys and values (None: where it pays)."""
         ids, B = self._seqs(seqs)
         qs = self._rows("q", q, B)
         layer, branches, group = _sizes(layer, branches, group)
         o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
         rc = _lib.mds_cache_attend_shared(self.ctx, layer, ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
                                           o.data_ptr(), q.shape[2], q.shape[1], branches, group,
-                                          self.head_dim ** -0.5 if scale is None else float(scale), B,
-                                          self._stream(stream))
+                                          self.head_dim ** -0.5 if scale is None else float(scale),
+                                          -1 if least_saved is None else min(max(int(least_saved), 0), (1 << 63) - 1),
+                                          B, self._stream(stream))
         if rc != MDS_OK:
             raise MdsError(rc, "mds_cache_attend_shared")
         return o

@@ -241,7 +241,7 @@ int mds_cache_append_rotated(mds_cache* c, int layer, const int32_t* seqs, const
 
 static int attend_call(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                        const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
-                       float scale, int group, int B, void* stream, const char* name) {
+                       float scale, int group, int64_t least, int B, void* stream, const char* name) {
   const int rc = batch(c, seqs, B);
   if (rc != MDS_OK) return rc;
   if (layer < 0 || layer >= c->cfg.layers || n < 0 || n > MDS_CACHE_MAX_NODES || branches < 1 || q_heads < 1 ||
@@ -255,21 +255,21 @@ static int attend_call(mds_cache* c, int layer, const int32_t* seqs, const int32
   DeviceGuard g(c->device);
   mds::cache::Attend a{seqs, counts, q, q_strides[0], q_strides[1], q_strides[2], out, layer, B, n,
                        (n - 1) / branches, q_heads, window, sinks, scale};
-  return done(group > 1 ? mds::cache::attend_shared(c->s, a, group, c->sms, stream_of(stream))
+  return done(group > 1 ? mds::cache::attend_shared(c->s, a, group, least, c->sms, stream_of(stream))
                         : mds::cache::attend(c->s, a, c->sms, stream_of(stream)), name);
 }
 
 int mds_cache_attend(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                      const int64_t* q_strides, void* out, int q_heads, int n, int branches, int window, int sinks,
                      float scale, int B, void* stream) {
-  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, window, sinks, scale, 1, B, stream,
+  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, window, sinks, scale, 1, 0, B, stream,
                      "mds_cache_attend");
 }
 
 int mds_cache_attend_shared(mds_cache* c, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                             const int64_t* q_strides, void* out, int q_heads, int n, int branches, int group,
-                            float scale, int B, void* stream) {
-  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, 0, 0, scale, group, B, stream,
+                            float scale, int64_t least_saved, int B, void* stream) {
+  return attend_call(c, layer, seqs, counts, q, q_strides, out, q_heads, n, branches, 0, 0, scale, group, least_saved, B, stream,
                      "mds_cache_attend_shared");
 }
 

@@ -60,7 +60,30 @@ struct Params {
   float one = 1.f;
   int members = 1, nodes = 0;      // sequences of a group, and nodes of one
   float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
+  int worth = 0;                   // tokens that must be saved for the prefix to be attended to by itself
 };
+
+// The launches of attention over a shared prefix follow one another without a
+// pause: each may start while the one before ends, and waits for it before it
+// reads anything.  (Every block waits, so that a launch is over only when all
+// before it are.  Letting the next one start earlier than that costs more than
+// it gives: 45 us for 37 with 8 sequences over 4100 tokens.)
+__device__ __forceinline__ void after_launch_before() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+inline cudaError_t launch_behind(void (*kernel)(Params), int grid, int threads, int smem, cudaStream_t st, const Params& p) {
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = st;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, p);
+}
 
 // A sequence's part of the call.
 template <int kPart>
@@ -278,8 +301,9 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   // what a group's live sequences share is the least of what each shares with the first
   if constexpr (kPart == kPrefix) {
-    // q: the place of the first live sequence; live: nodes up to the last one
+    // q: the place of the first live sequence; live: nodes up to the last one; end: live ones
     for (int g = tid; g < p.a.B; g += blockDim.x) seqs[g] = Seq<kPart>{INT_MAX, INT_MAX, 0, 0};
+    if (tid == 0) prefix[0] = 0;
     __syncthreads();
     for (int b = tid; b < p.a.B * p.members; b += blockDim.x) {
       const int2 x = __ldg(p.s.share + b);
@@ -288,16 +312,22 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
         atomicMin(&q.len, x.x);
         atomicMin(&q.q, b);
         atomicMax(&q.live, (b % p.members + 1) * p.nodes);
+        atomicAdd(&q.end, 1);
       }
     }
     __syncthreads();
+    for (int g = tid; g < p.a.B; g += blockDim.x)
+      if (seqs[g].end > 1) atomicAdd(reinterpret_cast<int*>(prefix), (seqs[g].end - 1) * seqs[g].len);
+    __syncthreads();
+    const bool worth = *reinterpret_cast<const int*>(prefix) >= p.worth;
     for (int g = tid; g < p.a.B; g += blockDim.x) {
       const Seq<kPart> q = seqs[g];
-      seqs[g] = q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
+      seqs[g] = worth && q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
     }
   } else {
     if constexpr (kPart == kRest) {
       for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = INT_MAX;
+      if (tid == 0) prefix[0] = 0;
       __syncthreads();
     }
     for (int b = tid; b < p.a.B; b += blockDim.x) {
@@ -312,8 +342,16 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
     }
     if constexpr (kPart == kRest) {
       __syncthreads();
-      for (int b = tid; b < p.a.B; b += blockDim.x)
-        if (b % p.members) seqs[b].from = seqs[b / p.members * p.members].from;
+      // saved: for each live sequence what is shared, but once for a group
+      for (int b = tid; b < p.a.B; b += blockDim.x) {
+        const int from = seqs[b / p.members * p.members].from;
+        if (b % p.members) seqs[b].from = from;
+        const int times = (seqs[b].live > 0) - (b % p.members == 0);
+        if (from != INT_MAX && times) atomicAdd(reinterpret_cast<int*>(prefix), times * from);
+      }
+      __syncthreads();
+      if (*reinterpret_cast<const int*>(prefix) < p.worth)
+        for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = 0;
     }
   }
   __syncthreads();

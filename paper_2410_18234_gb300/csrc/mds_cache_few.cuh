@@ -293,6 +293,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
     }
     mbar_init_fence();
   }
+  if constexpr (kPart != kAll) after_launch_before();
   plan<T, kPart>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B];
   const long long per = (total + gridDim.x - 1) / gridDim.x;
@@ -560,12 +561,15 @@ cudaError_t launch_few(const State& s, const Attend& a, const Shared& x, int sms
   p.members = x.members;
   p.nodes = x.nodes;
   p.prior = x.prior;
+  p.worth = x.worth;
   const int grid = attend_grid(sms, F::kRows, D, kPart == kAll ? kPartFloats : kPieceFloats);
   p.stages = kStageMax;
   // A stage's tiles all belong to one set: a consumer waits for each of the
   // stage's phases in turn (a wait tells two phases apart, not three).
   static_assert(kStageMax % F::kSets == 0, "stages by sets");
   while (p.stages > 2 && F::template smem<kPart>(p.stages, a.B) > 227 * 1024) p.stages -= F::kSets;
+  if constexpr (kPart != kAll)
+    return launch_behind(few_kernel<T, D, NT, kPart>, grid, F::kThreads + 64, F::template smem<kPart>(p.stages, a.B), st, p);
   few_kernel<T, D, NT, kPart><<<grid, F::kThreads + 64, F::template smem<kPart>(p.stages, a.B), st>>>(p);
   return cudaGetLastError();
 }

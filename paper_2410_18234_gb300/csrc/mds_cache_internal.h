@@ -86,11 +86,12 @@ cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st);  
 cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st);   // mds_cache_many.cu
 // Groups of `members` sequences of the list, over their common prefix and each
 // over its rest (mds_cache_shared.cu; the launches: _shared_few.cu, _shared_many.cu).
-cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms, cudaStream_t st);
+cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t least, int sms, cudaStream_t st);
 struct Shared {
   int members, nodes;
   bool prefix;     // the prefix's launch; else the rest's
   float* prior;
+  int worth;
 };
 // Rows of a tile of rows in the prefix's launch, by the kernel that it is.
 inline int even_rows(int64_t rows, int most) {   // as even as it goes

@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     }
     mbar_init_fence();
   }
+  if constexpr (kPart != kAll) after_launch_before();
   plan<__nv_bfloat16, kPart>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B];
   const long long per = (total + gridDim.x - 1) / gridDim.x;
@@ -862,6 +863,7 @@ template <int D, int kSteps, int kPart>
 cudaError_t launch_many(const Params& p, int sms, cudaStream_t st) {
   const Layout l = layout_of<kPart>(D, 24 * kSteps, p.a.B);
   const int grid = attend_grid(sms, p.rows_per, D, kPart == kAll ? kPartFloats : kPieceFloats);
+  if constexpr (kPart != kAll) return launch_behind(many_kernel<D, kSteps, kPart>, grid, kThreads, l.bytes, st, p);
   many_kernel<D, kSteps, kPart><<<grid, kThreads, l.bytes, st>>>(p);
   return cudaGetLastError();
 }
@@ -889,6 +891,7 @@ cudaError_t attend_part(const State& s, const Attend& a, const Shared& x, int sm
   p.members = x.members;
   p.nodes = x.nodes;
   p.prior = x.prior;
+  p.worth = x.worth;
   const int size = p.rows_per <= 48 ? 2 : p.rows_per <= 96 ? 4 : 6;
   if (s.head_dim == 64)
     return size == 2 ? launch_many<64, 2, kPart>(p, sms, st) : size == 4 ? launch_many<64, 4, kPart>(p, sms, st) : launch_many<64, 6, kPart>(p, sms, st);

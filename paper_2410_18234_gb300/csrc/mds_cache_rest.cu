@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_kernel(const __grid_constant
     for (int i = 0; i < X::kStages; ++i) mbar_init(full + i, 1 + 32);   // the byte count, and the lanes' scale copies
   if (tid == 0) *abort = 0, cut[0] = cut[5] = -1;
   mbar_init_fence();
+  after_launch_before();
   plan<T, kRest, true>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B], share = (total + gridDim.x - 1) / gridDim.x;   // of a block of threads
   const int slack = (int)max(share / 4, (long long)kBlockSlack);
@@ -400,8 +401,8 @@ cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cu
   p.members = x.members;
   p.nodes = x.nodes;
   p.prior = x.prior;
-  rest_kernel<D><<<attend_grid(sms, kRows, D, kPieceFloats), kThreads, Rest<D>::smem(a.B), st>>>(p);
-  return cudaGetLastError();
+  p.worth = x.worth;
+  return launch_behind(rest_kernel<D>, attend_grid(sms, kRows, D, kPieceFloats), kThreads, Rest<D>::smem(a.B), st, p);
 }
 
 }  // namespace

@@ -6,6 +6,8 @@
 // Pages that several sequences hold are the same memory at the same slots, so
 // a prefix is the page indices at which the tables of all of a group's live
 // sequences agree, cut to committed tokens and to whole key tiles.
+#include <algorithm>
+
 #include "mds_cache_attend.cuh"
 
 namespace mds {
@@ -14,6 +16,23 @@ namespace cache {
 namespace {
 
 constexpr int kNarrow = 48;
+// Where the caller does not say, bytes of keys and values that must be saved
+// for prefixes to be attended to by themselves: less is over sooner without
+// the prefix's launch.  In us, shared / not (this call) / mds_cache_attend, 32
+// heads on 8 of 128 dimensions, G sequences a group:
+//   rows 4:    8 sequences, G 8,  4096 tokens ( 56 MB saved)  39 /  39 /  29
+//              2,           G 2, 32768        ( 64 MB)        47 /  61 /  39
+//              8,           G 8,  8192        (112 MB)        41 /  49 /  37
+//              8,           G 8, 16384        (224 MB)        47 /  70 /  53
+//             64,           G 64, 2048        (252 MB)        49 /  72 /  66
+//   rows 36:   8,           G 8,  2048        ( 28 MB)        50 /  41 /  31
+//              8,           G 8,  8192        (112 MB)        68 /  63 /  52
+//   rows 132: 16,           G 8,  4096        (112 MB)       137 /  95 /  78
+//             32,           G 32, 4096        (248 MB)       173 / 146 / 127
+// Weights, not bytes, bind rows of more than 16 a sequence; from about 100 on a
+// tile of rows is full without other sequences'.
+constexpr int64_t kWorthFew = 48 << 20, kWorthMany = 192 << 20;
+constexpr int kFullRows = 96;
 
 // One block of threads a sequence: the tokens that it shares with the first
 // live sequence of its group (none if it is the only one), and its live nodes.
@@ -59,6 +78,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   const int per = (p.rows_per + 7) / 8, r = blockIdx.x % per * 8 + (threadIdx.x >> 5);
   const int rt = blockIdx.x / per % p.row_tiles, h = blockIdx.x / per / p.row_tiles % p.s.kv_heads;
   const int b = blockIdx.x / per / p.row_tiles / p.s.kv_heads, row = rt * p.rows_per + r;
+  after_launch_before();
   if (r >= p.rows_per || row >= p.rows) return;
   const int2 cut = *reinterpret_cast<const int2*>(prior_of<D>(p, row_at(p, b, h, rt * p.rows_per)) + 2);
   if (cut.x < 0 || query_at<kPrefix>(p, b, row / p.g, p.a.n) < 0) return;
@@ -98,12 +118,17 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
 
 }  // namespace
 
-cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms, cudaStream_t st) {
+cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t least, int sms, cudaStream_t st) {
   const int g = a.heads / s.kv_heads, groups = a.B / members;
   // as many groups at a time as their rows' sums over the prefix have room for
   const int64_t row = (int64_t)a.n * a.heads * (s.head_dim + 4) * members;
   const int at_once = (int)(((int64_t)kPartFloats - kPieceFloats) / row);
-  if (members < 2 || at_once == 0) return attend(s, a, sms, st);
+  const int64_t own = (int64_t)a.n * g;   // rows of one sequence
+  const bool few_rows = s.dtype == MDS_F32 || own <= kFewRows;
+  if (members < 2 || at_once == 0 || (least < 0 && !few_rows && own > kFullRows)) return attend(s, a, sms, st);
+  if (least < 0) least = few_rows ? kWorthFew : kWorthMany;
+  const int64_t token = 2 * (int64_t)s.kv_heads * s.head_dim;
+  const int worth = (int)std::min<int64_t>((least + token - 1) / token, INT_MAX);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
   for (int g0 = 0; g0 < groups; g0 += at_once) {
     const int some = groups - g0 < at_once ? groups - g0 : at_once, b0 = g0 * members;
@@ -117,7 +142,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms,
     y.B = some;
     y.n = a.n * members;
     y.L = y.n - 1;
-    Shared z{members, a.n, true, s.part + kPieceFloats};
+    Shared z{members, a.n, true, s.part + kPieceFloats, worth};
     const int64_t rows = (int64_t)y.n * g;
     const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
     Params p{s, y, 0, g, (int)rows, 0, 0, 0};
@@ -134,15 +159,13 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int sms,
       e = few ? shared_few(s, y, z, sms, st) : many ? shared_many(s, y, z, sms, st) : shared_wide(s, y, z, sms, st);
     if (e == cudaSuccess) {
       const int blocks = some * s.kv_heads * p.row_tiles * ((p.rows_per + 7) / 8);
-      if (s.head_dim == 64) join_kernel<64><<<blocks, 256, 0, st>>>(p);
-      else join_kernel<128><<<blocks, 256, 0, st>>>(p);
-      e = cudaGetLastError();
+      e = launch_behind(s.head_dim == 64 ? join_kernel<64> : join_kernel<128>, blocks, 256, 0, st, p);
     }
     z.prefix = false;
     if (e == cudaSuccess)
       e = s.dtype == MDS_F32 ? shared_few(s, x, z, sms, st)
-          : (int64_t)a.n * g <= 8 ? shared_rest(s, x, z, sms, st)
-          : (int64_t)a.n * g <= 16 ? shared_few(s, x, z, sms, st) : shared_many(s, x, z, sms, st);
+          : own <= 8 ? shared_rest(s, x, z, sms, st)
+          : few_rows ? shared_few(s, x, z, sms, st) : shared_many(s, x, z, sms, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

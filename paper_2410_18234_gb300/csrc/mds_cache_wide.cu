@@ -2,7 +2,7 @@
 // the instructions' rows, two halves of up to 128 of them at a time.
 //
 //   S_h [128 rows][128 slots] = Q_h K^T     (half precision)
-//   P_h = 2^(c S_h - m), in S_h's place     (bfloat16)
+//   P_h = 2^(c S_h - m)                     (bfloat16)
 //   O_h [128 rows][D]        += P_h V       (bfloat16)
 //
 // Nothing of a prefix is masked, so a row's weights are two threads' (64 slots
@@ -11,10 +11,15 @@
 // every tile.  The two take their row's maximum over the tile first, move the
 // reference if that passes it by 2^32 (and O with it: rare), and weigh then.
 // The halves alternate: one's weights are taken while the other's products
-// run, and keys and values are widened once for both.
+// run, and keys and values are widened once for both.  Heads of 128 dimensions
+// fill tensor memory with S and O, and P takes S's place: the half's next
+// scores wait until its sums have read P.  Heads of 64 leave P a place of its
+// own.
 //
-// Four warps widen (keys, values, the groups' queries), eight weigh each half;
-// one each copies keys, copies values, issues products, walks the line.
+// Four warps widen keys and four values (and all of them the groups' queries),
+// eight weigh each half; one each copies keys, copies values, issues products,
+// walks the line.  Values are widened into two buffers, as they are the longer
+// work and would keep the products waiting from one.
 #include "mds_cache_tensor.cuh"
 
 namespace mds {
@@ -22,15 +27,15 @@ namespace cache {
 
 namespace {
 
-constexpr int kThreads = 768, kWeigh = 512;   // all, those that weigh
+constexpr int kThreads = 896, kWeigh = 512;   // all, those that weigh
 constexpr int kHalf = 128, kMostRows = kWideRows;
 static_assert(kMostRows == 2 * kHalf, "two halves");
 constexpr int kScaleRing = 8;   // tiles whose key scales are held
 constexpr float kMove = 32.f;   // weights stay below 2^32
 
 enum Bar {
-  kKFull = 0, kKEmpty = kKFull + 4, kVFull = kKEmpty + 4, kVEmpty = kVFull + 4, kWideK = kVEmpty + 4, kWideKFree = kWideK + 2,
-  kWideV = kWideKFree + 2, kWideVFree, kS, kP = kS + 2, kPV = kP + 2, kQ = kPV + 2, kOFree = kQ + 2, kJob = kOFree + 2,
+  kKFull = 0, kKEmpty = kKFull + 4, kVFull = kKEmpty + 4, kVEmpty = kVFull + 4, kWideK = kVEmpty + 4, kWideKFree,
+  kWideV, kWideVFree = kWideV + 2, kS = kWideVFree + 2, kP = kS + 2, kPV = kP + 2, kQ = kPV + 2, kOFree = kQ + 2, kJob = kOFree + 2,
   kJobFree = kJob + kJobs, kBars = kJobFree + kJobs
 };
 
@@ -39,8 +44,8 @@ template <int D>
 struct Wide {
   static constexpr int kTileBytes = kTile * D;
   static constexpr int kK = 2, kV = D == 128 ? 1 : 2;     // tiles as they are stored, in rings
-  static constexpr int q = 0, wide_k = q + kMostRows * D * 2, wide_v = wide_k + 2 * kTileBytes * 2,
-                       k_ring = wide_v + kTileBytes * 2, v_ring = k_ring + kK * kTileBytes, small = v_ring + kV * kTileBytes;
+  static constexpr int q = 0, wide_k = q + kMostRows * D * 2, wide_v = wide_k + kTileBytes * 2,
+                       k_ring = wide_v + 2 * kTileBytes * 2, v_ring = k_ring + kK * kTileBytes, small = v_ring + kV * kTileBytes;
   static int bytes(int B) {
     return 1024 + small + kScaleRing * 8 * 4 + 4 * 8 * 4 + kMostRows * (2 * 8 + 2 * 4 + 2 * 2 * 4) + (kBars + 1) / 2 * 16 +
            kJobs * (int)sizeof(Job) + 16 + seq_bytes<kPrefix>(B);
@@ -111,23 +116,24 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       mbar_init(bar + kVFull + i, 1 + 32);
       mbar_init(bar + kVEmpty + i, 4);
     }
-    mbar_init(bar + kWideV, 4);
-    mbar_init(bar + kWideVFree, 1);
+    mbar_init(bar + kWideK, 4);
+    mbar_init(bar + kWideKFree, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar + kWideK + i, 4);
-      mbar_init(bar + kWideKFree + i, 1);
+      mbar_init(bar + kWideV + i, 4);
+      mbar_init(bar + kWideVFree + i, 1);
       mbar_init(bar + kS + i, 1);
       mbar_init(bar + kP + i, 8);
       mbar_init(bar + kPV + i, 1);
-      mbar_init(bar + kQ + i, 4);
+      mbar_init(bar + kQ + i, 8);
       mbar_init(bar + kOFree + i, 8);
     }
     for (int i = 0; i < kJobs; ++i) {
       mbar_init(bar + kJob + i, 1);
-      mbar_init(bar + kJobFree + i, 7 + kWeigh / 32);   // every warp but the scheduler's
+      mbar_init(bar + kJobFree + i, 11 + kWeigh / 32);   // every warp but the scheduler's
     }
     mbar_init_fence();
   }
+  after_launch_before();
   plan<T, kPrefix>(p, prefix, seqs, D);
   __syncthreads();
   const long long total = prefix[p.a.B];
@@ -141,7 +147,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   __syncthreads();   // the plan's sums have been read
   after_sync();
   const uint32_t tmem = *tmem_at;
-  const uint32_t t_s = tmem, t_o = tmem + 2 * kTile;   // S and O of half h: kTile h further
+  constexpr bool kApart = D == 64;
+  // of half h: S 128 columns, O D, P 64, or in S's two halves
+  const uint32_t t_s = tmem, t_o = tmem + 2 * kTile, t_p = kApart ? t_o + 2 * D : t_s;
+  constexpr uint32_t kHalfP = kApart ? 64 : kTile, kPartP = kApart ? 32 : 64;   // from a half to the next, from 64 slots to the next
   auto hold = [&](int b, unsigned parity) { wait(bar + b, parity, abort); };
   // a role takes the jobs in turn
   auto job_at = [&](int n) -> const Job& {
@@ -196,23 +205,38 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     }
     report(abort, s.status);
   } else if (warp == 1) {
-    // ---- products, issued by one thread.  A half's weights lie where its
-    // scores were, so its next scores wait until its sums have read them.
+    // ---- products, issued by one thread
     const uint32_t id_s = instruction(kTile, 0, 0), id_o = instruction(D, 1, 0) | 1u << 16;   // V's contiguous axis is its columns
     const uint64_t q_op = operand(smem_u32(base + W::q), 16), k_op = operand(smem_u32(base + W::wide_k), 16);
     const uint64_t v_op = operand(smem_u32(base + W::wide_v), kTile * 128);
     int tile = 0, group = 0;
     auto sums = [&](int t, int h, bool first) {
       hold(kP + h, t & 1);
-      if (h == 0) hold(kWideV, t & 1);
+      if (h == 0) hold(kWideV + (t & 1), (t >> 1) & 1);
       if (first) hold(kOFree + h, (group & 1) ^ 1);
       after_sync();
       if (elected()) {
+        const uint64_t v = v_op + ((t & 1) * (W::kTileBytes * 2) >> 4);
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)   // 16 slots: 8 columns of weights (64 slots' from column 64 on), 2048 bytes of V
-          mma_ts(t_o + h * kTile, t_s + h * kTile + (k >> 2) * 64 + (k & 3) * 8, v_op + k * (2048 >> 4), id_o, !(first && k == 0));
+        for (int k = 0; k < kTile / 16; ++k)   // 16 slots: 8 columns of weights, 2048 bytes of V
+          mma_ts(t_o + h * D, t_p + h * kHalfP + (k >> 2) * kPartP + (k & 3) * 8, v + k * (2048 >> 4), id_o, !(first && k == 0));
         commit_to(bar + kPV + h);
-        if (h == halves - 1) commit_to(bar + kWideVFree);
+        if (h == halves - 1) commit_to(bar + kWideVFree + (t & 1));
+      }
+      __syncwarp();
+    };
+    auto scores = [&](int t, int h) {
+      if (h == 0) hold(kWideK, t & 1);
+      after_sync();
+      if (elected()) {
+        const uint64_t q = q_op + (h * (kHalf * D * 2) >> 4);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t step = ((k >> 2) * kTile * 128 + (k & 3) * 32) >> 4;
+          mma_ss(t_s + h * kTile, q + step, k_op + step, id_s, k > 0);
+        }
+        commit_to(bar + kS + h);
+        if (h == halves - 1) commit_to(bar + kWideKFree);
       }
       __syncwarp();
     };
@@ -222,44 +246,37 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       job_done(group);
       hold(kQ + (group & 1), (group >> 1) & 1);
       for (int i = 0; i < cnt; ++i, ++tile) {
-        const int wide = tile & 1;
         for (int h = 0; h < halves; ++h) {
-          if (i > 0) {
-            sums(tile - 1, h, i == 1);
-            hold(kPV + h, (tile - 1) & 1);
-          }
-          if (h == 0) hold(kWideK + wide, (tile >> 1) & 1);
-          after_sync();
-          if (elected()) {
-            const uint64_t q = q_op + (h * (kHalf * D * 2) >> 4), k0 = k_op + (wide * (W::kTileBytes * 2) >> 4);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint32_t step = ((k >> 2) * kTile * 128 + (k & 3) * 32) >> 4;
-              mma_ss(t_s + h * kTile, q + step, k0 + step, id_s, k > 0);
+          if (kApart) {
+            if (i > 0) hold(kP + h, (tile - 1) & 1);   // the scores before have been read
+            scores(tile, h);
+            if (i > 0) sums(tile - 1, h, i == 1);
+          } else {
+            if (i > 0) {
+              sums(tile - 1, h, i == 1);
+              hold(kPV + h, (tile - 1) & 1);
             }
-            commit_to(bar + kS + h);
-            if (h == halves - 1) commit_to(bar + kWideKFree + wide);
+            scores(tile, h);
           }
-          __syncwarp();
         }
       }
       for (int h = 0; h < halves; ++h) {
         sums(tile - 1, h, cnt == 1);
         // the next group's first scores may not overwrite the weights before they are read
-        hold(kPV + h, (tile - 1) & 1);
+        if (!kApart) hold(kPV + h, (tile - 1) & 1);
       }
       ++group;
     }
-  } else if (warp < 8) {
-    // ---- widen keys and values, and the groups' queries
+  } else if (warp < 12) {
+    // ---- widen keys, or values, and the groups' queries
     const int w4 = warp & 3;
     int ks = 0, vs = 0;
     unsigned kp = 0, vp = 0;
     auto keys = [&](int t) {
       hold(kKFull + ks, kp);
-      hold(kWideKFree + (t & 1), ((t >> 1) & 1) ^ 1);
+      hold(kWideKFree, (t & 1) ^ 1);
       const char* src = base + W::k_ring + ks * W::kTileBytes;
-      char* dst = base + W::wide_k + (t & 1) * (W::kTileBytes * 2);
+      char* dst = base + W::wide_k;
       constexpr int kUnits = D / 16;
 #pragma unroll 1
       for (int i0 = 0; i0 < kUnits; i0 += 4) {
@@ -286,20 +303,20 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(bar + kKEmpty + ks);
-        mbar_arrive(bar + kWideK + (t & 1));
+        mbar_arrive(bar + kWideK);
       }
       if (++ks == W::kK) ks = 0, kp ^= 1u;
     };
     auto values = [&](int t) {
       hold(kVFull + vs, vp);
-      hold(kWideVFree, (t & 1) ^ 1);
+      hold(kWideVFree + (t & 1), ((t >> 1) & 1) ^ 1);
       const float* sc = v_scales + vs * 8 + w4 * 2;
       unsigned rest[2], factor[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) factor[i] = value_factor(sc[i], rest[i]);
       const bool large = rest[0] != 0x3f803f80u || rest[1] != 0x3f803f80u;
       const char* src = base + W::v_ring + vs * W::kTileBytes;
-      char* dst = base + W::wide_v;
+      char* dst = base + W::wide_v + (t & 1) * (W::kTileBytes * 2);
       constexpr int kUnits = D / 16;
 #pragma unroll 1
       for (int i0 = 0; i0 < kUnits; i0 += 4) {
@@ -334,25 +351,25 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(bar + kVEmpty + vs);
-        mbar_arrive(bar + kWideV);
+        mbar_arrive(bar + kWideV + (t & 1));
       }
       if (++vs == W::kV) vs = 0, vp ^= 1u;
     };
-    // A group's queries, scaled to half precision, rows of 128 bytes; each
-    // warp's rows are its own from copy to scaling.
+    // A group's queries, scaled to half precision, rows of 128 bytes; a warp's
+    // 32 rows are its own from copy to scaling.
     auto queries = [&](int n, const Job& job) {
       constexpr int kUnits = D / 8, kAtOnce = 32 / kUnits;
       const T* q = static_cast<const T*>(p.a.q);
       int64_t* out = row_out + (n & 1) * kMostRows;
       float* coef = row_coef + (n & 1) * kMostRows;
-      int64_t from_row = 0;
-      for (int r0 = w4 * 64; r0 < w4 * 64 + 64; r0 += 32) {   // a row a lane
+      const int r0 = (warp - 4) * 32;
+      {   // a row a lane
         const int r = r0 + lane, h = r >> 7, in = r & (kHalf - 1);
         const int row = job.row0 + (h ? half0 + in : in), node = row / p.g, head = job.h * p.g + row - node * p.g;
         const bool mine = h ? half0 + in < p.rows_per : in < min(half0, p.rows_per);
         const int64_t from = mine ? query_at<kPrefix>(p, job.b, node, job.live) : -1;
         out[r] = from >= 0 ? row_at(p, job.b, job.h, row) : -1;
-        from_row = from >= 0 ? from + head * p.a.q_head : -1;
+        const int64_t from_row = from >= 0 ? from + head * p.a.q_head : -1;
         // its copies: 16 bytes a lane, kAtOnce rows at a time
 #pragma unroll 4
         for (int i = 0; i < 32; i += kAtOnce) {
@@ -369,15 +386,15 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
 #pragma unroll 4
-      for (int r0 = w4 * 64; r0 < w4 * 64 + 64; r0 += kAtOnce) {
-        const int r = r0 + lane / kUnits, unit = lane % kUnits;
+      for (int i = 0; i < 32; i += kAtOnce) {
+        const int r = r0 + i + lane / kUnits, unit = lane % kUnits;
         uint4* at_lane = reinterpret_cast<uint4*>(base + W::q + (r >> 7) * (kHalf * D * 2) + (unit >> 3) * (kHalf * 128) +
                                                   (r & 127) * 128 + (((unit & 7) ^ (r & 7)) << 4));
         const uint4 y = *at_lane;
         const unsigned w[4] = {y.x, y.y, y.z, y.w};
         unsigned bits = 0;   // the largest magnitude: bfloat16 order as their bits do
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bits = max(bits, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
+        for (int z = 0; z < 4; ++z) bits = max(bits, max(w[z] << 16 & 0x7fff0000u, w[z] & 0x7fff0000u));
 #pragma unroll
         for (int d = 1; d < kUnits; d *= 2) bits = max(bits, __shfl_xor_sync(kFull, bits, d));
         const int e = bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23) - 127 - 14, -112);
@@ -386,9 +403,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const float inv = p.a.scale == 0.f ? 0.f : copysignf(__uint_as_float((unsigned)(127 - e) << 23), p.a.scale);
         unsigned v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const __half2 a = __floats2half2_rn(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
-          v[i] = *reinterpret_cast<const unsigned*>(&a);
+        for (int z = 0; z < 4; ++z) {
+          const __half2 a = __floats2half2_rn(__uint_as_float(w[z] << 16) * inv, __uint_as_float(w[z] & 0xffff0000u) * inv);
+          v[z] = *reinterpret_cast<const unsigned*>(&a);
         }
         *at_lane = uint4{v[0], v[1], v[2], v[3]};
         if (unit == 0) coef[r] = p.a.scale == 0.f ? 1.f : fabsf(p.a.scale) * dev::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
@@ -404,23 +421,28 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int cnt = job.cnt;
       // the products of the group before have read its queries, and every warp
       // is done with what the rows of the group before that were
-      if (tile) hold(kWideKFree + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
+      if (tile) hold(kWideKFree, (tile - 1) & 1);
       if (n > 1) hold(kJobFree + ((n - 2) & (kJobs - 1)), ((n - 2) / kJobs) & 1);
       queries(n, job);
       job_done(n);
-      keys(tile);
       for (int i = 0; i < cnt; ++i, ++tile) {
-        if (i + 1 < cnt) keys(tile + 1);
-        values(tile);
+        if (warp < 8) {
+          keys(tile);
+        } else {
+          // every phase in turn: a wait does not tell one from the next but one
+          if (tile) hold(kWideKFree, (tile - 1) & 1);
+          values(tile);
+        }
       }
     }
   } else {
     // ---- weigh: 64 slots of a row of a half a thread
-    const int half = (warp - 8) >> 3, part = ((warp - 8) >> 2) & 1, w4 = warp & 3, r = half * kHalf + w4 * 32 + lane;
+    const int half = (warp - 12) >> 3, part = ((warp - 12) >> 2) & 1, w4 = warp & 3, r = half * kHalf + w4 * 32 + lane;
     const int mine = half ? half0 + w4 * 32 + lane : w4 * 32 + lane;   // row of the tile of rows
     const bool used = mine - lane < (half ? halves == 2 ? p.rows_per : 0 : min(half0, p.rows_per));   // the warp has rows
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    const uint32_t s_at = t_s + half * kTile + part * 64 + lanes, o_at = t_o + half * kTile + part * (D / 2) + lanes;
+    const uint32_t s_at = t_s + half * kTile + part * 64 + lanes, o_at = t_o + half * D + part * (D / 2) + lanes;
+    const uint32_t p_at = t_p + half * kHalfP + part * kPartP + lanes;
     // a row's two threads: theirs and the other's places
     auto tell = [&](int t, float x) {
       float* to = shared_row + (t & 1) * (2 * kMostRows) + r;
@@ -459,6 +481,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             top = fmaxf(top, __fmul_rn(m, rc * sc[j]));
           }
           top = fmaxf(top, tell(told++, top));
+          if (kApart && i > 0) {   // the weights before have been read
+            hold(kPV + half, (tile - 1) & 1);
+            after_sync();
+          }
           if (i == 0) {
             ref = top > kNone ? top : 0.f;
           } else if (__any_sync(kFull, top > ref + kMove)) {
@@ -495,8 +521,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
               w[z] = pack_bf16(ex2(e.x), ex2(e.y));
               sum = add2(sum, float2{__uint_as_float(w[z] << 16), __uint_as_float(w[z] & 0xffff0000u)});
             }
-            // their place has been read: block j's weights are columns 8 j .., its scores 16 j ..
-            tmem_st8(s_at + j * 8, w);
+            // in the scores' place, that has been read: block j's weights are columns 8 j .., its scores 16 j ..
+            tmem_st8(p_at + j * 8, w);
           }
           tmem_st_wait();
         }
@@ -547,8 +573,8 @@ cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cu
   p.members = x.members;
   p.nodes = x.nodes;
   p.prior = x.prior;
-  wide_kernel<D><<<attend_grid(sms, p.rows_per, D, kPieceFloats), kThreads, Wide<D>::bytes(a.B), st>>>(p);
-  return cudaGetLastError();
+  p.worth = x.worth;
+  return launch_behind(wide_kernel<D>, attend_grid(sms, p.rows_per, D, kPieceFloats), kThreads, Wide<D>::bytes(a.B), st, p);
 }
 
 }  // namespace

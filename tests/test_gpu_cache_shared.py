@@ -64,7 +64,8 @@ def bound(mag, big, o, T, D, dtype):
     return mag * (2 * score + 2 * weight + 2 * (T + 32) * u) * (1 + out) + np.abs(o) * out + 1e-30
 
 
-def check(c, m, rng, seqs, G, Hq, K, L, dtype="bf16", counts=None, only=None, factor=1.5, scale=None):
+def check(c, m, rng, seqs, G, Hq, K, L, dtype="bf16", counts=None, only=None, factor=1.5, scale=None,
+          least=0):
     """One call on a new tree of every sequence."""
     n = 1 + K * L
     real = [q for q in seqs if q >= 0]
@@ -74,7 +75,7 @@ def check(c, m, rng, seqs, G, Hq, K, L, dtype="bf16", counts=None, only=None, fa
     q = x[:, :, 1:]                       # rows that are not the tensor's own
     out = torch.full((len(seqs), n, Hq, m.D), 7.0, device=DEV, dtype=DT[dtype])
     given = None if counts is None else ints(counts)
-    o = c.attend_shared(0, ints(seqs), q, G, branches=K, counts=given, out=out, scale=scale)
+    o = c.attend_shared(0, ints(seqs), q, G, branches=K, counts=given, out=out, scale=scale, least_saved=least)
     assert o is out
     for b, s in enumerate(seqs):
         live = 0 if s < 0 else n if counts is None else min(max(counts[b], 0), n)
@@ -91,7 +92,7 @@ def check(c, m, rng, seqs, G, Hq, K, L, dtype="bf16", counts=None, only=None, fa
         lim = bound(mag, big, want, T, m.D, dtype)[:live]
         assert (err <= lim).all(), (b, s, float((err / lim).max()))
     # the same again, bit for bit, whatever the blocks' order
-    assert torch.equal(c.attend_shared(0, ints(seqs), q, G, branches=K, counts=given, scale=scale), o)
+    assert torch.equal(c.attend_shared(0, ints(seqs), q, G, branches=K, counts=given, scale=scale, least_saved=least), o)
     m.commit(real, [-1] * len(real))
     c.commit(ints(real), ints([-1] * len(real)), branches=K, length=L)
     assert c.status() == (0, "ok")
@@ -121,6 +122,9 @@ def test_groups_of_forks(D, page, H, g, dtype):
         check(c, m, rng, order, 3, H * g, K, L, dtype)
     # one group of all: nothing is shared by every sequence
     check(c, m, rng, order, 21, H * g, 2, 4, dtype)
+    # too little to save
+    check(c, m, rng, order, 3, H * g, 2, 4, dtype, least=None)
+    check(c, m, rng, order, 3, H * g, 1, 0, dtype, least=1 << 70)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -161,6 +165,23 @@ def test_many_groups_and_groups_too_large():
     grow(c, m, rng, list(range(B)), [int(x) for x in rng.integers(0, 60, B)])
     check(c, m, rng, list(range(B)), 4, Hq, K, L, only=[0, 27, 28, 31, 62])
     check(c, m, rng, list(range(B)), 64, Hq, K, L, only=[0, 63])
+
+
+def test_least_saved_is_an_exact_border():
+    """Two of three sequences' 256 tokens of 2 heads: 2 * 256 * 256 bytes; one
+    less and one more give the two ways' roundings."""
+    rng = np.random.default_rng(17)
+    c, m = both(60, 2, 64, 4, 12, 64)
+    grow(c, m, rng, [0], [300])
+    fork(c, m, [0, 0], [1, 2])
+    grow(c, m, rng, [0, 1, 2], [5, 40, 90])
+    saved = 2 * 256 * 2 * 2 * 64
+    q = 0.02 * tokens(rng, 4, 1, 8, 64)       # weights that are spread over all tokens, so that the two ways differ
+    seqs = ints([0, 1, 2, -1])
+    c.reserve(seqs, 1)
+    a, b, never, always = (c.attend_shared(0, seqs, q, 4, least_saved=x) for x in (saved, saved + 256, 1 << 40, 0))
+    assert torch.equal(a, always) and torch.equal(b, never) and not torch.equal(a, b)
+    assert (a.double() - b.double()).abs().max() <= 2.0 ** -7 * b.double().abs().max()
 
 
 @pytest.mark.parametrize("G", [2, 17, 100])
@@ -219,7 +240,7 @@ def test_far_apart_halves():
     c.append(0, ints([0, 1]), own, torch.full_like(own, 2.0 ** -30))
     for sign, want in ((1, 2.0 ** -30), (-1, 2.0 ** 30)):
         q = sign * torch.full((2, 1, 4, 64), 100.0, device=DEV, dtype=torch.bfloat16)
-        o = c.attend_shared(0, ints([0, 1]), q, 2)
+        o = c.attend_shared(0, ints([0, 1]), q, 2, least_saved=0)
         # scores of 80000 on one side, and below them on the other: one value alone
         assert (o == want).all()
     assert c.status() == (0, "ok")
@@ -235,16 +256,16 @@ def test_streams_and_graphs():
     seqs = ints([0, 1, 2, -1])
     q = tokens(rng, 4, 1, 8, 64)
     c.reserve(seqs, 1)
-    want = c.attend_shared(0, seqs, q, 4)
+    want = c.attend_shared(0, seqs, q, 4, least_saved=0)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    got = c.attend_shared(0, seqs, q, 4, stream=side)
+    got = c.attend_shared(0, seqs, q, 4, least_saved=0, stream=side)
     side.synchronize()
     assert torch.equal(got, want)
     out = torch.zeros_like(q)
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
-        c.attend_shared(0, seqs, q, 4, out=out)
+        c.attend_shared(0, seqs, q, 4, least_saved=0, out=out)
     g.replay()
     assert torch.equal(out, want)
     # sequence 2 loses what it shares behind slot 100, and grows again
@@ -254,7 +275,7 @@ def test_streams_and_graphs():
     c.append(0, ints([2]), k, k)
     c.commit(ints([2]), ints([199]), length=199)
     c.reserve(seqs, 1)
-    want = c.attend_shared(0, seqs, q, 4)
+    want = c.attend_shared(0, seqs, q, 4, least_saved=0)
     out.zero_()
     g.replay()
     assert torch.equal(out, want) and (out[2] != 0).any()
@@ -268,7 +289,7 @@ def test_tokens_that_are_not_reserved():
     fork(c, m, [0], [1])
     c.reserve(ints([0]), 1)
     q = tokens(rng, 2, 3, 4, 64)
-    o = c.attend_shared(0, ints([0, 1]), q, 2)
+    o = c.attend_shared(0, ints([0, 1]), q, 2, least_saved=0)
     assert c.status()[0] == cache.MDS_ST_BADSEQ
     assert o[0, 0].any() and not o[0, 1:].any() and not o[1].any()
     o = c.attend_shared(0, ints([0, 9]), q[:, :1], 2)
