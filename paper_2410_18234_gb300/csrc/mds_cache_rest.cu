@@ -34,7 +34,7 @@ template <int D>
 struct Rest {
   static constexpr int kStage = 2 * kBlock * D, kStages = kRing / kStage;
   static constexpr int kPiece = kRows * kPieceRow<D> * 4;
-  static int smem(int B) {
+  static constexpr int smem(int B) {
     return 1024 + kWarps * (kRing + kPiece + kStages * 16) + kRows * 8 + 64 + (B + 2) / 2 * 16 + seq_bytes<kRest>(B);
   }
 };
@@ -396,6 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_kernel(const __grid_constant
 
 template <int D>
 cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st) {
+  static_assert(Rest<D>::smem(MDS_CACHE_MAX_BATCH) <= 227 * 1024, "shared memory for the largest batch");
   Params p{s, a, kBlock, a.heads / s.kv_heads, 0, 1, 0, kRows};
   p.rows = a.n * p.g;
   p.members = x.members;

@@ -46,8 +46,8 @@ struct Wide {
   static constexpr int kK = 2, kV = D == 128 ? 1 : 2;     // tiles as they are stored, in rings
   static constexpr int q = 0, wide_k = q + kMostRows * D * 2, wide_v = wide_k + kTileBytes * 2,
                        k_ring = wide_v + 2 * kTileBytes * 2, v_ring = k_ring + kK * kTileBytes, small = v_ring + kV * kTileBytes;
-  static int bytes(int B) {
-    return 1024 + small + kScaleRing * 8 * 4 + 4 * 8 * 4 + kMostRows * (2 * 8 + 2 * 4 + 2 * 2 * 4) + (kBars + 1) / 2 * 16 +
+  static constexpr int bytes(int B) {
+    return 1024 + small + kScaleRing * 8 * 4 + 4 * 8 * 4 + kMostRows * (2 * 4 + 2 * 4 + 2 * 2 * 4) + (kBars + 1) / 2 * 16 +
            kJobs * (int)sizeof(Job) + 16 + seq_bytes<kPrefix>(B);
   }
 };
@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   at += kScaleRing * 8 * 4;
   float* v_scales = reinterpret_cast<float*>(at);          // [W::kV][8], by the ring's slot
   at += 4 * 8 * 4;
-  int64_t* row_out = reinterpret_cast<int64_t*>(at);       // [2][rows], by group: a row's place in the call, -1: not live
-  at += 2 * kMostRows * 8;
+  int* row_out = reinterpret_cast<int*>(at);               // [2][rows], by group: a row's place in the call, -1: not live
+  at += 2 * kMostRows * 4;
   float* row_coef = reinterpret_cast<float*>(at);          // [2][rows]: of scores, to log2 units
   at += 2 * kMostRows * 4;
   float* shared_row = reinterpret_cast<float*>(at);        // [2][2][rows]: what a row's two threads tell one another, by tile
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     auto queries = [&](int n, const Job& job) {
       constexpr int kUnits = D / 8, kAtOnce = 32 / kUnits;
       const T* q = static_cast<const T*>(p.a.q);
-      int64_t* out = row_out + (n & 1) * kMostRows;
+      int* out = row_out + (n & 1) * kMostRows;
       float* coef = row_coef + (n & 1) * kMostRows;
       const int r0 = (warp - 4) * 32;
       {   // a row a lane
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const int row = job.row0 + (h ? half0 + in : in), node = row / p.g, head = job.h * p.g + row - node * p.g;
         const bool mine = h ? half0 + in < p.rows_per : in < min(half0, p.rows_per);
         const int64_t from = mine ? query_at<kPrefix>(p, job.b, node, job.live) : -1;
-        out[r] = from >= 0 ? row_at(p, job.b, job.h, row) : -1;
+        out[r] = from >= 0 ? (int)row_at(p, job.b, job.h, row) : -1;   // `prior` has fewer than 2^18 rows
         const int64_t from_row = from >= 0 ? from + head * p.a.q_head : -1;
         // its copies: 16 bytes a lane, kAtOnce rows at a time
 #pragma unroll 4
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int cnt = job.cnt;
       hold(kQ + (n & 1), (n >> 1) & 1);
       const float rc = row_coef[(n & 1) * kMostRows + r];
-      const int64_t out = row_out[(n & 1) * kMostRows + r];
+      const int out = row_out[(n & 1) * kMostRows + r];
       float ref = 0.f;
       float2 sum{0.f, 0.f};
       for (int i = 0; i < cnt && half < halves; ++i, ++tile) {
@@ -566,6 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 
 template <int D>
 cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st) {
+  static_assert(Wide<D>::bytes(MDS_CACHE_MAX_BATCH / 2) <= 227 * 1024, "shared memory for groups of two of the largest batch");
   Params p{s, a, s.page_tokens < kTile ? s.page_tokens : kTile, a.heads / s.kv_heads, 0, 0, 0, 0};
   p.rows = a.n * p.g;
   p.rows_per = even_rows(p.rows, kWideRows);

@@ -282,6 +282,62 @@ def test_streams_and_graphs():
     assert c.status() == (0, "ok")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,K,L", [(2, 1, 0), (3, 1, 0), (6, 1, 0), (6, 2, 4), (3, 1, 30)])
+def test_queries_that_are_not_numbers_stay_in_their_rows(G, K, L, dtype):
+    """One head of one node is NaN, one infinite: every other row as without, up
+    to roundings.  A warp's rows move their references together, so an infinite
+    row's moves put the weights of others at other places of their rounding:
+    each of the two answers is within its bound of the exact one, 2 * 2^-8 of
+    the largest value for weights in the sum and in the normaliser and 2^-8 for
+    the output (32-bit queries: 2^-20 covers the few units in 2^-24)."""
+    rng = np.random.default_rng(18)
+    c, m = both(200, 2, 64, 6, 30, 64, dtype)
+    grow(c, m, rng, [0], [700], dtype)
+    fork(c, m, [0] * 5, [1, 2, 3, 4, 5])
+    grow(c, m, rng, list(range(6)), [5, 40, 90, 0, 33, 200], dtype)
+    n = 1 + K * L
+    grow(c, m, rng, list(range(6)), [n] * 6, dtype, keep=False)
+    q = 0.05 * tokens(rng, 6, n, 10, 64, dtype=dtype)
+    want = c.attend_shared(0, ints(range(6)), q, G, branches=K, least_saved=0)
+    bad = q.clone()
+    bad[1, 0, 3, 7], bad[4, n - 1, 8, 0] = float("nan"), float("inf")
+    got = c.attend_shared(0, ints(range(6)), bad, G, branches=K, least_saved=0)
+    same = torch.ones(6, n, 10, dtype=torch.bool, device=DEV)
+    same[1, 0, 3] = same[4, n - 1, 8] = False
+    largest = max(float(np.abs(m.get(s, 0, 0, m.lens[s] + n)[1]).max()) for s in range(6))
+    assert torch.isfinite(want).all() and torch.isfinite(got[same]).all()
+    assert float((got[same] - want[same]).abs().max()) <= 2 * 3 * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -20) * largest
+    assert got[1, 0, 3].isnan().all()
+    assert c.status() == (0, "ok")
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "f32"), (64, "bf16")])
+def test_the_largest_batches(D, dtype):
+    """1024 sequences in groups of 2, of 32 and all together."""
+    rng = np.random.default_rng(19)
+    B = 1024
+    c = cache.Cache(1, 3 * B + 64, 1, D, B, 8, page_tokens=128, dtype=dtype)
+    x = tokens(rng, 1, 300, 1, D, dtype=dtype)
+    c.reserve(ints([0]), 300)
+    c.append(0, ints([0]), x, x)
+    c.commit(ints([0]), ints([299]), length=299)
+    c.fork(ints([0] * (B - 1)), ints(range(1, B)))
+    seqs = ints(rng.permutation(B))
+    c.reserve(seqs, 9)
+    y = tokens(rng, B, 9, 1, D, dtype=dtype)
+    c.append(0, seqs, y, y)
+    for n, K in ((1, 1), (9, 2)):
+        q = 0.05 * tokens(rng, B, n, 4, D, dtype=dtype)
+        want = c.attend(0, seqs, q, branches=K)
+        for G in (2, 32, 1024):
+            got = c.attend_shared(0, seqs, q, G, branches=K, least_saved=0)
+            # each is within its bound of the exact sum: here at most twice the weights' and the outputs' roundings
+            tol = 4 * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -18) * float(torch.maximum(x.abs().max(), y.abs().max()))
+            assert float((got - want).abs().max()) <= tol
+    assert c.status() == (0, "ok")
+
+
 def test_tokens_that_are_not_reserved():
     rng = np.random.default_rng(16)
     c, m = both(60, 1, 64, 2, 24, 16)
