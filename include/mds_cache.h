@@ -8,7 +8,8 @@
  *   per model layer:
  *     mds_cache_append   their keys and values, quantised to 8 bits (_append_rotated:
  *                        with rotary positions)
- *     mds_cache_attend   attention of every tree node over the cache
+ *     mds_cache_attend   attention of every tree node over the cache (_attend_shared:
+ *                        for sequences that share a prefix)
  *   mds_verify           the target logits of the nodes against the drafts
  *   mds_cache_commit     the root and the accepted branch stay, packed; the
  *                        other tokens and the pages behind them go

@@ -9,7 +9,7 @@ one given.  A step of multi-draft decoding:
     c.reserve(seqs, 1 + K * L)
     for layer in range(layers):
         c.append(layer, seqs, k, v)                    # [B][1 + K * L][kv_heads][head_dim]; append_rotated: with positions
-        o = c.attend(layer, seqs, q, branches=K)       # [B][1 + K * L][q_heads][head_dim]
+        o = c.attend(layer, seqs, q, branches=K)       # [B][1 + K * L][q_heads][head_dim]; attend_shared: forks of a prompt
     out_tokens, accept_len, _ = verifier.verify(...)   # mds.Verifier
     c.commit(seqs, accept_len, branches=K, length=L, draft_tokens=tokens, out_tokens=out_tokens)
 """
