@@ -86,10 +86,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _sizes(*given):
     """`given` as integers that the C interface's 32 bits hold: ctypes would cut larger ones."""
-    out = [int(x) for x in given]
-    for x in out:
-        if not -1 << 31 <= x < 1 << 31:
-            raise MdsError(MDS_ESHAPE, f"a size of {x}")
+    out = tuple(map(int, given))
+    if not -1 << 31 <= min(out) <= max(out) < 1 << 31:
+        raise MdsError(MDS_ESHAPE, f"a size of {min(out)} or {max(out)}")
     return out
 
 
@@ -165,6 +164,7 @@ class Cache:
         self.kv_heads, self.head_dim = int(kv_heads), int(head_dim)
         self.max_seqs, self.max_pages = int(max_seqs), int(max_pages)
         self.ctx = None
+        self._layouts = {}
         cfg = _config(layers, pages, kv_heads, head_dim, max_seqs, max_pages, page_tokens, dtype)
         if cfg.dtype not in mds.TORCH_DTYPES:
             raise MdsError(MDS_EINVAL, "mds_cache_create")
@@ -211,15 +211,26 @@ class Cache:
         return t.data_ptr()
 
     def _seqs(self, seqs):
-        if seqs.dim() != 1:
-            raise MdsError(MDS_ESHAPE, f"seqs has shape {tuple(seqs.shape)}, expected (B,)")
-        B = seqs.shape[0]
-        return self._ints("seqs", seqs, (B,)), B
+        s = seqs.shape
+        if len(s) != 1:
+            raise MdsError(MDS_ESHAPE, f"seqs has shape {tuple(s)}, expected (B,)")
+        return self._ints("seqs", seqs, s), s[0]
 
     def _rows(self, name, t, B, heads=None):
         """Check [B][n][heads][head_dim] of any strides but the last; strides of the first three axes."""
         if t.dtype is not self.dtype or t.get_device() != self._index:
             raise MdsError(MDS_EINVAL, f"{name}: {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
+        # layouts that passed before: a call's checks take longer than its launch
+        key = (t.shape, t.stride(), B, heads)
+        known = self._layouts.get(key)
+        if known is None:
+            known = self._layout(name, t, B, heads)
+            if len(self._layouts) >= 256:
+                self._layouts.clear()
+            self._layouts[key] = known
+        return known
+
+    def _layout(self, name, t, B, heads):
         s = t.shape
         if len(s) != 4 or s[0] != B or s[3] != self.head_dim or (heads is not None and s[2] != heads) or \
                 max(s) >= 1 << 31:
@@ -235,13 +246,14 @@ class Cache:
         """`given`, checked, or new tensors, allocated on the stream that writes them."""
         if given is not None:
             for t in given:
-                if tuple(t.shape) != shape:
-                    raise MdsError(MDS_ESHAPE, f"out has shape {tuple(t.shape)}, expected {shape}")
+                if t.shape != shape:
+                    raise MdsError(MDS_ESHAPE, f"out has shape {tuple(t.shape)}, expected {tuple(shape)}")
                 if t.dtype is not self.dtype or t.get_device() != self._index or not t.is_contiguous():
                     raise MdsError(MDS_EINVAL, f"out: contiguous {self.dtype} on {self.device}")
             return given
         if stream is None:
-            return [torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(n)]
+            new = torch.empty(shape, dtype=self.dtype, device=self.device)
+            return (new,) if n == 1 else (new, torch.empty(shape, dtype=self.dtype, device=self.device))
         if isinstance(stream, torch.cuda.Stream):
             with torch.cuda.stream(stream):
                 return tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(n))
@@ -292,7 +304,7 @@ class Cache:
         ids, B = self._seqs(seqs)
         xs = self._rows("x", x, B)
         branches, = _sizes(branches)
-        o, = self._outs(tuple(x.shape), stream, None if out is None else (out,))
+        o, = self._outs(x.shape, stream, None if out is None else (out,))
         if out is not None and x.numel():
             self._apart(out, x)
         rc = _lib.mds_cache_rotate(self.ctx, ids, self._ints("counts", counts, (B,)), rotary._ref,
@@ -316,7 +328,7 @@ class Cache:
             qs = self._rows("q", q, B)
             if q.shape[1] != k.shape[1]:
                 raise MdsError(MDS_ESHAPE, f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
-            o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
+            o, = self._outs(q.shape, stream, None if out is None else (out,))
             if out is not None and q.numel():
                 self._apart(out, q, (k, v))
         elif out is not None:
@@ -338,7 +350,7 @@ class Cache:
         ids, B = self._seqs(seqs)
         qs = self._rows("q", q, B)
         layer, branches, window, sinks = _sizes(layer, branches, window, sinks)
-        o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
+        o, = self._outs(q.shape, stream, None if out is None else (out,))
         rc = _lib.mds_cache_attend(self.ctx, layer, ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
                                    o.data_ptr(), q.shape[2], q.shape[1], branches, window, sinks,
                                    self.head_dim ** -0.5 if scale is None else float(scale), B, self._stream(stream))
@@ -357,7 +369,7 @@ class Cache:
         ids, B = self._seqs(seqs)
         qs = self._rows("q", q, B)
         layer, branches, group = _sizes(layer, branches, group)
-        o, = self._outs(tuple(q.shape), stream, None if out is None else (out,))
+        o, = self._outs(q.shape, stream, None if out is None else (out,))
         rc = _lib.mds_cache_attend_shared(self.ctx, layer, ids, self._ints("counts", counts, (B,)), q.data_ptr(), qs,
                                           o.data_ptr(), q.shape[2], q.shape[1], branches, group,
                                           self.head_dim ** -0.5 if scale is None else float(scale),

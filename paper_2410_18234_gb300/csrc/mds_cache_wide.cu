@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const char* src = base + W::k_ring + ks * W::kTileBytes;
       char* dst = base + W::wide_k;
       constexpr int kUnits = D / 16;
-#pragma unroll 1
+#pragma unroll
       for (int i0 = 0; i0 < kUnits; i0 += 4) {
         uint4 y[4];
 #pragma unroll
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const char* src = base + W::v_ring + vs * W::kTileBytes;
       char* dst = base + W::wide_v + (t & 1) * (W::kTileBytes * 2);
       constexpr int kUnits = D / 16;
-#pragma unroll 1
+#pragma unroll
       for (int i0 = 0; i0 < kUnits; i0 += 4) {
         uint4 y[4];
 #pragma unroll
