@@ -36,7 +36,7 @@ constexpr float kMove = 32.f;   // weights stay below 2^32
 enum Bar {
   kKFull = 0, kKEmpty = kKFull + 4, kVFull = kKEmpty + 4, kVEmpty = kVFull + 4, kWideK = kVEmpty + 4, kWideKFree,
   kWideV, kWideVFree = kWideV + 2, kS = kWideVFree + 2, kP = kS + 2, kPV = kP + 2, kQ = kPV + 2, kOFree = kQ + 2, kJob = kOFree + 2,
-  kJobFree = kJob + kJobs, kBars = kJobFree + kJobs
+  kJobFree = kJob + kJobs, kQFree = kJobFree + kJobs, kBars
 };
 
 // Shared memory from a 1024-byte boundary on.
@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     }
     mbar_init(bar + kWideK, 4);
     mbar_init(bar + kWideKFree, 1);
+    mbar_init(bar + kQFree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar + kWideV + i, 4);
       mbar_init(bar + kWideVFree + i, 1);
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       }
       __syncwarp();
     };
-    auto scores = [&](int t, int h) {
+    auto scores = [&](int t, int h, bool last) {
       if (h == 0) hold(kWideK, t & 1);
       after_sync();
       if (elected()) {
@@ -237,6 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         }
         commit_to(bar + kS + h);
         if (h == halves - 1) commit_to(bar + kWideKFree);
+        if (h == halves - 1 && last) commit_to(bar + kQFree);
       }
       __syncwarp();
     };
@@ -249,14 +251,14 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         for (int h = 0; h < halves; ++h) {
           if (kApart) {
             if (i > 0) hold(kP + h, (tile - 1) & 1);   // the scores before have been read
-            scores(tile, h);
+            scores(tile, h, i + 1 == cnt);
             if (i > 0) sums(tile - 1, h, i == 1);
           } else {
             if (i > 0) {
               sums(tile - 1, h, i == 1);
               hold(kPV + h, (tile - 1) & 1);
             }
-            scores(tile, h);
+            scores(tile, h, i + 1 == cnt);
           }
         }
       }
@@ -421,18 +423,16 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int cnt = job.cnt;
       // the products of the group before have read its queries, and every warp
       // is done with what the rows of the group before that were
-      if (tile) hold(kWideKFree, (tile - 1) & 1);
+      // (of a barrier's phases a warp waits for each in turn, and the next is not
+      // over before the warp has done its part for it: a wait does not tell a
+      // phase from the next but one)
+      if (n) hold(kQFree, (n - 1) & 1);
       if (n > 1) hold(kJobFree + ((n - 2) & (kJobs - 1)), ((n - 2) / kJobs) & 1);
       queries(n, job);
       job_done(n);
       for (int i = 0; i < cnt; ++i, ++tile) {
-        if (warp < 8) {
-          keys(tile);
-        } else {
-          // every phase in turn: a wait does not tell one from the next but one
-          if (tile) hold(kWideKFree, (tile - 1) & 1);
-          values(tile);
-        }
+        if (warp < 8) keys(tile);
+        else values(tile);
       }
     }
   } else {
@@ -525,6 +525,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             tmem_st8(p_at + j * 8, w);
           }
           tmem_st_wait();
+        } else if (kApart && i > 0) {
+          hold(kPV + half, (tile - 1) & 1);
         }
         before_sync();
         __syncwarp();
