@@ -60,7 +60,7 @@ struct Params {
   float one = 1.f;
   int members = 1, nodes = 0;      // sequences of a group, and nodes of one
   float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
-  int worth = 0;                   // tokens that must be saved for the prefix to be attended to by itself
+  int64_t worth = 0;               // tokens that must be saved for the prefix to be attended to by itself
 };
 
 // The launches of attention over a shared prefix follow one another without a
@@ -293,6 +293,15 @@ __device__ __forceinline__ bool find(const State& s, const int32_t* seqs, const 
   return bad;
 }
 
+// Adds every thread's x to a sum in shared memory, a warp's at a time (64-bit
+// additions there are loops: one a thread took some 10 us of a call with 256
+// sequences).
+__device__ __forceinline__ void add_up(long long* to, long long x) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) x += __shfl_xor_sync(kFull, x, d);
+  if (x && (threadIdx.x & 31) == 0) atomicAdd(reinterpret_cast<unsigned long long*>(to), (unsigned long long)x);
+}
+
 // The plan, by all of the block's threads: seqs and the exclusive sums of
 // their tiles (kFine: of blocks of 16 slots, and kRestExtra), and zeros in the rows of nodes
 // that are not live.
@@ -316,10 +325,12 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
       }
     }
     __syncthreads();
+    long long saved = 0;
     for (int g = tid; g < p.a.B; g += blockDim.x)
-      if (seqs[g].end > 1) atomicAdd(reinterpret_cast<int*>(prefix), (seqs[g].end - 1) * seqs[g].len);
+      if (seqs[g].end > 1) saved += (seqs[g].end - 1ll) * seqs[g].len;
+    add_up(prefix, saved);
     __syncthreads();
-    const bool worth = *reinterpret_cast<const int*>(prefix) >= p.worth;
+    const bool worth = prefix[0] >= p.worth;
     for (int g = tid; g < p.a.B; g += blockDim.x) {
       const Seq<kPart> q = seqs[g];
       seqs[g] = worth && q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
@@ -343,14 +354,16 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
     if constexpr (kPart == kRest) {
       __syncthreads();
       // saved: for each live sequence what is shared, but once for a group
+      long long saved = 0;
       for (int b = tid; b < p.a.B; b += blockDim.x) {
         const int from = seqs[b / p.members * p.members].from;
         if (b % p.members) seqs[b].from = from;
         const int times = (seqs[b].live > 0) - (b % p.members == 0);
-        if (from != INT_MAX && times) atomicAdd(reinterpret_cast<int*>(prefix), times * from);
+        if (from != INT_MAX) saved += (long long)times * from;
       }
+      add_up(prefix, saved);
       __syncthreads();
-      if (*reinterpret_cast<const int*>(prefix) < p.worth)
+      if (prefix[0] < p.worth)
         for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = 0;
     }
   }

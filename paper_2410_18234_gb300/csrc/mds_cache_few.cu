@@ -15,7 +15,7 @@ cudaError_t configure() {
   return e;
 }
 
-// Rows of 16-bit queries beyond 16 go to the kernel of mds_cache_many.cu (which
+// Rows of 16-bit queries beyond 16 go to the kernel of mds_cache_many.cuh (which
 // has no second term for 32-bit queries).  Both kernels, in us: 64 sequences of
 // 500 to 2000 tokens with 32 heads, and 8 of 30000 to 60000 with 8:
 //    8 rows: here 222, there 228    144, 193

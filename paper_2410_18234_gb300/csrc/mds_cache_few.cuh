@@ -1,5 +1,5 @@
 // Attention of draft-tree nodes over the 8-bit paged cache, for few rows a
-// key/value head and for 32-bit queries; many rows: mds_cache_many.cu.
+// key/value head and for 32-bit queries; many rows: mds_cache_many.cuh.
 //
 //   o_i = sum_t w_it v_t / sum_t w_it,   w_it = 2^(c q_i . k_t - m_i),   c = scale * log2(e)
 //

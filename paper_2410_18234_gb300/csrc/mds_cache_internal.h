@@ -1,7 +1,6 @@
 // Internal interface of the key/value cache (declared in
 // include/mds_cache.h) between its entry points (mds_cache_api.cu) and its
-// kernels (mds_cache_pages.cu, mds_cache_rotary.cu, mds_cache_few.cu,
-// mds_cache_many.cu).
+// kernels (the other mds_cache_*.cu).
 #pragma once
 #include <cuda_runtime.h>
 
@@ -91,7 +90,7 @@ struct Shared {
   int members, nodes;
   bool prefix;     // the prefix's launch; else the rest's
   float* prior;
-  int worth;
+  int64_t worth;
 };
 // Rows of a tile of rows in the prefix's launch, by the kernel that it is.
 inline int even_rows(int64_t rows, int most) {   // as even as it goes

@@ -1,6 +1,6 @@
 // Attention of draft-tree nodes over the 8-bit paged cache where 17 or more
 // rows (nodes x query heads) share a key/value head: trees with shared heads,
-// chunks of prompts.  The mathematics is that of mds_cache_few.cu; the
+// chunks of prompts.  The mathematics is that of mds_cache_few.cuh; the
 // products run on the tensor cores with their accumulators in tensor memory.
 //
 // Transposed.  A tile of 128 slots meets up to 144 rows:

@@ -20,6 +20,12 @@
 // one float by rounding to odd (of the two floats around it the one whose last
 // bit is set), which a second rounding cannot tell from the sum itself.  What
 // is stored is the quantiser's answer on the exact rotation.
+//
+// What binds it.  Queries: memory.  4 prompts of 4099 tokens, 32 heads of 128,
+// bfloat16 (268 MB): 47 us, 5.7 TB/s, 84 % of a copy.  Keys and values: the
+// quantiser's instructions (half of the issue slots) and its registers.  256
+// trees of 33 nodes on 8 heads with 32 heads of queries (152 MB): 53 us, 2.9
+// TB/s; every key in two floats would take 12 us more.
 #include <cfloat>
 
 #include "mds_cache_quant.cuh"
@@ -345,6 +351,8 @@ __device__ __forceinline__ void fill(float (*table)[16 * P], const Turns& t, int
 // warp, like append's; those blocks come first, as they take longest).  It
 // starts its loads, fills a table of the rows' cosines and sines while they
 // are under way, and turns the heads by it.
+// Blocks an SM: queries 2, 3, 4 take 49, 49, 47 us on the prompts above; 16-bit
+// keys 2, 3 61 and 53 on the trees.
 template <typename T, int D, bool kStore, bool kI>
 __global__ void __launch_bounds__(kThreads, !kStore ? 4 : sizeof(T) * D <= 256 ? 3 : 2)
     rotary_kernel(const __grid_constant__ Call<T> p) {
@@ -592,7 +600,9 @@ cudaError_t launch(const State& s, const Rotate& a, cudaStream_t st) {
   p.L = a.L > 0 ? a.L : 1;
   p.chunks = a.k ? (a.n + 2 * kBlock - 2) / kBlock : (a.n + kBlock - 1) / kBlock;
   p.q_heads = a.heads;
-  // heads for which a table is filled: eight times a thread's 16 numbers
+  // heads for which a table is filled: eight times a thread's 16 numbers (2, 4
+  // and 8 times: 53, 47, 47 us on the prompts above, and 105, 92, 86 on
+  // the trees, an append and a read, before keys had three blocks an SM)
   const int rows = a.n < kBlock ? a.n : kBlock, each = 8 * kThreads / (D / 16) / rows;
   p.q_each = a.heads < each ? a.heads : each;
   p.kv_parts = a.k ? (2 * s.kv_heads + 7) / 8 : 0;

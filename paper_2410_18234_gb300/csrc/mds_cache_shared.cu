@@ -15,6 +15,12 @@ namespace cache {
 
 namespace {
 
+// Rows of a group up to which the prefix's launch is the transposed kernel for
+// many rows, which has them as columns, so that none are empty.  The wide one
+// has 128 rows a product, filled or not: at 32 rows (16 groups of 8 sequences
+// over 1500 to 12000 tokens) the call takes 131 us with the former and 185 with
+// the latter, at 32 rows of one group (8 over 4100) 37 and 43; at 1024 rows 253
+// and 206, at 576 rows of heads of 64 391 and 366.
 constexpr int kNarrow = 48;
 // Where the caller does not say, bytes of keys and values that must be saved
 // for prefixes to be attended to by themselves: less is over sooner without
@@ -30,7 +36,11 @@ constexpr int kNarrow = 48;
 //   rows 132: 16,           G 8,  4096        (112 MB)       137 /  95 /  78
 //             32,           G 32, 4096        (248 MB)       173 / 146 / 127
 // Weights, not bytes, bind rows of more than 16 a sequence; from about 100 on a
-// tile of rows is full without other sequences'.
+// tile of rows is full without other sequences'.  What is shared is known to
+// the device alone, and the call without sharing is still four launches: where
+// the tables have no room for savings at which mds_cache_attend falls behind
+// (kAloneFew: 37 us for 41 at 112 MB, 53 for 47 at 224), the host calls that.
+constexpr int64_t kAloneFew = 160 << 20;
 constexpr int64_t kWorthFew = 48 << 20, kWorthMany = 192 << 20;
 constexpr int kFullRows = 96;
 
@@ -126,9 +136,13 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
   const int64_t own = (int64_t)a.n * g;   // rows of one sequence
   const bool few_rows = s.dtype == MDS_F32 || own <= kFewRows;
   if (members < 2 || at_once == 0 || (least < 0 && !few_rows && own > kFullRows)) return attend(s, a, sms, st);
+  const int64_t alone = least < 0 && few_rows ? kAloneFew : 0;
   if (least < 0) least = few_rows ? kWorthFew : kWorthMany;
   const int64_t token = 2 * (int64_t)s.kv_heads * s.head_dim;
-  const int worth = (int)std::min<int64_t>((least + token - 1) / token, INT_MAX);
+  const int64_t worth = least / token + (least % token != 0);
+  // the most that the sequences' tables have room to share
+  const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
+  if (most < std::max(worth, alone / token)) return attend(s, a, sms, st);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
   for (int g0 = 0; g0 < groups; g0 += at_once) {
     const int some = groups - g0 < at_once ? groups - g0 : at_once, b0 = g0 * members;

@@ -179,9 +179,26 @@ def test_least_saved_is_an_exact_border():
     q = 0.02 * tokens(rng, 4, 1, 8, 64)       # weights that are spread over all tokens, so that the two ways differ
     seqs = ints([0, 1, 2, -1])
     c.reserve(seqs, 1)
-    a, b, never, always = (c.attend_shared(0, seqs, q, 4, least_saved=x) for x in (saved, saved + 256, 1 << 40, 0))
+    a, b, never, always = (c.attend_shared(0, seqs, q, 4, least_saved=x) for x in (saved, saved + 256, 2 * saved, 0))
     assert torch.equal(a, always) and torch.equal(b, never) and not torch.equal(a, b)
     assert (a.double() - b.double()).abs().max() <= 2.0 ** -7 * b.double().abs().max()
+
+
+def test_savings_that_no_table_has_room_for():
+    """Then, and by default in a small cache, the call is attend's."""
+    rng = np.random.default_rng(18)
+    c, m = both(60, 2, 64, 4, 12, 64)
+    grow(c, m, rng, [0], [300])
+    fork(c, m, [0, 0], [1, 2])
+    grow(c, m, rng, [0, 1, 2], [5, 40, 90])
+    q, seqs = 0.02 * tokens(rng, 4, 1, 8, 64), ints([0, 1, 2, -1])
+    c.reserve(seqs, 1)
+    room = 3 * 12 * 64 * 2 * 2 * 64           # bytes of three tables of 12 pages
+    want = c.attend(0, seqs, q)
+    for least in (None, room + 1, 1 << 40, 1 << 80):
+        assert torch.equal(c.attend_shared(0, seqs, q, 4, least_saved=least), want)
+    o = c.attend_shared(0, seqs, q, 4, least_saved=room)
+    assert (o.double() - want.double()).abs().max() <= 2.0 ** -7 * want.double().abs().max()
 
 
 @pytest.mark.parametrize("G", [2, 17, 100])
