@@ -22,10 +22,10 @@ namespace {
 // the latter, at 32 rows of one group (8 over 4100) 37 and 43; at 1024 rows 253
 // and 206, at 576 rows of heads of 64 391 and 366.
 constexpr int kNarrow = 48;
-// Where the caller does not say, bytes of keys and values that must be saved
-// for prefixes to be attended to by themselves: less is over sooner without
-// the prefix's launch.  In us, shared / not (this call) / mds_cache_attend, 32
-// heads on 8 of 128 dimensions, G sequences a group:
+// Where the caller does not say, prefixes are attended to by themselves where
+// that pays: less is over sooner without the prefix's launch.  In us, shared /
+// not (this call) / mds_cache_attend, 32 heads on 8 of 128 dimensions, G
+// sequences a group:
 //   rows 4:    8 sequences, G 8,  4096 tokens ( 56 MB saved)  39 /  39 /  29
 //              2,           G 2, 32768        ( 64 MB)        47 /  61 /  39
 //              8,           G 8,  8192        (112 MB)        41 /  49 /  37
@@ -35,14 +35,35 @@ constexpr int kNarrow = 48;
 //              8,           G 8,  8192        (112 MB)        68 /  63 /  52
 //   rows 132: 16,           G 8,  4096        (112 MB)       137 /  95 /  78
 //             32,           G 32, 4096        (248 MB)       173 / 146 / 127
-// Weights, not bytes, bind rows of more than 16 a sequence; from about 100 on a
-// tile of rows is full without other sequences'.  What is shared is known to
-// the device alone, and the call without sharing is still four launches: where
-// the tables have no room for savings at which mds_cache_attend falls behind
-// (kAloneFew: 37 us for 41 at 112 MB, 53 for 47 at 224), the host calls that.
-constexpr int64_t kAloneFew = 160 << 20;
+// So many bytes must be saved, by the rows of a sequence (few, many).
 constexpr int64_t kWorthFew = 48 << 20, kWorthMany = 192 << 20;
+// Weights, not bytes, bind rows of more than 16 a sequence, and a row's sums
+// over the prefix are written and read again, whatever its length: of more than
+// 8 rows a sequence each takes so many tokens saved.  Shared / attend, at
+// tokens saved a sequence:
+//   rows 20: 3072 152 / 166, 3840  83 /  91
+//   rows 36: 3072 164 / 166, 3840  99 /  92, 7680 125 / 152
+//   rows 72: 3072 257 / 196, 7680 175 / 176, 15360 251 / 308
+//   rows 80: 6144 384 / 333, 7680 178 / 175, 15360 254 / 309
+//   rows 92: 3072 269 / 199, 7680 196 / 176
+constexpr int64_t kWorthRow = 100;
+// From about 100 rows on a tile of rows is full without other sequences'.
 constexpr int kFullRows = 96;
+// So are tiles of 8 or 16 rows of 32-bit queries, which the prefix's launch
+// takes too, from three quarters on.  32 sequences over 16384 tokens: 1 row 61 /
+// 201, 4 rows 117 / 201, 8 rows 195 / 203, 9 rows 220 / 337, 12 rows 281 / 337,
+// 16 rows 359 / 338, 36 rows 789 / 979; 64 over 4096: 8 rows 136 / 125, 12 rows
+// 189 / 197, 16 rows 234 / 199.
+bool full_rows(int dtype, int64_t own) {
+  if (dtype != MDS_F32) return own > kFullRows;
+  const int64_t tiles = own <= 8 ? 8 : (own + 15) / 16 * 16;
+  return 4 * own > 3 * tiles;
+}
+// What is shared is known to the device alone, and the call without sharing is
+// still four launches: where the tables have no room for savings at which
+// mds_cache_attend falls behind (few rows: 37 us for 41 at 112 MB, 53 for 47 at
+// 224), the host calls that.
+constexpr int64_t kAloneFew = 160 << 20;
 
 // One block of threads a sequence: the tokens that it shares with the first
 // live sequence of its group (none if it is the only one), and its live nodes.
@@ -135,14 +156,15 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
   const int at_once = (int)(((int64_t)kPartFloats - kPieceFloats) / row);
   const int64_t own = (int64_t)a.n * g;   // rows of one sequence
   const bool few_rows = s.dtype == MDS_F32 || own <= kFewRows;
-  if (members < 2 || at_once == 0 || (least < 0 && !few_rows && own > kFullRows)) return attend(s, a, sms, st);
-  const int64_t alone = least < 0 && few_rows ? kAloneFew : 0;
-  if (least < 0) least = few_rows ? kWorthFew : kWorthMany;
+  const bool choose = least < 0;
+  if (members < 2 || at_once == 0 || (choose && full_rows(s.dtype, own))) return attend(s, a, sms, st);
+  if (choose) least = few_rows ? kWorthFew : kWorthMany;
   const int64_t token = 2 * (int64_t)s.kv_heads * s.head_dim;
-  const int64_t worth = least / token + (least % token != 0);
+  const int64_t worth = least / token + (least % token != 0);   // tokens
+  const int64_t each = choose && own > 8 ? kWorthRow * own : 0;    // of each sequence
   // the most that the sequences' tables have room to share
   const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
-  if (most < std::max(worth, alone / token)) return attend(s, a, sms, st);
+  if (most < std::max({worth, each * a.B, choose && few_rows ? kAloneFew / token : 0})) return attend(s, a, sms, st);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
   for (int g0 = 0; g0 < groups; g0 += at_once) {
     const int some = groups - g0 < at_once ? groups - g0 : at_once, b0 = g0 * members;
@@ -156,7 +178,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
     y.B = some;
     y.n = a.n * members;
     y.L = y.n - 1;
-    Shared z{members, a.n, true, s.part + kPieceFloats, worth};
+    Shared z{members, a.n, true, s.part + kPieceFloats, std::max(worth, each * x.B)};
     const int64_t rows = (int64_t)y.n * g;
     const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
     Params p{s, y, 0, g, (int)rows, 0, 0, 0};
