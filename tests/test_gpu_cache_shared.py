@@ -68,7 +68,7 @@ def check(c, m, rng, seqs, G, Hq, K, L, dtype="bf16", counts=None, only=None, fa
           least=0):
     """One call on a new tree of every sequence."""
     n = 1 + K * L
-    real = [q for q in seqs if q >= 0]
+    real = sorted({q for q in seqs if q >= 0})
     if real:
         grow(c, m, rng, real, [n] * len(real), dtype, keep=False)
     x = factor * tokens(rng, len(seqs), n, Hq + 1, m.D, dtype=dtype)
@@ -199,6 +199,21 @@ def test_savings_that_no_table_has_room_for():
         assert torch.equal(c.attend_shared(0, seqs, q, 4, least_saved=least), want)
     o = c.attend_shared(0, seqs, q, 4, least_saved=room)
     assert (o.double() - want.double()).abs().max() <= 2.0 ** -7 * want.double().abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,L", [(1, 0), (2, 1), (3, 2), (1, 8)])
+def test_the_default_in_long_tables_and_a_sequence_twice(K, L, dtype):
+    """Tables with room for any savings, so that the device decides (against
+    sharing 256 tokens); the same sequence at several places of a group, and of
+    two groups, is attended to at each, shared or not."""
+    rng = np.random.default_rng(K + 10 * L)
+    c, m = both(60, 2, 128, 8, 4096, 128, dtype)
+    grow(c, m, rng, [0], [300], dtype)
+    fork(c, m, [0, 0], [1, 2])
+    grow(c, m, rng, [0, 1, 2], [5, 40, 90], dtype)
+    for least in (None, 0):
+        check(c, m, rng, [0, 1, 1, 2, 0, 2, -1, 0], 4, 8, K, L, dtype, least=least)
 
 
 @pytest.mark.parametrize("G", [2, 17, 100])
