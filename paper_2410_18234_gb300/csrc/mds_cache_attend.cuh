@@ -164,6 +164,11 @@ __device__ __forceinline__ void wait(uint64_t* bar, unsigned parity, int* abort)
     }
   }
 }
+// Whether the block gave up, the same answer for a warp's lanes: a loader then
+// starts no more copies, as their places may still be written or read.
+__device__ __forceinline__ bool gave_up(const int* abort) {
+  return __any_sync(kFull, *reinterpret_cast<const volatile int*>(abort));
+}
 // By the thread that started the copies: whether the block gave up; then it
 // leaves the copies in flight time to land before the block ends.
 __device__ __noinline__ void report(int* abort, uint32_t* status) {

@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         const int next = page_of(i + 1);
         const int t = tile_slot(grp, i) + blk * kBlock;
         wait(empty + stage, phase, abort);
+        if (gave_up(abort)) break;
         const bool copies = page >= 0 && (t & (p.span - 1)) == 0;   // the first block of its span
         const unsigned takes = __ballot_sync(kFull, copies);
         if (lane == 0) mbar_expect_tx(full + stage, __popc(takes) * p.span * D);

@@ -236,6 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         const unsigned takes = __ballot_sync(kFull, copies);
         const int64_t row = (((layer0 + page) * 2 + kv) * s.kv_heads + h) * s.page_tokens + r;
         hold(empty + slot, parity);
+        if (gave_up(abort)) break;
         if (lane == 0) mbar_expect_tx(bar + full + slot, __popc(takes) * p.span * D);
         __syncwarp();
         if (page >= 0) {

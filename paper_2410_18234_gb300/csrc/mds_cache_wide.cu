@@ -198,6 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const int64_t row = (((layer0 + page) * 2 + kv) * s.kv_heads + h) * s.page_tokens +
                             ((i * kTile + blk * kBlock) & (s.page_tokens - 1));
         hold(empty + slot, parity);
+        if (gave_up(abort)) break;
         if (lane == 0) mbar_expect_tx(bar + full + slot, W::kTileBytes);
         __syncwarp();
         if (page >= 0) {
