@@ -39,13 +39,13 @@ constexpr int kNarrow = 48;
 constexpr int64_t kWorthFew = 48 << 20, kWorthMany = 192 << 20;
 // Weights, not bytes, bind rows of more than 16 a sequence, and a row's sums
 // over the prefix are written and read again, whatever its length: of more than
-// 8 rows a sequence each takes so many tokens saved.  Shared / attend, at
-// tokens saved a sequence:
-//   rows 20: 3072 152 / 166, 3840  83 /  91
-//   rows 36: 3072 164 / 166, 3840  99 /  92, 7680 125 / 152
-//   rows 72: 3072 257 / 196, 7680 175 / 176, 15360 251 / 308
-//   rows 80: 6144 384 / 333, 7680 178 / 175, 15360 254 / 309
-//   rows 92: 3072 269 / 199, 7680 196 / 176
+// 8 rows a sequence each takes so many tokens saved.  Shared / attend, of 64
+// sequences in groups of 4 (a) and 32 in groups of 16 (b), by prefix:
+//   rows 20: a 4096  152 / 166, b 4096  83 /  91
+//   rows 36: a 4096  164 / 166, b 4096  99 /  92, 8192 125 / 152
+//   rows 72: a 4096  257 / 196, b 8192 175 / 176, 16384 251 / 308
+//   rows 80: a 8192  384 / 333, b 8192 178 / 175, 16384 254 / 309
+//   rows 92: a 4096  269 / 199, b 8192 196 / 176
 constexpr int64_t kWorthRow = 100;
 // From about 100 rows on a tile of rows is full without other sequences'.
 constexpr int kFullRows = 96;
