@@ -135,8 +135,8 @@ int mds_cache_reserve(mds_cache* cache, const int32_t* seqs, const int32_t* coun
  * of each sequence, as far as they are reserved (MDS_ST_BADSEQ where not, or
  * where their page is shared).  k and v are dtype: the element of
  * sequence b of the list, token i, head h and dimension d is at
- * b * strides[0] + i * strides[1] + h * strides[2] + d, strides in elements,
- * multiples of 16 bytes, the bases aligned to 16 bytes (MDS_EINVAL
+ * b * strides[0] + i * strides[1] + h * strides[2] + d, strides in elements
+ * (of either sign), multiples of 16 bytes, the bases aligned to 16 bytes (MDS_EINVAL
  * otherwise). */
 int mds_cache_append(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* k,
                      const int64_t* k_strides, const void* v, const int64_t* v_strides, int n, int B, void* stream);

@@ -449,15 +449,17 @@ __device__ __forceinline__ float* piece_of(const Params& p, int block, bool begi
 }
 
 // Where node `node` of sequence b of the list (kPrefix: of group b) has its
-// queries, from the call's first; -1 for a node that is not live.
+// queries, from the call's first, which strides below 0 put behind it; kNowhere
+// for a node that is not live.
+constexpr int64_t kNowhere = INT64_MIN;
 template <int kPart>
 __device__ __forceinline__ int64_t query_at(const Params& p, int b, int node, int live) {
   if constexpr (kPart == kPrefix) {
-    if (node >= live) return -1;
+    if (node >= live) return kNowhere;
     const int m = b * p.members + node / p.nodes, i = node % p.nodes;
-    return i < __ldg(p.s.share + m).y ? m * p.a.q_seq + i * p.a.q_tok : -1;
+    return i < __ldg(p.s.share + m).y ? m * p.a.q_seq + i * p.a.q_tok : kNowhere;
   } else {
-    return node < live ? b * p.a.q_seq + node * p.a.q_tok : -1;
+    return node < live ? b * p.a.q_seq + node * p.a.q_tok : kNowhere;
   }
 }
 

@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
       const int row = row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
       float x[4] = {0.f, 0.f, 0.f, 0.f};
       const int64_t from = query_at<kPart>(p, job.b, node, job.live);
-      if (lane * 4 < D && from >= 0) {
+      if (lane * 4 < D && from != kNowhere) {
         const T* src = static_cast<const T*>(p.a.q) + from + head * p.a.q_head + lane * 4;
         if constexpr (sizeof(T) == 4) {
           const float4 y = __ldg(reinterpret_cast<const float4*>(src));
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
         }
         if (tid < 256) {
           const int r = tid >> 5, d = lane * 2, row = row0 + m * 8 + r;
-          if (kPart == kPrefix ? query_at<kPart>(p, job.b, row / p.g, job.live) >= 0 : row / p.g < job.live) {
+          if (kPart == kPrefix ? query_at<kPart>(p, job.b, row / p.g, job.live) != kNowhere : row / p.g < job.live) {
             float2 o{0.f, 0.f}, po{0.f, 0.f}, pl{kNone, 0.f};   // the prefix's sums, reference and normaliser
             if (kPart == kRest && whole && prior) {
               const float* pr = prior_of<D>(p, row_at(p, job.b, job.h, row));

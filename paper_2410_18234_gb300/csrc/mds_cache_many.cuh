@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         for (int r = lane; r < p.rows_per; r += 32) {
           const int row = job.row0 + r, node = row / p.g;
           const int64_t from = query_at<kPart>(p, job.b, node, job.live);
-          if (from >= 0) {
+          if (from != kNowhere) {
             const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.a.q) + from + (h * p.g + row - node * p.g) * p.a.q_head;
             asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
             if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
@@ -345,12 +345,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       asm volatile("bar.sync 5, 128;" ::: "memory");
       for (int r = wt; r < N; r += 128) {
         const int row = job.row0 + r, node = row / p.g, head = job.h * p.g + row - node * p.g;
-        const int64_t from = r < p.rows_per ? query_at<kPart>(p, job.b, node, job.live) : -1;
-        const bool live = from >= 0;
+        const int64_t from = r < p.rows_per ? query_at<kPart>(p, job.b, node, job.live) : kNowhere;
+        const bool live = from != kNowhere;
         const int own = node > 0 && p.a.L > 0 ? 1 + (node - 1) / p.a.L * p.a.L : 1;
         rows[r] = Row{own, node > 0 ? node - own + 1 : 0,
                       live ? (((int64_t)job.b * p.a.n + node) * p.a.heads + head) * D : -1};
-        q_at[r] = live ? from + head * p.a.q_head : -1;
+        q_at[r] = live ? from + head * p.a.q_head : kNowhere;
       }
       asm volatile("bar.sync 5, 128;" ::: "memory");
       // each warp copies its rows (16 bytes a lane), then scales them in place
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         const int r = r0 + lane / kUnits, unit = lane % kUnits;
         const int64_t from = q_at[r];
         char* dst = to + (unit >> 3) * N * 128 + r * 128 + (((unit & 7) ^ (r & 7)) << 4);
-        if (from >= 0)
+        if (from != kNowhere)
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(q + from + unit * 8) : "memory");
         else
           *reinterpret_cast<uint4*>(dst) = uint4{0, 0, 0, 0};

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   after_launch_before();
   if (r >= p.rows_per || row >= p.rows) return;
   const int2 cut = *reinterpret_cast<const int2*>(prior_of<D>(p, row_at(p, b, h, rt * p.rows_per)) + 2);
-  if (cut.x < 0 || query_at<kPrefix>(p, b, row / p.g, p.a.n) < 0) return;
+  if (cut.x < 0 || query_at<kPrefix>(p, b, row / p.g, p.a.n) == kNowhere) return;
   const int64_t stride = 2 * (int64_t)p.rows_per * R;
   const float* first = piece_of<D>(p, cut.x, true) + r * R;
   const float* later = piece_of<D>(p, cut.x, false) + r * R;   // + stride for each block further

@@ -378,9 +378,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         const int r = r0 + lane, h = r >> 7, in = r & (kHalf - 1);
         const int row = job.row0 + (h ? half0 + in : in), node = row / p.g, head = job.h * p.g + row - node * p.g;
         const bool mine = h ? half0 + in < p.rows_per : in < min(half0, p.rows_per);
-        const int64_t from = mine ? query_at<kPrefix>(p, job.b, node, job.live) : -1;
-        out[r] = from >= 0 ? (int)row_at(p, job.b, job.h, row) : -1;   // `prior` has fewer than 2^18 rows
-        const int64_t from_row = from >= 0 ? from + head * p.a.q_head : -1;
+        const int64_t from = mine ? query_at<kPrefix>(p, job.b, node, job.live) : kNowhere;
+        out[r] = from != kNowhere ? (int)row_at(p, job.b, job.h, row) : -1;   // `prior` has fewer than 2^18 rows
+        const int64_t from_row = from != kNowhere ? from + head * p.a.q_head : kNowhere;
         // its copies: 16 bytes a lane, kAtOnce rows at a time
 #pragma unroll 4
         for (int i = 0; i < 32; i += kAtOnce) {
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           const int64_t src = __shfl_sync(kFull, from_row, x);
           char* dst = base + W::q + (rr >> 7) * (kHalf * D * 2) + (unit >> 3) * (kHalf * 128) + (rr & 127) * 128 +
                       (((unit & 7) ^ (rr & 7)) << 4);
-          if (src >= 0)
+          if (src != kNowhere)
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(q + src + unit * 8) : "memory");
           else
             *reinterpret_cast<uint4*>(dst) = uint4{0, 0, 0, 0};
