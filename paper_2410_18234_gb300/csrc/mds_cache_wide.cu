@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             after_sync();
           }
           if (i == 0) {
-            ref = top > kNone ? top : 0.f;
+            ref = top;   // kNone where no score is finite: a later tile's moves it, and what it leaves weighs nothing
           } else if (__any_sync(kFull, top > ref + kMove)) {
             // the sums so far follow; O of the tiles before is complete
             const bool moves = top > ref + kMove;
