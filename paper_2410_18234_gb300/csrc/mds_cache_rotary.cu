@@ -537,8 +537,11 @@ __global__ void __launch_bounds__(kThreads, !kStore ? 4 : sizeof(T) * D <= 256 ?
     float inv;
     const float scale = block_scale(exact ? known : max(known, most), &inv);
     if (lane == 0) *scale_at = scale;
+    // Beside numbers that do not turn a small magnitude puts the error's factor
+    // below the normal floats, where it would be rounded itself, or times a sum
+    // |a| + |b| that is not finite no number at all: then all are computed exactly.
     const float off = inv * p.t.magnitude.x * 0x1p-21f;
-    unsigned unsure = exact ? (1u << (2 * kPasses)) - 1u : 0u;
+    unsigned unsure = exact || off < FLT_MIN ? (1u << (2 * kPasses)) - 1u : 0u;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
       if (i * kRows >= to) break;

@@ -1,0 +1,68 @@
+"""Rotated keys at the ends of the floats' range: stored like the quantiser's
+answer on the rotation in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA GPU", allow_module_level=True)
+
+from cache_model import quantise  # noqa: E402
+from paper_2410_18234_gb300 import cache  # noqa: E402
+from test_gpu_cache_rotary import DEV, DT, ints, turned, wide  # noqa: E402
+
+
+def stored(k, r, interleaved=False):
+    """What the cache holds of keys [n][H][D] from position 0 on, and what it should."""
+    n, H, D = k.shape
+    c = cache.Cache(1, -(-n // 128) + 1, H, D, 1, -(-n // 128) + 1, page_tokens=128,
+                    dtype="f32" if k.dtype == torch.float32 else "bf16")
+    c.reserve(ints([0]), n)
+    c.append_rotated(0, ints([0]), k[None], torch.zeros_like(k[None]), r)
+    got = wide(c.read(0, ints([0]), None, n)[0][0])
+    new = turned(wide(k), np.arange(n), r.freqs, r.struct.dim, interleaved, r.struct.magnitude)[0]
+    want = np.concatenate([np.stack([quantise(new[t:t + 16, h]) for h in range(H)], 1) for t in range(0, n, 16)])
+    return got, want, c.status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("magnitude", [2.0 ** -9, 2.0 ** -10, 2.0 ** -12, 2.0 ** -20])
+def test_pairs_of_the_largest_numbers_beside_large_ones(magnitude, interleaved, dtype):
+    """|a| + |b| passes the largest float, and the block's step is decided by a
+    number that does not turn: every stored number is finite and right."""
+    rng = np.random.default_rng(4)
+    k = rng.standard_normal((16, 2, 128)) * 2.0 ** 100
+    k[:, :, :64] = rng.choice([-1.0, 1.0], (16, 2, 64)) * rng.uniform(0.8, 0.99, (16, 2, 64)) * 2.0 ** 128
+    k[3, :, 100] = 2.75e38
+    k = torch.tensor(k, device=DEV).to(DT[dtype])
+    assert torch.isfinite(k).all()
+    got, want, status = stored(k, cache.Rotary(64, magnitude=magnitude, interleaved=interleaved), interleaved)
+    assert status == (0, "ok") and np.isfinite(got).all()
+    np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("magnitude", [2.0 ** -9, 2.0 ** -10, 2.0 ** -11])
+def test_borders_beside_large_numbers(magnitude):
+    """Rotated numbers within 2^-23 of themselves of a border of the rounding,
+    on either side, closer than 32-bit rotations tell: the exact ones decide."""
+    rng = np.random.default_rng(5)
+    n, H, top = 512, 2, 2.0 ** 119                       # the block's step: 1 is 2^119
+    r = cache.Rotary(64, magnitude=magnitude)
+    c, s = (turned(np.broadcast_to(x, (n, 1, 128)), np.arange(n), r.freqs, 64, False, magnitude)[0][:, 0, :32]
+            for x in ((np.arange(128) < 32) * 1.0, (np.arange(128) // 32 == 1) * -1.0))
+    k = np.zeros((n, H, 128))
+    # of pair (a, b) the first becomes a c - b s: halfway between two numbers of four bits
+    border = rng.choice([-1, 1], (n, H, 32)) * (rng.integers(8, 16, (n, H, 32)) + 0.5) / 8 * 2.0 ** rng.integers(-6, -4, (n, H, 32)) * top
+    b = rng.standard_normal((n, H, 32)) * 0.004 * top / magnitude
+    b = b.astype(np.float32).astype(float)
+    a = (border + b * s[:, None]) / np.where(np.abs(c) > 0.4 * magnitude, c, 1e9)[:, None]
+    k[..., :32], k[..., 32:64] = a, b
+    k[::16, :, 127] = 2.9e38
+    k = torch.tensor(k, device=DEV).float()
+    assert torch.isfinite(k).all()
+    got, want, status = stored(k, r)
+    assert status == (0, "ok")
+    np.testing.assert_array_equal(got, want)
