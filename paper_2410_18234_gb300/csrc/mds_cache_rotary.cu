@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, !kStore ? 4 : sizeof(T) * D <= 256 ?
     // Beside numbers that do not turn a small magnitude puts the error's factor
     // below the normal floats, where it would be rounded itself, or times a sum
     // |a| + |b| that is not finite no number at all: then all are computed exactly.
-    const float off = inv * p.t.magnitude.x * 0x1p-21f;
+    const float off = inv * (p.t.magnitude.x * 0x1p-21f);   // in this order not infinite
     unsigned unsure = exact || off < FLT_MIN ? (1u << (2 * kPasses)) - 1u : 0u;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {

@@ -66,3 +66,15 @@ def test_borders_beside_large_numbers(magnitude):
     got, want, status = stored(k, r)
     assert status == (0, "ok")
     np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pairs_of_zeros_among_the_least_numbers(dtype):
+    """The largest step's inverse, 2^117, times a magnitude of 2^20 passes the
+    largest float; pairs of zeros stay zeros."""
+    rng = np.random.default_rng(7)
+    k = rng.choice([0.0, 2.0 ** -133, -(2.0 ** -132)], (32, 2, 64))
+    k[:, :, 8:16] = k[:, :, 24:32] = 0.0
+    got, want, status = stored(torch.tensor(k, device=DEV).to(DT[dtype]), cache.Rotary(32, magnitude=1.9 * 2.0 ** 19))
+    assert status == (0, "ok")
+    np.testing.assert_array_equal(got, want if dtype == "f32" else wide(torch.tensor(want).bfloat16()))
