@@ -258,10 +258,14 @@ struct Rows {
   bool key;
 };
 
-// The numbers of quad q of row r, turned to floats rounded to odd; 0 for what
-// is no number.  Whether any is not finite.
+// The numbers of quad q of row r times 2^shift, turned to floats rounded to odd;
+// 0 for what is no number.  Whether any is not finite.  A pair is turned with
+// its larger number brought to [1, 2) by a power of two (the largest and the
+// least floats to within 2^24 of that): no product passes the largest float
+// where the rotation does not, and none leaves a rest below the least.
 template <typename T, int D, bool kI>
-__device__ bool exact_quad(const Rows<T>& w, const Lane<D / 16, kI>& at, int r, int q, float* x) {
+__device__ bool exact_quad(const Rows<T>& w, const Lane<D / 16, kI>& at, int r, int q, int shift, float* x) {
+  auto power = [](int e) { return __uint_as_float((unsigned)(127 + min(max(e, -126), 127)) << 23); };
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int word = word_of<kI>(q, half), d = (word < 2 ? at.first : at.second) * 8 + (word & 1) * 4;
@@ -276,10 +280,16 @@ __device__ bool exact_quad(const Rows<T>& w, const Lane<D / 16, kI>& at, int r, 
       turn_cos_sin(w.t->turn[at.pair(4 * q + i)] * (uint64_t)(w.position + depth_of(w.node0 + r, w.L)), c, s);
       c = product(c, w.t->magnitude);
       s = product(s, w.t->magnitude);
-      const float y = odd_sum(a, c.x, c.y, -b, s.x, s.y);
-      b = odd_sum(a, s.x, s.y, b, c.x, c.y);
+      const int e = min(max((int)(__float_as_uint(fmaxf(fabsf(a), fabsf(b))) >> 23), 1), 253) - 127;
+      // beyond the powers there are, a number is stored as 0 or the largest either way
+      const float down = power(-e), up = power(e + shift);
+      a *= down, b *= down;
+      const float y = odd_sum(a, c.x, c.y, -b, s.x, s.y) * up;
+      b = odd_sum(a, s.x, s.y, b, c.x, c.y) * up;
       a = y;
     }
+  } else {
+    for (int i = 0; i < 8; ++i) x[i] *= power(shift);
   }
   bool odd = false;
   for (int i = 0; i < 8; ++i) {
@@ -302,7 +312,7 @@ __device__ __noinline__ unsigned exact_largest(const Rows<T>& w, int lane) {
     for (int q = 0; q < 2; ++q) {
       if (r < w.from) continue;
       float x[8];
-      odd = exact_quad<T, D, kI>(w, at, r, q, x) || odd;
+      odd = exact_quad<T, D, kI>(w, at, r, q, 0, x) || odd;
       for (int i = 0; i < 8; ++i) {
         const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu;
         m = max(m, a >= kInf ? 0u : a);
@@ -315,17 +325,18 @@ template <typename T, int D, bool kI>
 __device__ __noinline__ void exact_store(const Rows<T>& w, int lane, unsigned mask, float inv) {
   constexpr int U = D / 16;
   const Lane<U, kI> at(*w.t, lane % U);
+  const int shift = (int)(__float_as_uint(inv) >> 23) - 127;
 #pragma unroll 1
   for (; mask; mask &= mask - 1) {
     const int bit = __ffs(mask) - 1, r = (bit >> 1) * (32 / U) + lane / U, q = bit & 1;
     if (r < w.from || r >= w.to) continue;
     float x[8];
-    exact_quad<T, D, kI>(w, at, r, q, x);
+    exact_quad<T, D, kI>(w, at, r, q, shift, x);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int word = word_of<kI>(q, half), d = (word < 2 ? at.first : at.second) * 8 + (word & 1) * 4;
       *reinterpret_cast<unsigned*>(w.base + swizzled(r * D + d)) =
-          encode4(x[4 * half] * inv, x[4 * half + 1] * inv, x[4 * half + 2] * inv, x[4 * half + 3] * inv);
+          encode4(x[4 * half], x[4 * half + 1], x[4 * half + 2], x[4 * half + 3]);
     }
   }
 }

@@ -1,5 +1,7 @@
 """Rotated keys at the ends of the floats' range: stored like the quantiser's
 answer on the rotation in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -12,6 +14,8 @@ if not torch.cuda.is_available():
 from cache_model import quantise  # noqa: E402
 from paper_2410_18234_gb300 import cache  # noqa: E402
 from test_gpu_cache_rotary import DEV, DT, ints, turned, wide  # noqa: E402
+
+LARGEST = float(np.finfo(np.float32).max)
 
 
 def stored(k, r, interleaved=False):
@@ -76,5 +80,45 @@ def test_pairs_of_zeros_among_the_least_numbers(dtype):
     k = rng.choice([0.0, 2.0 ** -133, -(2.0 ** -132)], (32, 2, 64))
     k[:, :, 8:16] = k[:, :, 24:32] = 0.0
     got, want, status = stored(torch.tensor(k, device=DEV).to(DT[dtype]), cache.Rotary(32, magnitude=1.9 * 2.0 ** 19))
+    assert status == (0, "ok")
+    np.testing.assert_array_equal(got, want if dtype == "f32" else wide(torch.tensor(want).bfloat16()))
+
+
+def test_products_beyond_the_largest_float_whose_sums_are_not():
+    """magnitude * a * cos is 1.05 of the largest float, the two rotated
+    numbers are 7/8 of it, where the step's size is decided."""
+    turn, to = math.radians(25), math.radians(20)
+    r = cache.Rotary(16, freqs=[turn] * 8, magnitude=2.0)
+    k = torch.zeros(2, 1, 64, device=DEV)
+    size = math.sqrt(2) * 448 * 2.0 ** 119 / 2
+    k[1, 0, 0], k[1, 0, 8], k[0, 0, 30] = size * math.cos(to), size * math.sin(to), 1e37
+    assert 2 * float(k[1, 0, 0]) * math.cos(turn) > LARGEST
+    got, want, status = stored(k, r)
+    assert status == (0, "ok")
+    np.testing.assert_array_equal(got, want)
+    assert got[1, 0, 0] == got[1, 0, 8] == 448 * 2.0 ** 119
+
+
+def test_rests_of_products_below_the_smallest_float():
+    """(1 + 2^-30) * 2^-127 lies above the border between 0 and the least
+    stored number, by less than a float this small can say."""
+    r = cache.Rotary(16, magnitude=1 + 2.0 ** -30)
+    k = torch.zeros(1, 1, 64, device=DEV)
+    k[0, 0, 3], k[0, 0, 12], k[0, 0, 40] = 2.0 ** -127, -(2.0 ** -127), 2.0 ** -125
+    got, want, status = stored(k, r)
+    assert status == (0, "ok") and want[0, 0, 3] == 2.0 ** -126
+    np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("magnitude", [2.0 ** -20, 1.1875, 1.9 * 2.0 ** 19])
+def test_blocks_of_every_size(magnitude, dtype):
+    """From the least floats to rotations of the largest."""
+    rng = np.random.default_rng(6)
+    n = 16 * 140
+    most = min(126.0, 125 - math.log2(magnitude))
+    size = np.repeat(np.linspace(-149, most - 4, n // 16), 16)[:, None, None]
+    k = np.clip(rng.standard_normal((n, 2, 64)), -8, 8) * 2.0 ** size * 2.0 ** rng.uniform(-6, 0, (n, 2, 1))
+    got, want, status = stored(torch.tensor(k, device=DEV).to(DT[dtype]), cache.Rotary(48, magnitude=magnitude))
     assert status == (0, "ok")
     np.testing.assert_array_equal(got, want if dtype == "f32" else wide(torch.tensor(want).bfloat16()))
