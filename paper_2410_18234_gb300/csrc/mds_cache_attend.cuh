@@ -60,7 +60,7 @@ struct Params {
   float one = 1.f;
   int members = 1, nodes = 0;      // sequences of a group, and nodes of one
   float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
-  int64_t worth = 0;               // tokens that must be saved for the prefix to be attended to by itself
+  int64_t worth = 0, each = 0;     // tokens that must be saved, in all and a live sequence, for the prefix to be attended to by itself
 };
 
 // The launches of attention over a shared prefix follow one another without a
@@ -307,6 +307,14 @@ __device__ __forceinline__ void add_up(long long* to, long long x) {
   if (x && (threadIdx.x & 31) == 0) atomicAdd(reinterpret_cast<unsigned long long*>(to), (unsigned long long)x);
 }
 
+// What decides whether prefixes are attended to by themselves, in one number:
+// tokens saved (at most 2^30), and live sequences above.
+constexpr int kLiveShift = 40;
+__device__ __forceinline__ bool worth_it(const Params& p, long long x) {
+  const long long saved = x & ((1ll << kLiveShift) - 1), live = x >> kLiveShift;
+  return saved >= p.worth && saved >= p.each * live;
+}
+
 // The plan, by all of the block's threads: seqs and the exclusive sums of
 // their tiles (kFine: of blocks of 16 slots, and kRestExtra), and zeros in the rows of nodes
 // that are not live.
@@ -332,10 +340,10 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
     __syncthreads();
     long long saved = 0;
     for (int g = tid; g < p.a.B; g += blockDim.x)
-      if (seqs[g].end > 1) saved += (seqs[g].end - 1ll) * seqs[g].len;
+      if (seqs[g].end > 0) saved += (seqs[g].end - 1ll) * seqs[g].len + ((long long)seqs[g].end << kLiveShift);
     add_up(prefix, saved);
     __syncthreads();
-    const bool worth = prefix[0] >= p.worth;
+    const bool worth = worth_it(p, prefix[0]);
     for (int g = tid; g < p.a.B; g += blockDim.x) {
       const Seq<kPart> q = seqs[g];
       seqs[g] = worth && q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
@@ -365,10 +373,11 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
         if (b % p.members) seqs[b].from = from;
         const int times = (seqs[b].live > 0) - (b % p.members == 0);
         if (from != INT_MAX) saved += (long long)times * from;
+        if (seqs[b].live > 0) saved += 1ll << kLiveShift;
       }
       add_up(prefix, saved);
       __syncthreads();
-      if (prefix[0] < p.worth)
+      if (!worth_it(p, prefix[0]))
         for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = 0;
     }
   }

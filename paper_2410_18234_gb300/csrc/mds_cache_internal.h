@@ -90,7 +90,7 @@ struct Shared {
   int members, nodes;
   bool prefix;     // the prefix's launch; else the rest's
   float* prior;
-  int64_t worth;
+  int64_t worth, each;   // tokens that must be saved in all, and for each live sequence
 };
 // Rows of a tile of rows in the prefix's launch, by the kernel that it is.
 inline int even_rows(int64_t rows, int most) {   // as even as it goes

@@ -409,6 +409,7 @@ cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cu
   p.nodes = x.nodes;
   p.prior = x.prior;
   p.worth = x.worth;
+  p.each = x.each;
   return launch_behind(rest_kernel<D>, attend_grid(sms, kRows, D, kPieceFloats), kThreads, Rest<D>::smem(a.B), st, p);
 }
 

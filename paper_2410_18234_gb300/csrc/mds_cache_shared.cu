@@ -161,7 +161,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
   if (choose) least = few_rows ? kWorthFew : kWorthMany;
   const int64_t token = 2 * (int64_t)s.kv_heads * s.head_dim;
   const int64_t worth = least / token + (least % token != 0);   // tokens
-  const int64_t each = choose && own > 8 ? kWorthRow * own : 0;    // of each sequence
+  const int64_t each = choose && own > 8 ? kWorthRow * own : 0;    // of each live sequence
   // the most that the sequences' tables have room to share
   const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
   if (most < std::max({worth, each * a.B, choose && few_rows ? kAloneFew / token : 0})) return attend(s, a, sms, st);
@@ -178,7 +178,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
     y.B = some;
     y.n = a.n * members;
     y.L = y.n - 1;
-    Shared z{members, a.n, true, s.part + kPieceFloats, std::max(worth, each * x.B)};
+    Shared z{members, a.n, true, s.part + kPieceFloats, worth, each};
     const int64_t rows = (int64_t)y.n * g;
     const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
     Params p{s, y, 0, g, (int)rows, 0, 0, 0};
