@@ -68,6 +68,7 @@ size_t carve(const mds_cache_config& c, char* base, State& s) {
   take(s.free_count, 64);
   s.n_copies = s.free_count + 1;
   s.status = reinterpret_cast<uint32_t*>(s.free_count + 2);
+  s.saved = reinterpret_cast<int64_t*>(s.free_count + 4);
   take(s.part, mds::cache::kPartFloats * 4);
   s.layers = c.layers;
   s.pages = c.pages;

@@ -61,6 +61,7 @@ struct Params {
   int members = 1, nodes = 0;      // sequences of a group, and nodes of one
   float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
   int64_t worth = 0, each = 0;     // tokens that must be saved, in all and a live sequence, for the prefix to be attended to by itself
+  const int64_t* saved = nullptr;  // what the call saves, where that is not what its plan sees
 };
 
 // The launches of attention over a shared prefix follow one another without a
@@ -308,9 +309,10 @@ __device__ __forceinline__ void add_up(long long* to, long long x) {
 }
 
 // What decides whether prefixes are attended to by themselves, in one number:
-// tokens saved (at most 2^30), and live sequences above.
+// tokens saved (at most 2^30), and live sequences above.  x: of the plan.
 constexpr int kLiveShift = 40;
 __device__ __forceinline__ bool worth_it(const Params& p, long long x) {
+  if (p.saved) x = *p.saved;
   const long long saved = x & ((1ll << kLiveShift) - 1), live = x >> kLiveShift;
   return saved >= p.worth && saved >= p.each * live;
 }

@@ -23,7 +23,7 @@ cudaError_t configure() {
 //   17 rows: here 509, there 234    296, 193
 cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st) {
   if (s.dtype != MDS_F32 && (int64_t)a.n * (a.heads / s.kv_heads) > 16) return attend_many(s, a, sms, st);
-  return attend_few<kAll>(s, a, Shared{1, a.n, false, nullptr, 0, 0}, sms, st);
+  return attend_few<kAll>(s, a, Shared{1, a.n, false, nullptr, 0, 0, nullptr}, sms, st);
 }
 
 }  // namespace cache

@@ -564,6 +564,7 @@ cudaError_t launch_few(const State& s, const Attend& a, const Shared& x, int sms
   p.prior = x.prior;
   p.worth = x.worth;
   p.each = x.each;
+  p.saved = x.saved;
   const int grid = attend_grid(sms, F::kRows, D, kPart == kAll ? kPartFloats : kPieceFloats);
   p.stages = kStageMax;
   // A stage's tiles all belong to one set: a consumer waits for each of the

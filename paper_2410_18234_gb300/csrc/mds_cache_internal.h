@@ -37,6 +37,7 @@ struct State {
   int2* share;        // [MDS_CACHE_MAX_BATCH] attend over prefixes: tokens shared with the group's first, live nodes
   float* part;        // attend's partial sums; from kPieceFloats on rows' sums over a prefix
   uint32_t* status;
+  int64_t* saved;     // attend over prefixes in several turns: what the whole call saves
   int layers, pages, page_tokens, page_log, kv_heads, head_dim, max_seqs, max_pages, dtype;
 };
 
@@ -91,6 +92,7 @@ struct Shared {
   bool prefix;     // the prefix's launch; else the rest's
   float* prior;
   int64_t worth, each;   // tokens that must be saved in all, and for each live sequence
+  const int64_t* saved;  // of the call, where it has several turns
 };
 // Rows of a tile of rows in the prefix's launch, by the kernel that it is.
 inline int even_rows(int64_t rows, int most) {   // as even as it goes

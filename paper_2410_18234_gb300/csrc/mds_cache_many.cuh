@@ -894,6 +894,7 @@ cudaError_t attend_part(const State& s, const Attend& a, const Shared& x, int sm
   p.prior = x.prior;
   p.worth = x.worth;
   p.each = x.each;
+  p.saved = x.saved;
   const int size = p.rows_per <= 48 ? 2 : p.rows_per <= 96 ? 4 : 6;
   if (s.head_dim == 64)
     return size == 2 ? launch_many<64, 2, kPart>(p, sms, st) : size == 4 ? launch_many<64, 4, kPart>(p, sms, st) : launch_many<64, 6, kPart>(p, sms, st);

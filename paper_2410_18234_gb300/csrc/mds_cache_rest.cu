@@ -410,6 +410,7 @@ cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cu
   p.prior = x.prior;
   p.worth = x.worth;
   p.each = x.each;
+  p.saved = x.saved;
   return launch_behind(rest_kernel<D>, attend_grid(sms, kRows, D, kPieceFloats), kThreads, Rest<D>::smem(a.B), st, p);
 }
 

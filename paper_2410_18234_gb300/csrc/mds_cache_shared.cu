@@ -67,7 +67,7 @@ constexpr int64_t kAloneFew = 160 << 20;
 
 // One block of threads a sequence: the tokens that it shares with the first
 // live sequence of its group (none if it is the only one), and its live nodes.
-// A group's first block marks its tiles of rows as not cut.
+// With `prior` a group's first block marks its tiles of rows as not cut.
 template <int D>
 __global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Params p) {
   const State& s = p.s;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Para
   const int n = p.nodes, members = p.members;
   __shared__ int first_s, differ_s, others_s;
   const int tid = threadIdx.x, b = blockIdx.x, g0 = b / members * members;
-  if (b == g0)
+  if (b == g0 && p.prior)
     for (int x = tid; x < s.kv_heads * p.row_tiles; x += 256)
       *reinterpret_cast<int2*>(prior_of<D>(p, row_at(p, b / members, x / p.row_tiles, x % p.row_tiles * p.rows_per)) + 2) = int2{-1, -1};
   if (tid == 0) first_s = INT_MAX, differ_s = INT_MAX, others_s = 0;
@@ -99,6 +99,26 @@ __global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Para
   }
   __syncthreads();
   if (tid == 0) s.share[b] = live <= 0 ? int2{INT_MAX, 0} : others_s ? int2{(differ_s << s.page_log) & -kTile, live} : int2{0, live};
+}
+
+// What a call in several turns saves in all its groups, a thread a place, from
+// what each place shares: one number, as plans take it.
+__global__ void __launch_bounds__(MDS_CACHE_MAX_BATCH) total_kernel(const __grid_constant__ Params p) {
+  __shared__ int from_s[MDS_CACHE_MAX_BATCH];
+  __shared__ long long saved_s;
+  const int b = threadIdx.x, first = b / p.members * p.members;
+  const int2 x = b < p.a.B ? p.s.share[b] : int2{INT_MAX, 0};
+  from_s[b] = INT_MAX;
+  if (b == 0) saved_s = 0;
+  __syncthreads();
+  if (x.y > 0) atomicMin(&from_s[first], x.x);
+  __syncthreads();
+  const int from = from_s[first];
+  long long saved = x.y > 0 ? from + (1ll << kLiveShift) : 0;
+  if (b == first && from != INT_MAX) saved -= from;   // once for a group
+  add_up(&saved_s, saved);
+  __syncthreads();
+  if (b == 0) *p.s.saved = saved_s;
 }
 
 // A row a warp: the pieces of its tile of rows, where that was cut, in their order.
@@ -166,6 +186,17 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
   const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
   if (most < std::max({worth, each * a.B, choose && few_rows ? kAloneFew / token : 0})) return attend(s, a, sms, st);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
+  const bool turns = groups > at_once;
+  if (turns) {   // no turn's own savings decide
+    Params p{s, a, 0, g, 0, 0, 0, 0};
+    p.members = members;
+    p.nodes = a.n;
+    if (s.head_dim == 64) share_kernel<64><<<a.B, 256, 0, st>>>(p);
+    else share_kernel<128><<<a.B, 256, 0, st>>>(p);
+    total_kernel<<<1, MDS_CACHE_MAX_BATCH, 0, st>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   for (int g0 = 0; g0 < groups; g0 += at_once) {
     const int some = groups - g0 < at_once ? groups - g0 : at_once, b0 = g0 * members;
     Attend x = a;
@@ -178,7 +209,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
     y.B = some;
     y.n = a.n * members;
     y.L = y.n - 1;
-    Shared z{members, a.n, true, s.part + kPieceFloats, worth, each};
+    Shared z{members, a.n, true, s.part + kPieceFloats, worth, each, turns ? s.saved : nullptr};
     const int64_t rows = (int64_t)y.n * g;
     const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
     Params p{s, y, 0, g, (int)rows, 0, 0, 0};

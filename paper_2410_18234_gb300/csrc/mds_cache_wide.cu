@@ -587,6 +587,7 @@ cudaError_t launch(const State& s, const Attend& a, const Shared& x, int sms, cu
   p.prior = x.prior;
   p.worth = x.worth;
   p.each = x.each;
+  p.saved = x.saved;
   return launch_behind(wide_kernel<D>, attend_grid(sms, p.rows_per, D, kPieceFloats), kThreads, Wide<D>::bytes(a.B), st, p);
 }
 

@@ -1,4 +1,6 @@
-"""Which calls of attend_shared share, whatever places are unused."""
+"""Which calls of attend_shared share: the savings of the whole call decide,
+whatever places are unused."""
+import numpy as np
 import pytest
 import torch
 
@@ -8,13 +10,41 @@ if not torch.cuda.is_available():
     pytest.skip("needs a CUDA GPU", allow_module_level=True)
 
 from paper_2410_18234_gb300 import cache  # noqa: E402
-from test_gpu_cache_shared import DEV, ints  # noqa: E402
+from test_gpu_cache_shared import DEV, both, fork, grow, ints, tokens  # noqa: E402
 
 
 def near(a, b, largest):
     """Each within its bound of the exact answer: 2 * 2^-8 of the largest value
     for the weights in the sum and in the normaliser, 2^-8 for the output."""
     return float((a.double() - b.double()).abs().max()) <= 2 * 3 * 2.0 ** -8 * float(largest)
+
+
+def forks(rng, B, G, prefix, page=64, H=1, D=64, pages=0, max_pages=12):
+    """B / G groups of forks of prefix(group) tokens that went on by 0 to 60 tokens."""
+    c, m = both(pages or B * 3 + B // G * 8, H, D, B, max_pages, page)
+    roots = list(range(0, B, G))
+    grow(c, m, rng, roots, [prefix(i) for i in range(B // G)])
+    fork(c, m, [r for r in roots for _ in range(G - 1)], [r + j for r in roots for j in range(1, G)])
+    grow(c, m, rng, list(range(B)), [int(x) for x in rng.integers(0, 60, B)])
+    return c, m
+
+
+def test_savings_of_a_call_in_several_turns():
+    """4 groups of 64 sequences of 576 rows, of which the workspace holds the
+    sums of two groups: what must be saved is compared with what all save."""
+    rng = np.random.default_rng(31)
+    B, G, n, Hq = 256, 64, 9, 64
+    c, m = forks(rng, B, G, lambda i: 300 + 60 * i)                  # 256, 256, 384, 384 shared
+    seqs = ints(range(B))
+    c.reserve(seqs, n)
+    c.append(0, seqs, *(tokens(rng, B, n, 1, 64) for _ in range(2)))
+    q = 0.02 * tokens(rng, B, n, Hq, 64)
+    largest = c.read(0, seqs, None, 600)[1].abs().max()
+    saved = 63 * (256 + 256 + 384 + 384) * 2 * 64                     # bytes
+    a, b, always, never = (c.attend_shared(0, seqs, q, G, branches=2, least_saved=x) for x in (saved, saved + 128, 0, 2 * saved))
+    assert torch.equal(b, never) and torch.equal(a, always) and not torch.equal(a, b)
+    assert near(a, c.attend(0, seqs, q, branches=2), largest)
+    assert c.status() == (0, "ok")
 
 
 def test_unused_places_do_not_count():
