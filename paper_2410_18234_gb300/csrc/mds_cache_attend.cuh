@@ -309,12 +309,18 @@ __device__ __forceinline__ void add_up(long long* to, long long x) {
 }
 
 // What decides whether prefixes are attended to by themselves, in one number:
-// tokens saved (at most 2^30), and live sequences above.  x: of the plan.
+// tokens saved (at most 2^30), and live sequences above.
 constexpr int kLiveShift = 40;
 __device__ __forceinline__ bool worth_it(const Params& p, long long x) {
-  if (p.saved) x = *p.saved;
   const long long saved = x & ((1ll << kLiveShift) - 1), live = x >> kLiveShift;
   return saved >= p.worth && saved >= p.each * live;
+}
+
+// Where what the call saves is known before (several turns): whether a launch
+// has nothing to do, those of the turns or the one for the whole call.
+template <int kPart>
+__device__ __forceinline__ bool idle(const Params& p) {
+  return p.saved && worth_it(p, *p.saved) == (kPart == kAll);
 }
 
 // The plan, by all of the block's threads: seqs and the exclusive sums of
@@ -345,7 +351,7 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
       if (seqs[g].end > 0) saved += (seqs[g].end - 1ll) * seqs[g].len + ((long long)seqs[g].end << kLiveShift);
     add_up(prefix, saved);
     __syncthreads();
-    const bool worth = worth_it(p, prefix[0]);
+    const bool worth = p.saved || worth_it(p, prefix[0]);
     for (int g = tid; g < p.a.B; g += blockDim.x) {
       const Seq<kPart> q = seqs[g];
       seqs[g] = worth && q.live > 0 && q.len > 0 ? Seq<kPart>{p.a.seqs[q.q], q.len, q.live, q.len} : Seq<kPart>{-1, 0, 0, 0};
@@ -379,7 +385,7 @@ __device__ void plan(const Params& p, long long* prefix, Seq<kPart>* seqs, int h
       }
       add_up(prefix, saved);
       __syncthreads();
-      if (!worth_it(p, prefix[0]))
+      if (!p.saved && !worth_it(p, prefix[0]))
         for (int b = tid; b < p.a.B; b += blockDim.x) seqs[b].from = 0;
     }
   }

@@ -21,9 +21,9 @@ cudaError_t configure() {
 //    8 rows: here 222, there 228    144, 193
 //   16 rows: here 287, there 232    167, 193
 //   17 rows: here 509, there 234    296, 193
-cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st) {
-  if (s.dtype != MDS_F32 && (int64_t)a.n * (a.heads / s.kv_heads) > 16) return attend_many(s, a, sms, st);
-  return attend_few<kAll>(s, a, Shared{1, a.n, false, nullptr, 0, 0, nullptr}, sms, st);
+cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st, const Shared& x) {
+  if (s.dtype != MDS_F32 && (int64_t)a.n * (a.heads / s.kv_heads) > 16) return attend_many(s, a, sms, st, x);
+  return attend_few<kAll>(s, a, x, sms, st);
 }
 
 }  // namespace cache

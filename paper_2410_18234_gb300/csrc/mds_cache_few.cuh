@@ -294,6 +294,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
     mbar_init_fence();
   }
   if constexpr (kPart != kAll) after_launch_before();
+  if (idle<kPart>(p)) return;
   plan<T, kPart>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B];
   const long long per = (total + gridDim.x - 1) / gridDim.x;

@@ -82,18 +82,19 @@ struct Attend {
   int layer, B, n, L, heads, window, sinks;
   float scale;
 };
-cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st);        // mds_cache_few.cu
-cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st);   // mds_cache_many.cu
 // Groups of `members` sequences of the list, over their common prefix and each
 // over its rest (mds_cache_shared.cu; the launches: _shared_few.cu, _shared_many.cu).
 cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t least, int sms, cudaStream_t st);
 struct Shared {
-  int members, nodes;
-  bool prefix;     // the prefix's launch; else the rest's
-  float* prior;
-  int64_t worth, each;   // tokens that must be saved in all, and for each live sequence
-  const int64_t* saved;  // of the call, where it has several turns
+  int members = 1, nodes = 0;
+  bool prefix = false;     // the prefix's launch; else the rest's
+  float* prior = nullptr;
+  int64_t worth = 0, each = 0;     // tokens that must be saved in all, and for each live sequence
+  const int64_t* saved = nullptr;  // of the call, where it has several turns
 };
+// x: where it has `saved`, the launch is for what is not worth sharing, and is over at once where it is.
+cudaError_t attend(const State& s, const Attend& a, int sms, cudaStream_t st, const Shared& x = {});        // mds_cache_few.cu
+cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st, const Shared& x = {});   // mds_cache_many.cu
 // Rows of a tile of rows in the prefix's launch, by the kernel that it is.
 inline int even_rows(int64_t rows, int most) {   // as even as it goes
   const int64_t tiles = (rows + most - 1) / most;

@@ -6,8 +6,8 @@ namespace cache {
 
 cudaError_t configure_many() { return configure_part<kAll>(); }
 
-cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st) {
-  return attend_part<kAll>(s, a, Shared{1, a.n, false, nullptr, 0, 0, nullptr}, sms, st);
+cudaError_t attend_many(const State& s, const Attend& a, int sms, cudaStream_t st, const Shared& x) {
+  return attend_part<kAll>(s, a, x, sms, st);
 }
 
 }  // namespace cache

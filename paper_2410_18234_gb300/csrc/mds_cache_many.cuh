@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
     mbar_init_fence();
   }
   if constexpr (kPart != kAll) after_launch_before();
+  if (idle<kPart>(p)) return;
   plan<__nv_bfloat16, kPart>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B];
   const long long per = (total + gridDim.x - 1) / gridDim.x;

@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_kernel(const __grid_constant
   if (tid == 0) *abort = 0, cut[0] = cut[5] = -1;
   mbar_init_fence();
   after_launch_before();
+  if (idle<kRest>(p)) return;
   plan<T, kRest, true>(p, prefix, seqs, D);   // ends in a barrier
   const long long total = prefix[p.a.B], share = (total + gridDim.x - 1) / gridDim.x;   // of a block of threads
   const int slack = (int)max(share / 4, (long long)kBlockSlack);

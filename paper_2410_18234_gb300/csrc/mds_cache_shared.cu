@@ -186,8 +186,10 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
   const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
   if (most < std::max({worth, each * a.B, choose && few_rows ? kAloneFew / token : 0})) return attend(s, a, sms, st);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
+  // In several turns no turn's own savings decide, and what is not worth
+  // sharing is left to one launch over the whole call.
   const bool turns = groups > at_once;
-  if (turns) {   // no turn's own savings decide
+  if (turns) {
     Params p{s, a, 0, g, 0, 0, 0, 0};
     p.members = members;
     p.nodes = a.n;
@@ -235,6 +237,7 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
           : few_rows ? shared_few(s, x, z, sms, st) : shared_many(s, x, z, sms, st);
     if (e != cudaSuccess) return e;
   }
+  if (turns) return attend(s, a, sms, st, Shared{1, a.n, false, nullptr, worth, each, s.saved});
   return cudaSuccess;
 }
 

@@ -143,6 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     mbar_init_fence();
   }
   after_launch_before();
+  if (idle<kPrefix>(p)) return;
   plan<T, kPrefix>(p, prefix, seqs, D);
   __syncthreads();
   const long long total = prefix[p.a.B];
