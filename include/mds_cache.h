@@ -203,13 +203,18 @@ int mds_cache_attend(mds_cache* cache, int layer, const int32_t* seqs, const int
 /* mds_cache_attend without a window for sequences that share a prefix, such as
  * forks of one: each `group` (a divisor of B) places of the list in turn are a
  * group, and the pages that all of its live sequences hold at the same places,
- * as far as their tokens are committed, are read once for all of them instead
- * of once for each (in whole tiles of 128 tokens).  What is shared is found on
+ * as far as their tokens are committed, are attended to for all of them
+ * together instead of for each (in whole tiles of 128 tokens, by up to 256
+ * rows, in 32 bits 16, that read them together).  What is shared is found on
  * the device; a group that shares nothing is attended to all the same, and so
- * are all where sharing would save less than least_saved bytes of keys and
- * values (below 0: a default, at which it pays; 0: shared in any case).  The
- * result is mds_cache_attend's but for the order of 32-bit sums and the
- * references that weights are rounded at. */
+ * are all where sharing would save the call less than least_saved bytes of
+ * keys and values (below 0: a default; 0: shared in any case).
+ * Sums over prefixes take n * q_heads * (head_dim + 4) of 6291456 places of
+ * the workspace a sequence: a larger group is shared in as few parts, as equal
+ * as they go, as fit, each like a group of its own, and where two sequences do
+ * not fit, or the page tables have no room for such savings, the call is
+ * mds_cache_attend's.  The result is mds_cache_attend's but for the order of
+ * 32-bit sums and the references that weights are rounded at. */
 int mds_cache_attend_shared(mds_cache* cache, int layer, const int32_t* seqs, const int32_t* counts, const void* q,
                             const int64_t* q_strides, void* out, int q_heads, int n, int branches, int group,
                             float scale, int64_t least_saved, int B, void* stream);

@@ -363,9 +363,10 @@ class Cache:
         """`attend` (without a window) for sequences that share a prefix: each
         ``group`` (a divisor of B) sequences of the list in turn, such as the
         forks of one prompt; unused places pad a smaller group.  The pages
-        that all of a group hold, as far as they are committed, are read once
-        for all of them, unless that would save less than ``least_saved``
-        bytes of keys and values (None: where it pays)."""
+        that all of a group hold, as far as they are committed, are attended
+        to for all of them together, unless that would save the call less than
+        ``least_saved`` bytes of keys and values (None: a default, 0: in any
+        case; where two sequences' sums pass the workspace it is `attend`)."""
         ids, B = self._seqs(seqs)
         qs = self._rows("q", q, B)
         layer, branches, group = _sizes(layer, branches, group)

@@ -59,6 +59,7 @@ struct Params {
   // not, but not a product and a fused operation by this number.
   float one = 1.f;
   int members = 1, nodes = 0;      // sequences of a group, and nodes of one
+  int part = 0;                    // members that one turn takes, where several share a group (mds_cache_shared.cu)
   float* prior = nullptr;          // [B][n][heads][D + 4], like pieces
   int64_t worth = 0, each = 0;     // tokens that must be saved, in all and a live sequence, for the prefix to be attended to by itself
   const int64_t* saved = nullptr;  // what the call saves, where that is not what its plan sees

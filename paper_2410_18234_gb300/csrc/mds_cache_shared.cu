@@ -65,6 +65,12 @@ bool full_rows(int dtype, int64_t own) {
 // 224), the host calls that.
 constexpr int64_t kAloneFew = 160 << 20;
 
+// Whose group place b of the list is in: its first and last place and one.
+__device__ __forceinline__ int2 group_at(const Params& p, int b) {
+  const int first = b / p.members * p.members, end = first + p.members, part = (b - first) / p.part * p.part;
+  return int2{first + part, min(first + part + p.part, end)};
+}
+
 // One block of threads a sequence: the tokens that it shares with the first
 // live sequence of its group (none if it is the only one), and its live nodes.
 // With `prior` a group's first block marks its tiles of rows as not cut.
@@ -72,16 +78,16 @@ template <int D>
 __global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Params p) {
   const State& s = p.s;
   const int32_t *seqs = p.a.seqs, *counts = p.a.counts;
-  const int n = p.nodes, members = p.members;
+  const int n = p.nodes, g0 = group_at(p, blockIdx.x).x, g1 = group_at(p, blockIdx.x).y;
   __shared__ int first_s, differ_s, others_s;
-  const int tid = threadIdx.x, b = blockIdx.x, g0 = b / members * members;
+  const int tid = threadIdx.x, b = blockIdx.x;
   if (b == g0 && p.prior)
     for (int x = tid; x < s.kv_heads * p.row_tiles; x += 256)
-      *reinterpret_cast<int2*>(prior_of<D>(p, row_at(p, b / members, x / p.row_tiles, x % p.row_tiles * p.rows_per)) + 2) = int2{-1, -1};
+      *reinterpret_cast<int2*>(prior_of<D>(p, row_at(p, b / p.members, x / p.row_tiles, x % p.row_tiles * p.rows_per)) + 2) = int2{-1, -1};
   if (tid == 0) first_s = INT_MAX, differ_s = INT_MAX, others_s = 0;
   __syncthreads();
   int id, len, live, end, q0, len0, live0;
-  for (int i = g0 + tid; i < g0 + members; i += 256) {
+  for (int i = g0 + tid; i < g1; i += 256) {
     find(s, seqs, counts, i, n, &q0, &len0, &live0, &end);
     if (live0 > 0) atomicMin(&first_s, i);
     if (live0 > 0 && i != b) others_s = 1;
@@ -106,7 +112,7 @@ __global__ void __launch_bounds__(256) share_kernel(const __grid_constant__ Para
 __global__ void __launch_bounds__(MDS_CACHE_MAX_BATCH) total_kernel(const __grid_constant__ Params p) {
   __shared__ int from_s[MDS_CACHE_MAX_BATCH];
   __shared__ long long saved_s;
-  const int b = threadIdx.x, first = b / p.members * p.members;
+  const int b = threadIdx.x, first = group_at(p, b).x;
   const int2 x = b < p.a.B ? p.s.share[b] : int2{INT_MAX, 0};
   from_s[b] = INT_MAX;
   if (b == 0) saved_s = 0;
@@ -171,27 +177,34 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
 
 cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t least, int sms, cudaStream_t st) {
   const int g = a.heads / s.kv_heads, groups = a.B / members;
-  // as many groups at a time as their rows' sums over the prefix have room for
-  const int64_t row = (int64_t)a.n * a.heads * (s.head_dim + 4) * members;
-  const int at_once = (int)(((int64_t)kPartFloats - kPieceFloats) / row);
+  // As many sequences at a time as their rows' sums over the prefix have room
+  // for: several groups, one, or, of groups larger than that, as equal parts as
+  // go, each shared like a group of its own (a prefix read twice or three times
+  // is still not read by every sequence).
+  const int64_t at_once = ((int64_t)kPartFloats - kPieceFloats) / ((int64_t)a.n * a.heads * (s.head_dim + 4));
   const int64_t own = (int64_t)a.n * g;   // rows of one sequence
   const bool few_rows = s.dtype == MDS_F32 || own <= kFewRows;
   const bool choose = least < 0;
-  if (members < 2 || at_once == 0 || (choose && full_rows(s.dtype, own))) return attend(s, a, sms, st);
+  if (members < 2 || at_once < 2 || (choose && full_rows(s.dtype, own))) return attend(s, a, sms, st);
   if (choose) least = few_rows ? kWorthFew : kWorthMany;
   const int64_t token = 2 * (int64_t)s.kv_heads * s.head_dim;
   const int64_t worth = least / token + (least % token != 0);   // tokens
   const int64_t each = choose && own > 8 ? kWorthRow * own : 0;    // of each live sequence
-  // the most that the sequences' tables have room to share
-  const int64_t most = (int64_t)groups * (members - 1) * s.max_pages * s.page_tokens;
-  if (most < std::max({worth, each * a.B, choose && few_rows ? kAloneFew / token : 0})) return attend(s, a, sms, st);
+  const int parts = (int)((members + at_once - 1) / at_once), part = (members + parts - 1) / parts;
+  // the most that the sequences' tables have room to share, in all and in a full part
+  const int64_t room = (int64_t)s.max_pages * s.page_tokens;
+  if (groups * (members - parts) * room < std::max(worth, choose && few_rows ? kAloneFew / token : 0) ||
+      (part - 1) * room < each * part)
+    return attend(s, a, sms, st);
   const int es = s.dtype == MDS_F32 ? 4 : 2;
   // In several turns no turn's own savings decide, and what is not worth
   // sharing is left to one launch over the whole call.
-  const bool turns = groups > at_once;
+  const int together = parts > 1 ? 1 : (int)std::min((int64_t)groups, at_once / members);   // groups of a turn
+  const bool turns = parts > 1 || together < groups;
   if (turns) {
     Params p{s, a, 0, g, 0, 0, 0, 0};
     p.members = members;
+    p.part = part;
     p.nodes = a.n;
     if (s.head_dim == 64) share_kernel<64><<<a.B, 256, 0, st>>>(p);
     else share_kernel<128><<<a.B, 256, 0, st>>>(p);
@@ -199,26 +212,29 @@ cudaError_t attend_shared(const State& s, const Attend& a, int members, int64_t 
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  for (int g0 = 0; g0 < groups; g0 += at_once) {
-    const int some = groups - g0 < at_once ? groups - g0 : at_once, b0 = g0 * members;
+  for (int b0 = 0, some, of_each; b0 < a.B; b0 += some * of_each) {
+    // some groups of so many members, or a part of one
+    some = std::min(together, (a.B - b0) / members);
+    of_each = members;
+    if (parts > 1) some = 1, of_each = std::min(part, members - b0 % members);
     Attend x = a;
-    x.B = some * members;
+    x.B = some * of_each;
     x.seqs = a.seqs + b0;
     x.counts = a.counts ? a.counts + b0 : nullptr;
     x.q = static_cast<const char*>(a.q) + b0 * a.q_seq * es;
     x.out = static_cast<char*>(a.out) + (int64_t)b0 * a.n * a.heads * s.head_dim * es;
     Attend y = x;
     y.B = some;
-    y.n = a.n * members;
+    y.n = a.n * of_each;
     y.L = y.n - 1;
-    Shared z{members, a.n, true, s.part + kPieceFloats, worth, each, turns ? s.saved : nullptr};
+    Shared z{of_each, a.n, true, s.part + kPieceFloats, worth, each, turns ? s.saved : nullptr};
     const int64_t rows = (int64_t)y.n * g;
     const bool few = s.dtype == MDS_F32 || rows <= kFewRows, many = !few && rows <= kNarrow;
     Params p{s, y, 0, g, (int)rows, 0, 0, 0};
     // as the launch of the prefix cuts them
     p.rows_per = few ? (rows > 8 ? 16 : 8) : even_rows(rows, many ? kManyRows : kWideRows);
     p.row_tiles = (int)((rows + p.rows_per - 1) / p.rows_per);
-    p.members = members;
+    p.members = p.part = of_each;
     p.nodes = a.n;
     p.prior = z.prior;
     if (s.head_dim == 64) share_kernel<64><<<x.B, 256, 0, st>>>(p);

@@ -1,5 +1,5 @@
-"""Which calls of attend_shared share: the savings of the whole call decide,
-whatever places are unused."""
+"""Which calls of attend_shared share: the savings of the whole call decide, in
+groups of any size, whatever places are unused."""
 import numpy as np
 import pytest
 import torch
@@ -10,7 +10,7 @@ if not torch.cuda.is_available():
     pytest.skip("needs a CUDA GPU", allow_module_level=True)
 
 from paper_2410_18234_gb300 import cache  # noqa: E402
-from test_gpu_cache_shared import DEV, both, fork, grow, ints, tokens  # noqa: E402
+from test_gpu_cache_shared import DEV, both, check, fork, grow, ints, tokens  # noqa: E402
 
 
 def near(a, b, largest):
@@ -45,6 +45,41 @@ def test_savings_of_a_call_in_several_turns():
     assert torch.equal(b, never) and torch.equal(a, always) and not torch.equal(a, b)
     assert near(a, c.attend(0, seqs, q, branches=2), largest)
     assert c.status() == (0, "ok")
+
+
+@pytest.mark.parametrize("G,parts", [(64, (32, 32)), (53, (27, 26)), (130, (33, 33, 33, 31))])
+def test_groups_beyond_the_workspace(G, parts):
+    """Sums of 43 sequences of 33 nodes fit: a group is shared in as few parts
+    as hold it, each of which reads the prefix once."""
+    rng = np.random.default_rng(G)
+    n, Hq = 33, 64
+    c, m = forks(rng, 2 * G, G, lambda i: 300 + 130 * i)              # 256 and 384 shared
+    live = G - 3                                                      # the last places are unused
+    order = np.arange(2 * G).reshape(2, G)
+    order[:, live:] = -1
+    seqs = ints(order.ravel())
+    real = ints([x for x in order.ravel() if x >= 0])
+    check(c, m, rng, [int(x) for x in order.ravel()], G, Hq, 4, 8, only=[0, parts[0], G - 4, 2 * G - 4])
+    c.reserve(real, n)
+    c.append(0, real, *(tokens(rng, len(real), n, 1, 64) for _ in range(2)))
+    largest = c.read(0, real, None, 600)[1].abs().max()
+    q = 0.02 * tokens(rng, 2 * G, n, Hq, 64)
+    saved = (live - len(parts)) * (256 + 384) * 2 * 64
+    a, b, always, never = (c.attend_shared(0, seqs, q, G, branches=4, least_saved=x) for x in (saved, saved + 128, 0, 2 * saved))
+    assert torch.equal(a, always) and torch.equal(b, never) and not torch.equal(a, b)
+    alone = c.attend(0, seqs, q, branches=4)
+    assert near(a, alone, largest) and near(b, alone, largest)
+    assert not a.view(2, G, -1)[:, live:].any()
+    # each part as a group of its own, shared in any case: the same launches
+    at = 0
+    for members in parts:
+        ids = seqs.view(2, G)[:, at:at + members]
+        for g in range(2):
+            one = c.attend_shared(0, ids[g].contiguous(), q.view(2, G, n, Hq, 64)[g, at:at + members], members, branches=4,
+                                  least_saved=0)
+            assert torch.equal(one, a.view(2, G, n, Hq, 64)[g, at:at + members])
+        at += members
+    assert at == G and c.status() == (0, "ok")
 
 
 def test_unused_places_do_not_count():
