@@ -156,15 +156,17 @@ __device__ __forceinline__ bool try_wait(uint64_t* bar, unsigned parity) {
       : "memory");
   return done != 0;
 }
-__device__ __forceinline__ void wait(uint64_t* bar, unsigned parity, int* abort) {
+// False: it gave up.
+__device__ __forceinline__ bool wait(uint64_t* bar, unsigned parity, int* abort) {
   unsigned i = 0;
 #pragma unroll 1
   while (!try_wait(bar, parity)) {
     if (++i > kWaitTries || *reinterpret_cast<volatile int*>(abort)) {
       *reinterpret_cast<volatile int*>(abort) = 1;
-      break;
+      return false;
     }
   }
+  return true;
 }
 // Whether the block gave up, the same answer for a warp's lanes: a loader then
 // starts no more copies, as their places may still be written or read.

@@ -225,8 +225,9 @@ __global__ void __launch_bounds__(kThreads, 1) rest_kernel(const __grid_constant
       page = __ldg(table + (slot >> s.page_log));
     };
     find_group();
+    bool stop = false;   // a wait gave up, of any lane: no more copies, as their places may still be written
     auto fetch = [&] {
-      if (uf >= w1) return;
+      if (uf >= w1 || stop) return;
       if (lane == 0) mbar_expect_tx(full + put, X::kStage);
       __syncwarp();
       if (lane < 2) {
@@ -310,11 +311,11 @@ __global__ void __launch_bounds__(kThreads, 1) rest_kernel(const __grid_constant
       x.clear();
 #pragma unroll 1
       for (; u < end; ++u, t0 += kBlock) {
-        wait(full + get, parity, abort);
+        const bool there = wait(full + get, parity, abort);
         const char* kb = ring + get * X::kStage;
         few_block<T, D, 1>(p, kb, smem_u32(kb + kBlock * D), scales[get * 2], scales[get * 2 + 1], places,
                            [&](int i) { return query[i]; }, node, own, rc, t0, q.len, hi, x);
-        __syncwarp();
+        stop = __any_sync(kFull, !there) || stop;
         fetch();
         if (++get == X::kStages) get = 0, parity ^= 1u;
       }
