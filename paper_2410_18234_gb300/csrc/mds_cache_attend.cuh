@@ -173,9 +173,9 @@ __device__ __forceinline__ bool wait(uint64_t* bar, unsigned parity, int* abort)
 __device__ __forceinline__ bool gave_up(const int* abort) {
   return __any_sync(kFull, *reinterpret_cast<const volatile int*>(abort));
 }
-// By the thread that started the copies: whether the block gave up; then it
-// leaves the copies in flight time to land before the block ends.
-__device__ __noinline__ void report(int* abort, uint32_t* status) {
+// Behind a thread's last wait: says so if the block gave up, and leaves copies
+// and products in flight time to end before the block, and what it holds, goes.
+__device__ __forceinline__ void report(int* abort, uint32_t* status) {
   if (!*reinterpret_cast<volatile int*>(abort)) return;
   atomicOr(status, MDS_ST_TIMEOUT);
   for (int i = 0; i < 1000; ++i) __nanosleep(10000);

@@ -303,6 +303,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
 
   if (warp == F::kWarps + 1) {
     schedule<D>(p, seqs, locate(p, prefix, seqs, u0), per, u0, u1, jobs, ready, taken, abort);
+    report(abort, p.s.status);
     return;
   }
   auto job_at = [&](int n) -> const Job& {
@@ -552,6 +553,7 @@ __global__ void __launch_bounds__(Few<T, D, NT>::kThreads + 64, 1) few_kernel(co
     }
     job_done(n);
   }
+  report(abort, p.s.status);
 }
 
 template <typename T, int D, int NT, int kPart>

@@ -253,20 +253,21 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
         if (++slot == slots) slot = 0, parity ^= 1u;
       }
     }
-    report(abort, s.status);
   } else if (warp == 1) {
-    // ---- products, issued by one thread: S(t + 1) before O(t)
+    // ---- products, issued by one thread: S(t + 1) before O(t); none once a wait for them gave up
+    bool there = true;
+    auto need = [&](int b, unsigned parity) { there = wait(bar + b, parity, abort) && there; };
     const uint32_t id_s = instruction(N, 0, 0), id_o = instruction(N, 1, 1);
     const uint64_t q_op = operand(smem_u32(base + lay.q), 16), v_op = operand(smem_u32(base + lay.wide_v), 16384);
     const uint64_t w_op = operand(smem_u32(base + lay.w), 16);
     int tile = 0, group = 0;
     auto out_product = [&](int t, bool first) {
-      hold(kW + (t & 1), (t >> 1) & 1);
+      need(kW + (t & 1), (t >> 1) & 1);
       const int wide = t & (kWide - 1);
-      hold(kWideV + wide, (t / kWide) & 1);
-      if (first) hold(kOFree, (group & 1) ^ 1);
+      need(kWideV + wide, (t / kWide) & 1);
+      if (first) need(kOFree, (group & 1) ^ 1);
       after_sync();
-      if (elected()) {
+      if (elected() && there) {
         const uint64_t v = v_op + (wide * (128 * D * 2) >> 4);
         const uint64_t w = w_op + ((t & 1) * N * 256 >> 4);
 #pragma unroll
@@ -281,12 +282,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
       const int cnt = job_at(group).cnt;
       if (!cnt) break;
       job_done(group);
-      hold(kQ + (group & 1), (group >> 1) & 1);
+      need(kQ + (group & 1), (group >> 1) & 1);
       for (int i = 0; i < cnt; ++i, ++tile) {
-        hold(kWideK, tile & 1);
-        hold(kSFree + (tile & 1), ((tile >> 1) & 1) ^ 1);
+        need(kWideK, tile & 1);
+        need(kSFree + (tile & 1), ((tile >> 1) & 1) ^ 1);
         after_sync();
-        if (elected()) {
+        if (elected() && there) {
           const uint32_t to = t_s + (tile & 1) * N;
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
@@ -858,7 +859,11 @@ __global__ void __launch_bounds__(kThreads, 1) many_kernel(const __grid_constant
   before_sync();
   __syncthreads();
   after_sync();
-  if (warp == 2) tmem_free(tmem);
+  if (warp == 2) {
+    report(abort, p.s.status);
+    __syncwarp();
+    tmem_free(tmem);
+  }
 }
 
 template <int D, int kSteps, int kPart>

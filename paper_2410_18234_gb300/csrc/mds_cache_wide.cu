@@ -109,6 +109,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   at += kJobs * sizeof(Job);
   int* abort = reinterpret_cast<int*>(at);
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(abort + 1);
+  // the call's status, for the end: from the parameters there it costs the whole kernel spilled registers
+  uint32_t** status_at = reinterpret_cast<uint32_t**>(abort + 2);
   at += 16;
   Seq<kPrefix>* seqs = reinterpret_cast<Seq<kPrefix>*>(at);
   long long* prefix = reinterpret_cast<long long*>(base);  // before the queries
@@ -118,6 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   const int halves = p.rows_per > half0 ? 2 : 1;
   if (tid == 0) {
     *abort = 0;
+    *status_at = p.s.status;
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar + kKFull + i, 1 + 32);   // the loader's byte count, and its lanes' scale copies
       mbar_init(bar + kKEmpty + i, 4);
@@ -214,19 +217,20 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (++slot == slots) slot = 0, parity ^= 1u;
       }
     }
-    report(abort, s.status);
   } else if (warp == 1) {
-    // ---- products, issued by one thread
+    // ---- products, issued by one thread; none once a wait for them gave up
+    bool there = true;
+    auto need = [&](int b, unsigned parity) { there = wait(bar + b, parity, abort) && there; };
     const uint32_t id_s = instruction(kTile, 0, 0), id_o = instruction(D, 1, 0) | 1u << 16;   // V's contiguous axis is its columns
     const uint64_t q_op = operand(smem_u32(base + W::q), 16), k_op = operand(smem_u32(base + W::wide_k), 16);
     const uint64_t v_op = operand(smem_u32(base + W::wide_v), kTile * 128);
     int tile = 0, group = 0;
     auto sums = [&](int t, int h, bool first) {
-      hold(kP + h, t & 1);
-      if (h == 0) hold(kWideV + (t & 1), (t >> 1) & 1);
-      if (first) hold(kOFree + h, (group & 1) ^ 1);
+      need(kP + h, t & 1);
+      if (h == 0) need(kWideV + (t & 1), (t >> 1) & 1);
+      if (first) need(kOFree + h, (group & 1) ^ 1);
       after_sync();
-      if (elected()) {
+      if (elected() && there) {
         const uint64_t v = v_op + ((t & 1) * (W::kTileBytes * 2) >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)   // 16 slots: 8 columns of weights, 2048 bytes of V
@@ -237,9 +241,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       __syncwarp();
     };
     auto scores = [&](int t, int h, bool last) {
-      if (h == 0) hold(kWideK, t & 1);
+      if (h == 0) need(kWideK, t & 1);
       after_sync();
-      if (elected()) {
+      if (elected() && there) {
         const uint64_t q = q_op + (h * (kHalf * D * 2) >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -256,17 +260,17 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int cnt = job_at(group).cnt;
       if (!cnt) break;
       job_done(group);
-      hold(kQ + (group & 1), (group >> 1) & 1);
+      need(kQ + (group & 1), (group >> 1) & 1);
       for (int i = 0; i < cnt; ++i, ++tile) {
         for (int h = 0; h < halves; ++h) {
           if (kApart) {
-            if (i > 0) hold(kP + h, (tile - 1) & 1);   // the scores before have been read
+            if (i > 0) need(kP + h, (tile - 1) & 1);   // the scores before have been read
             scores(tile, h, i + 1 == cnt);
             if (i > 0) sums(tile - 1, h, i == 1);
           } else {
             if (i > 0) {
               sums(tile - 1, h, i == 1);
-              hold(kPV + h, (tile - 1) & 1);
+              need(kPV + h, (tile - 1) & 1);
             }
             scores(tile, h, i + 1 == cnt);
           }
@@ -275,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       for (int h = 0; h < halves; ++h) {
         sums(tile - 1, h, cnt == 1);
         // the next group's first scores may not overwrite the weights before they are read
-        if (!kApart) hold(kPV + h, (tile - 1) & 1);
+        if (!kApart) need(kPV + h, (tile - 1) & 1);
       }
       ++group;
     }
@@ -573,7 +577,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   before_sync();
   __syncthreads();
   after_sync();
-  if (warp == 2) tmem_free(tmem);
+  if (warp == 2) {
+    report(abort, *status_at);
+    __syncwarp();
+    tmem_free(tmem);
+  }
 }
 
 template <int D>
