@@ -16,12 +16,21 @@ namespace cache {
 namespace {
 
 // Rows of a group up to which the prefix's launch is the transposed kernel for
-// many rows, which has them as columns, so that none are empty.  The wide one
-// has 128 rows a product, filled or not: at 32 rows (16 groups of 8 sequences
-// over 1500 to 12000 tokens) the call takes 131 us with the former and 185 with
-// the latter, at 32 rows of one group (8 over 4100) 37 and 43; at 1024 rows 253
-// and 206, at 576 rows of heads of 64 391 and 366.
-constexpr int kNarrow = 48;
+// many rows, which has them as columns, so that few are empty: as many as it
+// has in one tile.  The wide one has two halves of 128 rows a product, filled
+// or not.  The call in us, transposed / wide, one group over 32768 tokens (a)
+// and 16 over 6000 (b; from 160 rows on 12 over 8000), 4 rows a sequence:
+//   rows   heads of 128: a         b     heads of 64: a        b
+//    32             50 / 66   92 / 133        46 / 53   76 /  98
+//    48             51 / 70   97 / 143        46 / 57   80 / 109
+//    64             57 / 70  108 / 145        53 / 57   96 / 111
+//    96             58 / 72  127 / 167        53 / 58  112 / 124
+//   128             67 / 75  150 / 176        60 / 60  127 / 131
+//   144             68 / 76  154 / 180        62 / 61  129 / 133
+//   160             73 / 81  170 / 169        67 / 62  152 / 127
+//   192             74 / 82  177 / 176        68 / 63  156 / 132
+//   256             84 / 86  217 / 195        76 / 65  191 / 146
+constexpr int kNarrow = kManyRows;
 // Where the caller does not say, prefixes are attended to by themselves where
 // that pays: less is over sooner without the prefix's launch.  In us, shared /
 // not (this call) / mds_cache_attend, 32 heads on 8 of 128 dimensions, G

@@ -37,7 +37,8 @@ namespace {
 
 constexpr int kThreads = 896, kWeigh = 512;   // all, those that weigh
 constexpr int kHalf = 128, kMostRows = kWideRows;
-static_assert(kMostRows == 2 * kHalf, "two halves");
+// Groups of more than kManyRows rows come here, so that every tile of rows has two halves.
+static_assert(kMostRows == 2 * kHalf && kManyRows >= kHalf, "two halves");
 constexpr int kScaleRing = 8;   // tiles whose key scales are held
 constexpr float kMove = 32.f;   // weights stay below 2^32
 
@@ -117,7 +118,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int half0 = min(((p.rows_per + 1) / 2 + 31) & ~31, kHalf);   // rows of the first half, the second's begin
-  const int halves = p.rows_per > half0 ? 2 : 1;
   if (tid == 0) {
     *abort = 0;
     *status_at = p.s.status;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         for (int k = 0; k < kTile / 16; ++k)   // 16 slots: 8 columns of weights, 2048 bytes of V
           mma_ts(t_o + h * D, t_p + h * kHalfP + (k >> 2) * kPartP + (k & 3) * 8, v + k * (2048 >> 4), id_o, !(first && k == 0));
         commit_to(bar + kPV + h);
-        if (h == halves - 1) commit_to(bar + kWideVFree + (t & 1));
+        if (h == 1) commit_to(bar + kWideVFree + (t & 1));
       }
       __syncwarp();
     };
@@ -251,8 +251,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           mma_ss(t_s + h * kTile, q + step, k_op + step, id_s, k > 0);
         }
         commit_to(bar + kS + h);
-        if (h == halves - 1) commit_to(bar + kWideKFree);
-        if (h == halves - 1 && last) commit_to(bar + kQFree);
+        if (h == 1) commit_to(bar + kWideKFree);
+        if (h == 1 && last) commit_to(bar + kQFree);
       }
       __syncwarp();
     };
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       job_done(group);
       need(kQ + (group & 1), (group >> 1) & 1);
       for (int i = 0; i < cnt; ++i, ++tile) {
-        for (int h = 0; h < halves; ++h) {
+        for (int h = 0; h < 2; ++h) {
           if (kApart) {
             if (i > 0) need(kP + h, (tile - 1) & 1);   // the scores before have been read
             scores(tile, h, i + 1 == cnt);
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           }
         }
       }
-      for (int h = 0; h < halves; ++h) {
+      for (int h = 0; h < 2; ++h) {
         sums(tile - 1, h, cnt == 1);
         // the next group's first scores may not overwrite the weights before they are read
         if (!kApart) need(kPV + h, (tile - 1) & 1);
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       {   // a row a lane
         const int r = r0 + lane, h = r >> 7, in = r & (kHalf - 1);
         const int row = job.row0 + (h ? half0 + in : in), node = row / p.g, head = job.h * p.g + row - node * p.g;
-        const bool mine = h ? half0 + in < p.rows_per : in < min(half0, p.rows_per);
+        const bool mine = h ? half0 + in < p.rows_per : in < half0;
         const int64_t from = mine ? query_at<kPrefix>(p, job.b, node, job.live) : kNowhere;
         out[r] = from != kNowhere ? (int)row_at(p, job.b, job.h, row) : -1;   // `prior` has fewer than 2^18 rows
         const int64_t from_row = from != kNowhere ? from + head * p.a.q_head : kNowhere;
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     // ---- weigh: 64 slots of a row of a half a thread
     const int half = (warp - 12) >> 3, part = ((warp - 12) >> 2) & 1, w4 = warp & 3, r = half * kHalf + w4 * 32 + lane;
     const int mine = half ? half0 + w4 * 32 + lane : w4 * 32 + lane;   // row of the tile of rows
-    const bool used = mine - lane < (half ? halves == 2 ? p.rows_per : 0 : min(half0, p.rows_per));   // the warp has rows
+    const bool used = mine - lane < (half ? p.rows_per : half0);   // the warp has rows
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
     const uint32_t s_at = t_s + half * kTile + part * 64 + lanes, o_at = t_o + half * D + part * (D / 2) + lanes;
     const uint32_t p_at = t_p + half * kHalfP + part * kPartP + lanes;
@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int out = row_out[(n & 1) * kMostRows + r];
       float ref = 0.f;
       float2 sum{0.f, 0.f};
-      for (int i = 0; i < cnt && half < halves; ++i, ++tile) {
+      for (int i = 0; i < cnt; ++i, ++tile) {
         hold(kS + half, tile & 1);
         after_sync();
         if (used) {
@@ -547,30 +547,28 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         if (lane == 0) mbar_arrive(bar + kP + half);
       }
       // ---- the group's or piece's end: the sums as they are
-      if (half < halves) {
-        float l = sum.x + sum.y;
-        if (used) l += tell(told++, l);
-        hold(kPV + half, (tile - 1) & 1);
-        after_sync();
-        if (used) {
-          float* to = job.whole() ? prior_of<D>(p, out) : piece_of<D>(p, blockIdx.x, job.off == 0) + mine * R;
+      float l = sum.x + sum.y;
+      if (used) l += tell(told++, l);
+      hold(kPV + half, (tile - 1) & 1);
+      after_sync();
+      if (used) {
+        float* to = job.whole() ? prior_of<D>(p, out) : piece_of<D>(p, blockIdx.x, job.off == 0) + mine * R;
 #pragma unroll 1
-          for (int j = 0; j < D / 32; ++j) {
-            float x[16];
-            tmem_ld16(x, o_at + j * 16);
-            tmem_ld_wait16(x);
-            if (out >= 0) {
+        for (int j = 0; j < D / 32; ++j) {
+          float x[16];
+          tmem_ld16(x, o_at + j * 16);
+          tmem_ld_wait16(x);
+          if (out >= 0) {
 #pragma unroll
-              for (int z = 0; z < 16; z += 4)   // of every four dimensions the order is 0, 2, 1, 3
-                __stcg(reinterpret_cast<float4*>(to + 4 + part * (D / 2) + j * 16 + z), float4{x[z], x[z + 2], x[z + 1], x[z + 3]});
-            }
+            for (int z = 0; z < 16; z += 4)   // of every four dimensions the order is 0, 2, 1, 3
+              __stcg(reinterpret_cast<float4*>(to + 4 + part * (D / 2) + j * 16 + z), float4{x[z], x[z + 2], x[z + 1], x[z + 3]});
           }
-          if (out >= 0 && part == 0) __stcg(reinterpret_cast<float2*>(to), float2{ref, l});
         }
-        before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar + kOFree + half);
+        if (out >= 0 && part == 0) __stcg(reinterpret_cast<float2*>(to), float2{ref, l});
       }
+      before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar + kOFree + half);
       job_done(n);
     }
   }

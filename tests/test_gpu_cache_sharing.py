@@ -105,3 +105,18 @@ def test_unused_places_do_not_count():
         o, always, alone = (c.attend_shared(0, seqs, q, 16, counts=counts, least_saved=x) for x in (None, 0, 2 * 2 * H * D * T))
         assert torch.equal(o, always) and not torch.equal(o, alone) and near(o, alone, largest)
     assert c.status() == (0, "ok")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_groups_at_the_ends_of_tiles(D):
+    """Rows of a group about 16, 48, 96 and 144, where one kernel's tiles or
+    its variants end, and 256: a sequence each, and a remainder of unused places."""
+    rng = np.random.default_rng(D)
+    B = 290
+    c, m = both(B * 2 + 12, 1, D, B, 12, 64)
+    grow(c, m, rng, [0], [333])
+    fork(c, m, [0] * (B - 1), list(range(1, B)))
+    grow(c, m, rng, list(range(B)), [int(x) for x in rng.integers(0, 40, B)])
+    for G in (16, 17, 48, 49, 96, 97, 144, 145, 160, 255, 256, 257, 289):
+        check(c, m, rng, list(range(G)), G, 1, 1, 0, only=[0, G // 2, G - 1])
+        check(c, m, rng, list(range(G - 1)) + [-1], G, 1, 1, 0, only=[0, G // 2, G - 2])
