@@ -584,29 +584,38 @@ template <typename T, int D, int NT, int kPart>
 cudaError_t configure_one() {
   return cudaFuncSetAttribute(few_kernel<T, D, NT, kPart>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
 }
+// Whether the launch of `kPart` is one of these kernels at up to 8 rows: of
+// 16-bit rests mds_cache_rest.cu's is.
+template <typename T, int kPart>
+constexpr bool kOneTile = kPart != kRest || sizeof(T) == 4;
 template <int kPart>
 cudaError_t configure_few() {
   cudaError_t e = configure_one<float, 64, 1, kPart>();
   if (e == cudaSuccess) e = configure_one<float, 64, 2, kPart>();
   if (e == cudaSuccess) e = configure_one<float, 128, 1, kPart>();
   if (e == cudaSuccess) e = configure_one<float, 128, 2, kPart>();
-  if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 64, 1, kPart>();
   if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 64, 2, kPart>();
-  if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 128, 1, kPart>();
   if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 128, 2, kPart>();
+  if constexpr (kOneTile<__nv_bfloat16, kPart>) {
+    if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 64, 1, kPart>();
+    if (e == cudaSuccess) e = configure_one<__nv_bfloat16, 128, 1, kPart>();
+  }
   return e;
+}
+
+template <typename T, int D, int kPart>
+cudaError_t attend_size(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st) {
+  if constexpr (kOneTile<T, kPart>)
+    if ((int64_t)a.n * (a.heads / s.kv_heads) <= 8) return launch_few<T, D, 1, kPart>(s, a, x, sms, st);
+  return launch_few<T, D, 2, kPart>(s, a, x, sms, st);
 }
 
 template <int kPart>
 cudaError_t attend_few(const State& s, const Attend& a, const Shared& x, int sms, cudaStream_t st) {
-  const bool two = (int64_t)a.n * (a.heads / s.kv_heads) > 8;   // tiles of 8 rows
-  if (s.dtype == MDS_F32) {
-    if (s.head_dim == 64) return two ? launch_few<float, 64, 2, kPart>(s, a, x, sms, st) : launch_few<float, 64, 1, kPart>(s, a, x, sms, st);
-    return two ? launch_few<float, 128, 2, kPart>(s, a, x, sms, st) : launch_few<float, 128, 1, kPart>(s, a, x, sms, st);
-  }
-  if (s.head_dim == 64)
-    return two ? launch_few<__nv_bfloat16, 64, 2, kPart>(s, a, x, sms, st) : launch_few<__nv_bfloat16, 64, 1, kPart>(s, a, x, sms, st);
-  return two ? launch_few<__nv_bfloat16, 128, 2, kPart>(s, a, x, sms, st) : launch_few<__nv_bfloat16, 128, 1, kPart>(s, a, x, sms, st);
+  if (s.dtype == MDS_F32)
+    return s.head_dim == 64 ? attend_size<float, 64, kPart>(s, a, x, sms, st) : attend_size<float, 128, kPart>(s, a, x, sms, st);
+  return s.head_dim == 64 ? attend_size<__nv_bfloat16, 64, kPart>(s, a, x, sms, st)
+                          : attend_size<__nv_bfloat16, 128, kPart>(s, a, x, sms, st);
 }
 
 }  // namespace
