@@ -35,34 +35,37 @@ constexpr int kNarrow = kManyRows;
 // that pays: less is over sooner without the prefix's launch.  In us, shared /
 // not (this call) / mds_cache_attend, 32 heads on 8 of 128 dimensions, G
 // sequences a group:
-//   rows 4:    8 sequences, G 8,  4096 tokens ( 56 MB saved)  39 /  39 /  29
-//              2,           G 2, 32768        ( 64 MB)        47 /  61 /  39
+//   rows 4:    8 sequences, G 8,  4096 tokens ( 56 MB saved)  39 /  40 /  29
+//              2,           G 2, 32768        ( 64 MB)        49 /  56 /  38
 //              8,           G 8,  8192        (112 MB)        41 /  49 /  37
-//              8,           G 8, 16384        (224 MB)        47 /  70 /  53
-//             64,           G 64, 2048        (252 MB)        49 /  72 /  66
-//   rows 36:   8,           G 8,  2048        ( 28 MB)        50 /  41 /  31
-//              8,           G 8,  8192        (112 MB)        68 /  63 /  52
-//   rows 132: 16,           G 8,  4096        (112 MB)       137 /  95 /  78
-//             32,           G 32, 4096        (248 MB)       173 / 146 / 127
+//              8,           G 8, 16384        (224 MB)        47 /  70 /  56
+//             64,           G 64, 2048        (252 MB)        49 /  74 /  68
+//   rows 36:   8,           G 8,  2048        ( 28 MB)        49 /  40 /  29
+//              8,           G 8,  8192        (112 MB)        66 /  62 /  51
+//   rows 132: 16,           G 8,  4096        (112 MB)        99 /  95 /  78
+//             32,           G 32, 4096        (248 MB)       153 / 143 / 125
+// The device chooses between the first two, as only it knows what is shared: a
+// call that shares little is slower than mds_cache_attend either way.
 // So many bytes must be saved, by the rows of a sequence (few, many).
 constexpr int64_t kWorthFew = 48 << 20, kWorthMany = 192 << 20;
 // Weights, not bytes, bind rows of more than 16 a sequence, and a row's sums
 // over the prefix are written and read again, whatever its length: of more than
-// 8 rows a sequence each takes so many tokens saved.  Shared / attend, of 64
-// sequences in groups of 4 (a) and 32 in groups of 16 (b), by prefix:
-//   rows 20: a 4096  152 / 166, b 4096  83 /  91
-//   rows 36: a 4096  164 / 166, b 4096  99 /  92, 8192 125 / 152
-//   rows 72: a 4096  257 / 196, b 8192 175 / 176, 16384 251 / 308
-//   rows 80: a 8192  384 / 333, b 8192 178 / 175, 16384 254 / 309
-//   rows 92: a 4096  269 / 199, b 8192 196 / 176
-constexpr int64_t kWorthRow = 100;
+// 8 rows a sequence each takes so many tokens saved.  Shared / not (this call),
+// of 64 sequences in groups of 4 (a, 3/4 of a prefix saved a sequence) and 32 in
+// groups of 16 (b, 15/16), by prefix:
+//   rows 20: a 4096  123 / 179, b 4096  82 / 102
+//   rows 36: a 4096  146 / 183, b 4096  98 / 103, 8192 124 / 166
+//   rows 72: a 4096  248 / 214, 8192 362 / 349, b 4096 134 / 124, 8192 173 / 191
+//   rows 80: a 4096  253 / 216, 8192 366 / 350, b 4096 138 / 123, 8192 175 / 192
+//   rows 92: a 4096  260 / 219, 8192 373 / 352, b 4096 150 / 125, 8192 193 / 193
+constexpr int64_t kWorthRow = 85;
 // From about 100 rows on a tile of rows is full without other sequences'.
 constexpr int kFullRows = 96;
 // So are tiles of 8 or 16 rows of 32-bit queries, which the prefix's launch
-// takes too, from three quarters on.  32 sequences over 16384 tokens: 1 row 61 /
-// 201, 4 rows 117 / 201, 8 rows 195 / 203, 9 rows 220 / 337, 12 rows 281 / 337,
-// 16 rows 359 / 338, 36 rows 789 / 979; 64 over 4096: 8 rows 136 / 125, 12 rows
-// 189 / 197, 16 rows 234 / 199.
+// takes too, from three quarters on.  Shared / mds_cache_attend, 32 sequences
+// over 16384 tokens: 1 row 61 / 199, 4 rows 117 / 199, 8 rows 191 / 200, 9 rows
+// 216 / 324, 12 rows 276 / 324, 16 rows 351 / 325, 36 rows 769 / 939; 64 in
+// groups of 32 over 4096: 8 rows 136 / 124, 12 rows 188 / 191, 16 rows 232 / 192.
 bool full_rows(int dtype, int64_t own) {
   if (dtype != MDS_F32) return own > kFullRows;
   const int64_t tiles = own <= 8 ? 8 : (own + 15) / 16 * 16;
@@ -70,7 +73,7 @@ bool full_rows(int dtype, int64_t own) {
 }
 // What is shared is known to the device alone, and the call without sharing is
 // still four launches: where the tables have no room for savings at which
-// mds_cache_attend falls behind (few rows: 37 us for 41 at 112 MB, 53 for 47 at
+// mds_cache_attend falls behind (few rows: 37 us for 41 at 112 MB, 56 for 47 at
 // 224), the host calls that.
 constexpr int64_t kAloneFew = 160 << 20;
 

@@ -82,9 +82,43 @@ def test_groups_beyond_the_workspace(G, parts):
     assert at == G and c.status() == (0, "ok")
 
 
+@pytest.mark.parametrize("least", [None, 0, 200000])
+def test_captured_calls_in_turns_and_parts(least):
+    """A replay decides again whether it shares: with prefixes of 300 and 430
+    tokens and when all but one sequence of each group have lost theirs."""
+    rng = np.random.default_rng(8)
+    G, n, Hq = 53, 33, 64
+    c, m = forks(rng, 2 * G, G, lambda i: 300 + 130 * i)
+    seqs = ints(range(2 * G))
+    c.reserve(seqs, n)
+    c.append(0, seqs, *(tokens(rng, 2 * G, n, 1, 64) for _ in range(2)))
+    q = 0.02 * tokens(rng, 2 * G, n, Hq, 64)
+    torch.cuda.synchronize()
+    graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(graph):
+        c.attend_shared(0, seqs, q, G, branches=4, least_saved=least, out=out)
+    for step in range(2):
+        want = c.attend_shared(0, seqs, q, G, branches=4, least_saved=least)
+        shared, alone = (c.attend_shared(0, seqs, q, G, branches=4, least_saved=x) for x in (0, 1 << 30))
+        out.fill_(7.0)
+        graph.replay()
+        assert torch.equal(out, want)
+        if step == 0:
+            assert torch.equal(alone, c.attend(0, seqs, q, branches=4)) and not torch.equal(shared, alone)
+            assert torch.equal(want, shared if least is not None else alone)
+            others = ints([x for x in range(2 * G) if x % G])
+            c.truncate(others, ints([40] * len(others)))
+            c.reserve(others, n)
+            c.append(0, others, *(tokens(rng, len(others), n, 1, 64) for _ in range(2)))
+        else:   # no tile of 128 tokens is shared any more
+            assert torch.equal(want, alone if least is None or least else shared)
+            assert near(shared, alone, c.read(0, seqs, None, 600)[1].abs().max())
+    assert c.status() == (0, "ok")
+
+
 def test_unused_places_do_not_count():
-    """By default 12 rows a sequence take 1200 tokens of savings a sequence:
-    8192 of two live ones are enough, in a list of 16 too."""
+    """By default 12 rows a sequence take some 1000 tokens of savings a live
+    sequence: 8192 of two are enough, in a list of 16 too."""
     H, D, T = 32, 128, 8192
     c = cache.Cache(1, T // 128 + 4, H, D, 4, 80, page_tokens=128)
     g = torch.Generator(device=DEV).manual_seed(5)
