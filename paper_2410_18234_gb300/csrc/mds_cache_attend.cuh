@@ -10,13 +10,14 @@
 // group cut between blocks is joined by the last of them to finish, which
 // adds the pieces in their order: results do not depend on timing.
 //
-// Parts.  A call is one launch (kAll), or two where sequences share a prefix:
-// kPrefix takes every group of sequences as one of `members` times as many
-// nodes over the prefix's tiles, and leaves each row's reference, normaliser
-// and sums in `prior`, or in pieces that a launch of its own joins (a few
-// groups may be cut into many pieces, which one block each would be long
-// over); kRest takes the sequences over the tiles behind it, and
-// joins what it finds there like one more piece.
+// Parts.  A call is one launch (kAll), or four where sequences share a prefix
+// (more in several turns, mds_cache_shared.cu).  The first finds what is
+// shared.  kPrefix takes every group of sequences as one of `members` times as
+// many nodes over the prefix's tiles, and leaves each row's reference,
+// normaliser and sums in `prior`, or in pieces that the third launch joins (a
+// few groups may be cut into many pieces, which one block each would be long
+// over).  kRest takes the sequences over the tiles behind it, and joins what it
+// finds there like one more piece.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -22,10 +22,13 @@
 // is stored is the quantiser's answer on the exact rotation.
 //
 // What binds it.  Queries: memory.  4 prompts of 4099 tokens, 32 heads of 128,
-// bfloat16 (268 MB): 47 us, 5.7 TB/s, 84 % of a copy.  Keys and values: the
-// quantiser's instructions (half of the issue slots) and its registers.  256
-// trees of 33 nodes on 8 heads with 32 heads of queries (152 MB): 53 us, 2.9
-// TB/s; every key in two floats would take 12 us more.
+// bfloat16 (268 MB): 47 us, 5.7 TB/s, 84 % of a copy; in 32 bits 94.  Keys and
+// values: the quantiser's instructions (half of the issue slots) and its
+// registers.  256 trees of 33 nodes on 8 heads with 32 heads of queries (194
+// MB, the begun blocks with them): 53 us, 3.7 TB/s; 4 prompts of 4099 tokens of
+// the same heads (369 MB): 80 us, 4.6 TB/s, in 32 bits with 16 heads of queries
+// and ragged lengths (283 MB) 74 us.  Every key in two floats would take 12 us
+// more on the trees.
 #include <cfloat>
 
 #include "mds_cache_quant.cuh"

@@ -23,11 +23,11 @@
 //
 // A tile of 256 rows takes some 4800 cycles, of which the products are issued
 // for 2400; the rest are waits for weights (770), a group's keys and queries
-// (620), sums that are not done (520) and values (250).  1024 rows on each of 8
-// heads of 128 dimensions over 32768 tokens (137 GFLOP): 150 us, 0.92 PFLOP/s,
-// half of the library's plain product.  The whole call, rests with it, took 261
+// (620), sums that are not done (520) and values (250; clock stamps of an
+// earlier build, 4 % off).  1024 rows on each of 8 heads of 128 dimensions over
+// 32768 tokens (137 GFLOP): 148 us, 0.93 PFLOP/s, half of the library's plain product.  The whole call, rests with it, took 261
 // us with a thread a row (too few warps to fill the exponentials' unit), 216
-// with two and all widening in the same warps, and takes 206.
+// with two and all widening in the same warps, and takes 200.
 #include "mds_cache_tensor.cuh"
 
 namespace mds {
